@@ -273,6 +273,86 @@ int fwg_waits(const fwg_handle *h);
  * FWG_OK after the synchronisation.  The mark is cleared by fwg_reset_queues. */
 int fwg_device_status(fwg_handle *h);
 
+/* ---------------------------------------------------------------------------
+ * Token operators: the two ends of a token model, for any vocabulary and width.
+ *
+ *   tokens -> fwg_embed -> (a stack) -> fwg_norm_quant -> fwg_matmul_quant -> logits -> fwg_log_probs
+ *
+ * and, for training, fwg_log_probs_grad and fwg_embed_grad.  fwg_log_probs takes the logits of
+ * fwg_teacher_forced and its like as they are.  The calls need no handle.  As above, everything is checked on
+ * the host before anything is enqueued, nothing is allocated and nothing waits: the work is enqueued on
+ * hip_stream (a hipStream_t, NULL = default stream) of the current device, and a call may be captured into a
+ * HIP graph.  A workspace holds nothing between calls; it must be 256-byte aligned and stay untouched until the
+ * call's work is done, and calls that may overlap need one each.  Where a *_workspace call answers 0 bytes,
+ * workspace may be NULL.
+ *
+ * Types are FWG_F32 or FWG_BF16.  Matrices are rows of consecutive elements, `stride` elements apart, and may
+ * start at any element; an input's stride may be 0 (one row repeated), an output's rows must not overlap.
+ * Outputs must not overlap inputs except where a call says so.  Zero rows are a no-op.  Sums, softmax statistics
+ * and norms are float32 (8-bit products: exact 32-bit integers), rounded once, to nearest even, where an output is
+ * bf16, and are added up in an order that depends on the sizes only: the same call gives the same bits.
+ * A token outside [0, vocab) is padding: it names no row and has log probability 0.
+ * ------------------------------------------------------------------------- */
+
+/* out[i] = scale * table[tokens[i]], i in [0, n); a padding token's row is zero.  table: [vocab][channels] of
+ * dtype, out: [n][channels] of out_dtype. */
+int fwg_embed(int32_t dtype, int32_t out_dtype, int64_t n, int32_t vocab, int32_t channels, const void *table,
+              int64_t table_stride, const int32_t *tokens, float scale, void *out, int64_t out_stride,
+              void *hip_stream);
+
+/* The table's gradient: out[v] = scale * sum over i with tokens[i] = v of grad[i], for every v in [0, vocab) (rows
+ * without a token become zero).  grad: [n][channels] of dtype, out: [vocab][channels] of out_dtype.  The tokens
+ * are sorted and each row's positions added up in a fixed order: no atomic additions, the same bits every time.
+ * n <= 2^30; n = 0 clears out. */
+int fwg_embed_grad_workspace(int64_t n, int32_t vocab, int32_t channels, size_t *bytes);
+int fwg_embed_grad(int32_t dtype, int32_t out_dtype, int64_t n, int32_t vocab, int32_t channels, const void *grad,
+                   int64_t grad_stride, const int32_t *tokens, float scale, void *out, int64_t out_stride,
+                   void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Rows in 8 bits: scale[r] = max|x[r]| / 127, q[r] = x[r] / scale[r] to the nearest whole number (ties to even),
+ * -127 .. 127.  For weights: one scale per output channel.  A row whose largest magnitude is below 2^-100 has
+ * scale and q of 0; one with a NaN or an infinity has scale NaN and q of 0.  1 <= channels <= 32768. */
+int fwg_quant_rows(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride, int8_t *q,
+                   int64_t q_stride, float *scale, void *hip_stream);
+
+/* Residual addition, RMS norm and rows in 8 bits: h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain, q and
+ * scale of y as in fwg_quant_rows (zero also where every |h gain| is below 2^-120; NaN also where the sum of
+ * squares leaves float32's range).  residual NULL: none; gain (float32 [channels]) NULL: ones.  Optional outputs:
+ * summed, h rounded to dtype (may be x or residual itself: the residual stream in place), and values, q * scale
+ * in bf16, for consumers that read bf16.  The norm is taken of the unrounded sum. */
+int fwg_norm_quant(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride,
+                   const void *residual, int64_t residual_stride, const float *gain, float eps, void *summed,
+                   int64_t summed_stride, int8_t *q, int64_t q_stride, float *scale, uint16_t *values,
+                   int64_t values_stride, void *hip_stream);
+
+/* out[m][n] = (sum over k of x[m][k] w[n][k]) * x_scale[m] * w_scale[n] + bias[n]: x: int8 [rows][inner], w: int8
+ * [outputs][inner] (PyTorch's layout), bias float32 or NULL, out: [rows][outputs] of out_dtype.  The sum is exact:
+ * 1 <= inner <= 131071.  rows <= 2^30. */
+int fwg_matmul_quant_workspace(int64_t rows, int32_t outputs, int32_t inner, size_t *bytes);
+int fwg_matmul_quant(int32_t out_dtype, int64_t rows, int32_t outputs, int32_t inner, const int8_t *x,
+                     int64_t x_stride, const float *x_scale, const int8_t *w, int64_t w_stride, const float *w_scale,
+                     const float *bias, void *out, int64_t out_stride, void *workspace, size_t ws_bytes,
+                     void *hip_stream);
+
+/* Per row of logits [rows][vocab] (of dtype): lse = log sum exp, logp = log probability of tokens[r], entropy (in
+ * nats), and the `top` most probable tokens (0 <= top <= 64, <= vocab) with their log probabilities, ordered by
+ * (logit descending, token ascending): top_ids, top_logp: [rows][top].  -inf is a masked token (probability 0).
+ * A row of -inf only has lse and log probabilities -inf, entropy 0 and the lowest tokens as alternatives.  A
+ * row with a NaN or +inf has NaN statistics; among the alternatives NaN ranks as -inf. */
+int fwg_log_probs_workspace(int32_t dtype, int64_t rows, int32_t vocab, int32_t top, size_t *bytes);
+int fwg_log_probs(int32_t dtype, int64_t rows, int32_t vocab, const void *logits, int64_t logits_stride,
+                  const int32_t *tokens, int32_t top, float *logp, float *entropy, float *lse, int32_t *top_ids,
+                  float *top_logp, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* The logits' gradient: out[r][j] = g (1[j = tokens[r]] - p_j) - gH p_j (log p_j + H), with p_j = exp(logit - lse[r]),
+ * H = entropy[r], g = grad_logp[r] (0 for padding), gH = grad_entropy[r]; grad_entropy NULL: 0 (entropy may then be
+ * NULL too).  lse and entropy as fwg_log_probs left them.  out: of the logits' dtype; may be the logits themselves
+ * (the same address and stride).  Rows of -inf only have gradient zero.  p_j carries lse's own rounding (2^-24 of
+ * |lse|): mask tokens with -inf, not with the type's lowest value, where a whole row may be masked. */
+int fwg_log_probs_grad(int32_t dtype, int64_t rows, int32_t vocab, const void *logits, int64_t logits_stride,
+                       const int32_t *tokens, const float *lse, const float *entropy, const float *grad_logp,
+                       const float *grad_entropy, void *out, int64_t out_stride, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,11 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfwg.so")
 EXPORTED = ["fwg_workspace_size", "fwg_create", "fwg_reset_queues", "fwg_generate", "fwg_generate_noalloc",
             "fwg_teacher_forced",
             "fwg_step_forced", "fwg_teacher_forced_parallel", "fwg_prime", "fwg_generate_naive", "fwg_naive_nodes",
-            "fwg_destroy", "fwg_last_error", "fwg_regime", "fwg_waits", "fwg_device_status"]
+            "fwg_destroy", "fwg_last_error", "fwg_regime", "fwg_waits", "fwg_device_status",
+            # the token operators (ops.py)
+            "fwg_embed", "fwg_embed_grad_workspace", "fwg_embed_grad", "fwg_quant_rows", "fwg_norm_quant",
+            "fwg_matmul_quant_workspace", "fwg_matmul_quant", "fwg_log_probs_workspace", "fwg_log_probs",
+            "fwg_log_probs_grad"]
 
 
 class FwgError(RuntimeError):
@@ -56,7 +60,7 @@ def load_library(path: Optional[str] = None):
     if not os.path.exists(p):
         raise FileNotFoundError(f"{p} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
     L = ctypes.CDLL(p)
-    vp, i32 = ctypes.c_void_p, ctypes.c_int32
+    vp, i32, i64, sz, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
     L.fwg_workspace_size.argtypes = [ctypes.POINTER(fwg_desc), ctypes.POINTER(ctypes.c_size_t)]
     L.fwg_create.argtypes = [ctypes.POINTER(fwg_desc), ctypes.POINTER(fwg_weights), vp, ctypes.c_size_t, vp,
                              ctypes.POINTER(vp)]
@@ -76,10 +80,20 @@ def load_library(path: Optional[str] = None):
     L.fwg_waits.argtypes = [vp]
     L.fwg_waits.restype = ctypes.c_int
     L.fwg_device_status.argtypes = [vp]
+    L.fwg_embed.argtypes = [i32, i32, i64, i32, i32, vp, i64, vp, f32, vp, i64, vp]
+    L.fwg_embed_grad_workspace.argtypes = [i64, i32, i32, ctypes.POINTER(sz)]
+    L.fwg_embed_grad.argtypes = [i32, i32, i64, i32, i32, vp, i64, vp, f32, vp, i64, vp, sz, vp]
+    L.fwg_quant_rows.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp]
+    L.fwg_norm_quant.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp, i64, vp]
+    L.fwg_matmul_quant_workspace.argtypes = [i64, i32, i32, ctypes.POINTER(sz)]
+    L.fwg_matmul_quant.argtypes = [i32, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+    L.fwg_log_probs_workspace.argtypes = [i32, i64, i32, i32, ctypes.POINTER(sz)]
+    L.fwg_log_probs.argtypes = [i32, i64, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.fwg_log_probs_grad.argtypes = [i32, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
     for name in ["fwg_workspace_size", "fwg_create", "fwg_reset_queues", "fwg_generate", "fwg_generate_noalloc",
                  "fwg_teacher_forced",
                  "fwg_step_forced", "fwg_teacher_forced_parallel", "fwg_prime", "fwg_generate_naive",
-                 "fwg_naive_nodes", "fwg_destroy", "fwg_device_status"]:
+                 "fwg_naive_nodes", "fwg_destroy", "fwg_device_status"] + EXPORTED[EXPORTED.index("fwg_embed"):]:
         getattr(L, name).restype = ctypes.c_int
     if path is None:
         _lib = L

@@ -14,12 +14,16 @@ SOURCES = [os.path.join(CSRC, "fwg_host.cpp"), os.path.join(CSRC, "fwg_kernels.h
            os.path.join(CSRC, "fwg_mfma.hip"), os.path.join(CSRC, "fwg_parallel.hip"),
            os.path.join(CSRC, "fwg_parstack.hip"), os.path.join(CSRC, "fwg_parhead.hip"),
            os.path.join(CSRC, "fwg_wave.hip"), os.path.join(CSRC, "fwg_split.hip"),
-           os.path.join(CSRC, "fwg_chain.hip"), os.path.join(CSRC, "fwg_wide.hip")]
+           os.path.join(CSRC, "fwg_chain.hip"), os.path.join(CSRC, "fwg_wide.hip"),
+           os.path.join(CSRC, "fwg_ops.cpp"), os.path.join(CSRC, "fwg_embed.hip"),
+           os.path.join(CSRC, "fwg_normq.hip"), os.path.join(CSRC, "fwg_matmulq.hip"),
+           os.path.join(CSRC, "fwg_logprob.hip")]
 HEADERS = [os.path.join(ROOT, "include", "fwg.h"), os.path.join(CSRC, "fwg_internal.h"),
            os.path.join(CSRC, "fwg_sample.h"), os.path.join(CSRC, "fwg_valu.h"),
            os.path.join(CSRC, "fwg_wave.h"), os.path.join(CSRC, "fwg_par.h"), os.path.join(CSRC, "fwg_mfma_dev.h"),
            os.path.join(CSRC, "fwg_bf16.h"), os.path.join(CSRC, "fwg_chain.h"),
-           os.path.join(CSRC, "fwg_xchg.h"), os.path.join(CSRC, "fwg_wide.h")]
+           os.path.join(CSRC, "fwg_xchg.h"), os.path.join(CSRC, "fwg_wide.h"),
+           os.path.join(CSRC, "fwg_ops.h"), os.path.join(CSRC, "fwg_ops_dev.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,302 @@
+"""The token operators of libfwg.so (include/fwg.h) on torch tensors: embedding lookup and its gradient, 8-bit
+rows with or without RMS norm, the 8-bit product, log probabilities and their gradient.
+
+Argument marshalling only, as in binding.py: every call checks its tensors, enqueues the library's kernels on the
+current stream of the current device and returns without waiting.  Matrices may have any number of leading
+dimensions as long as their rows lie evenly apart (views of consecutive rows, every n-th row, expanded rows as
+inputs); elements of a row are consecutive.  Nothing is copied to make an argument fit: what does not fit is
+refused (TypeError, ValueError; sizes that the library refuses raise FwgError).  `out` takes the results' tensors
+of an earlier call, so that a loop allocates nothing but the workspaces that some calls take from torch's
+allocator.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from .binding import FWG_BF16, FWG_F32, FwgError, _check, load_library  # noqa: F401 (FwgError: what calls raise)
+
+_TYPES = {torch.float32: FWG_F32, torch.bfloat16: FWG_BF16}
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        _lib = load_library()
+    return _lib
+
+
+def _stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _on_device(name: str, t) -> None:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} is not a tensor")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}: the call runs on the current device, "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def _typed(name: str, t, dtype) -> None:
+    _on_device(name, t)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}: {dtype} is wanted")
+
+
+def _matrix(name: str, t, out: bool = False):
+    """(element type, rows, width, stride) of a float32 or bfloat16 tensor seen as rows."""
+    _on_device(name, t)
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"{name} is {t.dtype}: float32 or bfloat16 is wanted")
+    return (kind,) + _rows(name, t, out)
+
+
+def _rows(name: str, t, out: bool = False):
+    """(rows, width, stride) of a tensor seen as rows of its last dimension."""
+    shape = t.shape
+    if not shape:
+        raise ValueError(f"{name} has no dimensions: rows are wanted")
+    width = shape[-1]
+    if width > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements of a row have to be consecutive (stride {t.stride(-1)})")
+    if t.dim() == 2:
+        rows, stride = shape[0], t.stride(0)
+    else:
+        rows, stride = 1, width
+        for n, s in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+            if n == 1:
+                continue
+            if rows > 1 and s != rows * stride:
+                raise ValueError(f"{name}: the rows of shape {tuple(shape)}, strides {t.stride()} do not lie evenly apart")
+            if rows == 1:
+                stride = s
+            rows *= n
+    if rows <= 1:
+        stride = width
+    elif out and stride < width:
+        raise ValueError(f"{name}: its rows overlap (stride {stride}, width {width})")
+    return rows, width, stride
+
+
+def _vector(name: str, t, n: int, dtype) -> int:
+    """Address of `n` consecutive elements."""
+    _typed(name, t, dtype)
+    if t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} elements: {n} are wanted")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} has to be contiguous")
+    return t.data_ptr()
+
+
+def _same(name: str, got: int, want: int, what: str) -> None:
+    if got != want:
+        raise ValueError(f"{name} has {got} {what}: {want} are wanted")
+
+
+def _shaped(name: str, t, shape) -> None:
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is wanted")
+
+
+def _workspace(need: int):
+    return torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+
+
+def _bytes(size, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(size(*args, ctypes.byref(n)))
+    return n.value
+
+
+def embed(table, tokens, scale: float = 1.0, out=None):
+    """scale * table[tokens].  table: float32 or bfloat16 [vocab][channels]; tokens: int32, any shape, contiguous;
+    a token outside [0, vocab) is padding and gives a zero row.  out: [*tokens.shape][channels], float32 or bfloat16
+    (default: of the table's type)."""
+    kind, vocab, channels, stride = _matrix("table", table)
+    _same("table", table.dim(), 2, "dimensions")
+    n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
+    ids = _vector("tokens", tokens, n, torch.int32)
+    shape = tokens.shape + (channels,)
+    if out is None:
+        out = torch.empty(shape, dtype=table.dtype, device=table.device)
+    okind, _, _, ostride = _matrix("out", out, True)
+    _shaped("out", out, shape)
+    _check(_library().fwg_embed(kind, okind, n, vocab, channels, table.data_ptr(), stride, ids, scale, out.data_ptr(),
+                                ostride, _stream()))
+    return out
+
+
+def embed_grad(grad, tokens, vocab: int, scale: float = 1.0, out=None):
+    """The gradient of embed() with respect to the table: out[v] = scale * (sum of grad over the positions of token
+    v), zero where there is none.  grad: float32 or bfloat16 [*tokens.shape][channels] (rows may be expanded); out:
+    float32 (default) or bfloat16 [vocab][channels].  Sums in float32 in an order that depends on the tokens only:
+    the same bits every time."""
+    kind, rows, channels, stride = _matrix("grad", grad)
+    n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
+    ids = _vector("tokens", tokens, n, torch.int32)
+    _shaped("grad", grad, tokens.shape + (channels,))
+    if out is None:
+        out = torch.empty((vocab, channels), dtype=torch.float32, device=grad.device)
+    okind, _, _, ostride = _matrix("out", out, True)
+    _shaped("out", out, (vocab, channels))
+    lib = _library()
+    need = _bytes(lib.fwg_embed_grad_workspace, n, vocab, channels)
+    ws = _workspace(need)
+    _check(lib.fwg_embed_grad(kind, okind, n, vocab, channels, grad.data_ptr(), stride, ids, scale, out.data_ptr(),
+                              ostride, None if ws is None else ws.data_ptr(), need, _stream()))
+    return out
+
+
+class QuantRows(NamedTuple):
+    """8-bit rows: row r stands for q[r] * scale[r]."""
+    q: torch.Tensor
+    scale: torch.Tensor
+
+
+class NormQuant(NamedTuple):
+    """8-bit rows of a norm, the residual stream after the addition, and the values that the rows stand for in
+    bfloat16 (None where they were not asked for)."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    summed: Optional[torch.Tensor]
+    values: Optional[torch.Tensor]
+
+
+def quant_rows(x, out=None) -> QuantRows:
+    """Rows in 8 bits with a scale each: scale = max|x| / 127, q = x / scale to the nearest (ties to even).  For
+    weights [outputs][inner] these are matmul_quant's w and w_scale."""
+    kind, rows, width, stride = _matrix("x", x)
+    if out is None:
+        out = QuantRows(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+                        torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device))
+    q, scale = out
+    _typed("out.q", q, torch.int8)
+    _shaped("out.q", q, x.shape)
+    _check(_library().fwg_quant_rows(kind, rows, width, x.data_ptr(), stride, q.data_ptr(),
+                                     _rows("out.q", q, True)[2], _vector("out.scale", scale, rows, torch.float32),
+                                     _stream()))
+    return out if isinstance(out, QuantRows) else QuantRows(*out)
+
+
+def norm_quant(x, gain=None, residual=None, eps: float = 1e-6, values: bool = False, out=None) -> NormQuant:
+    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain; y's rows in 8 bits as in quant_rows.  x, residual:
+    float32 or bfloat16 [..., channels]; gain: float32 [channels].  Results: q, scale, `summed` (h, rounded to x's
+    type; with a residual only) and, where values is true, `values` (q * scale in bfloat16).  out: a NormQuant or
+    the four tensors (None: not wanted); out's `summed` may be x or residual itself."""
+    kind, rows, width, stride = _matrix("x", x)
+    rp, rstride = None, 0
+    if residual is not None:
+        _typed("residual", residual, x.dtype)
+        _shaped("residual", residual, x.shape)
+        rp, rstride = residual.data_ptr(), _rows("residual", residual)[2]
+    if out is None:
+        out = NormQuant(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+                        torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device),
+                        None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device),
+                        torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
+    q, scale, summed, vals = out
+    _typed("out.q", q, torch.int8)
+    _shaped("out.q", q, x.shape)
+    sp, sstride, vp, vstride = None, 0, None, 0
+    if summed is not None:
+        _typed("out.summed", summed, x.dtype)
+        _shaped("out.summed", summed, x.shape)
+        sp, sstride = summed.data_ptr(), _rows("out.summed", summed, True)[2]
+    if vals is not None:
+        _typed("out.values", vals, torch.bfloat16)
+        _shaped("out.values", vals, x.shape)
+        vp, vstride = vals.data_ptr(), _rows("out.values", vals, True)[2]
+    _check(_library().fwg_norm_quant(kind, rows, width, x.data_ptr(), stride, rp, rstride,
+                                     None if gain is None else _vector("gain", gain, width, torch.float32), eps, sp,
+                                     sstride, q.data_ptr(), _rows("out.q", q, True)[2],
+                                     _vector("out.scale", scale, rows, torch.float32), vp, vstride, _stream()))
+    return out if isinstance(out, NormQuant) else NormQuant(*out)
+
+
+def matmul_quant(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=None):
+    """(x @ w.T) * x_scale[:, None] * w_scale + bias, the product of the 8-bit integers exact.  x: int8
+    [..., inner] with x_scale float32 [...]; w: int8 [outputs][inner] with w_scale float32 [outputs]; bias: float32
+    [outputs].  out: [..., outputs] of dtype (float32 or bfloat16)."""
+    _typed("x", x, torch.int8)
+    _typed("w", w, torch.int8)
+    rows, inner, stride = _rows("x", x)
+    _same("w", w.dim(), 2, "dimensions")
+    outputs, winner, wstride = _rows("w", w)
+    _same("w", winner, inner, "inner elements")
+    shape = x.shape[:-1] + (outputs,)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+    okind, _, _, ostride = _matrix("out", out, True)
+    _shaped("out", out, shape)
+    lib = _library()
+    need = _bytes(lib.fwg_matmul_quant_workspace, rows, outputs, inner)
+    ws = _workspace(need)
+    _check(lib.fwg_matmul_quant(okind, rows, outputs, inner, x.data_ptr(), stride,
+                                _vector("x_scale", x_scale, rows, torch.float32), w.data_ptr(), wstride,
+                                _vector("w_scale", w_scale, outputs, torch.float32),
+                                None if bias is None else _vector("bias", bias, outputs, torch.float32),
+                                out.data_ptr(), ostride, None if ws is None else ws.data_ptr(), need, _stream()))
+    return out
+
+
+class LogProbs(NamedTuple):
+    """Per row: the given token's log probability, the entropy (nats), log sum exp, and the most probable tokens
+    with their log probabilities ([..., top])."""
+    logp: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: torch.Tensor
+    top_logp: torch.Tensor
+
+
+def log_probs(logits, tokens, top: int = 0, out=None) -> LogProbs:
+    """Log probabilities of tokens (int32 [...]) under logits (float32 or bfloat16 [..., vocab]), with entropy, log
+    sum exp and the `top` (at most 64) most probable tokens, equal logits in the order of the tokens.  -inf masks
+    a token; a token outside [0, vocab) is padding and has log probability 0."""
+    kind, rows, vocab, stride = _matrix("logits", logits)
+    lead = logits.shape[:-1]
+    ids = _vector("tokens", tokens, rows, torch.int32)
+    _shaped("tokens", tokens, lead)
+    if out is None:
+        def new(dtype, *more):
+            return torch.empty(lead + more, dtype=dtype, device=logits.device)
+        out = LogProbs(new(torch.float32), new(torch.float32), new(torch.float32), new(torch.int32, top),
+                       new(torch.float32, top))
+    logp, entropy, lse, top_ids, top_logp = out
+    lib = _library()
+    need = _bytes(lib.fwg_log_probs_workspace, kind, rows, vocab, top)
+    ws = _workspace(need)
+    _check(lib.fwg_log_probs(kind, rows, vocab, logits.data_ptr(), stride, ids, top,
+                             _vector("out.logp", logp, rows, torch.float32),
+                             _vector("out.entropy", entropy, rows, torch.float32),
+                             _vector("out.lse", lse, rows, torch.float32),
+                             _vector("out.top_ids", top_ids, rows * top, torch.int32),
+                             _vector("out.top_logp", top_logp, rows * top, torch.float32),
+                             None if ws is None else ws.data_ptr(), need, _stream()))
+    return out if isinstance(out, LogProbs) else LogProbs(*out)
+
+
+def log_probs_grad(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, out=None):
+    """The gradient of log_probs() with respect to the logits, from the gradients of logp and (optional) entropy;
+    lse and entropy as log_probs() returned them (entropy may be None without grad_entropy).  out: of the logits'
+    shape and type; may be the logits themselves."""
+    kind, rows, vocab, stride = _matrix("logits", logits)
+    ids = _vector("tokens", tokens, rows, torch.int32)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _typed("out", out, logits.dtype)
+    _shaped("out", out, logits.shape)
+    if grad_entropy is not None and entropy is None:
+        raise ValueError("grad_entropy is given without entropy")
+    _check(_library().fwg_log_probs_grad(
+        kind, rows, vocab, logits.data_ptr(), stride, ids, _vector("lse", lse, rows, torch.float32),
+        None if entropy is None else _vector("entropy", entropy, rows, torch.float32),
+        _vector("grad_logp", grad_logp, rows, torch.float32),
+        None if grad_entropy is None else _vector("grad_entropy", grad_entropy, rows, torch.float32),
+        out.data_ptr(), _rows("out", out, True)[2], _stream()))
+    return out
