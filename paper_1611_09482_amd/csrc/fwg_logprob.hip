@@ -6,9 +6,9 @@
 // block and the parts of a row in a fixed order.  Differences are taken before the scaling by log2(e), so
 // logits near the type's limits (masks of the lowest value) neither overflow nor lose their place.
 //
-// The k alternatives are a list of (logit, index), one entry per lane in order (logit descending, index
-// ascending).  A batch whose largest logit does not pass the list's last entry costs one comparison per
-// lane; otherwise the batch's best elements are inserted one at a time, k at most.
+// The k alternatives are a list with one entry per lane in order (logit descending, index ascending).  A batch
+// whose largest logit does not pass the list's last entry costs one comparison per lane; otherwise the elements
+// that pass it are inserted one at a time.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -21,7 +21,6 @@ namespace lpr {
 
 using namespace opd;
 
-constexpr int kNoIndex = 0x7fffffff;
 constexpr int kWaves = 4, kThreadsLp = 64 * kWaves;
 constexpr float kFloor = -200.f;  // 2^-200 is zero in float32: products with it stay zero and finite
 
@@ -57,58 +56,79 @@ __device__ __forceinline__ Acc wave_join(Acc a) {
   return Acc{m, wave_sum(a.s), wave_sum(a.u)};
 }
 
-struct Entry {
-  float v;
-  int i;
-};
-// (v descending, index ascending)
-__device__ __forceinline__ bool before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+// An alternative as one double: the logit's bits are the high word, its place the low one, so that doubles
+// compare as (logit descending, index ascending).  Every float but NaN (which ranks as -inf), -inf included, makes a
+// finite double; for negative numbers a larger low word is a smaller double, so the place is stored as it is there
+// and inverted elsewhere.
+__device__ __forceinline__ double key_of(float z, int i) {
+  const int h = __float_as_int(fmaxf(z, -kInf) + 0.f);  // NaN out, one zero
+  return __hiloint2double(h, i ^ ~(h >> 31));
+}
+__device__ __forceinline__ double below(float v) { return key_of(v, -1); }  // below every key of logit v
+__device__ __forceinline__ float value_of(double key) { return __int_as_float(__double2hiint(key)); }
+__device__ __forceinline__ int index_of(double key) { return __double2loint(key) ^ ~(__double2hiint(key) >> 31); }
+__device__ __forceinline__ double lane_d(double v, int l) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
+}
+template <int CTRL> __device__ __forceinline__ double dpp_d(double v) {
+  return __hiloint2double(dpp_i<CTRL>(__double2hiint(v)), dpp_i<CTRL>(__double2loint(v)));
+}
+// Largest key of each row of 16 lanes, in all of its lanes; and of the wavefront.
+__device__ __forceinline__ double row16_max(double v) {
+  v = fmax(v, dpp_d<0xB1>(v));
+  v = fmax(v, dpp_d<0x4E>(v));
+  v = fmax(v, dpp_d<0x141>(v));
+  return fmax(v, dpp_d<0x140>(v));
+}
+__device__ __forceinline__ double wave_max_d(double v) {
+  v = row16_max(v);
+  return fmax(fmax(lane_d(v, 0), lane_d(v, 16)), fmax(lane_d(v, 32), lane_d(v, 48)));
+}
 
-// Puts the lanes' candidates z[j] with index idx(j) (kNoIndex: none; NaN ranks as -inf) that come before
-// the list's entry k - 1 into the list.
-template <int N, typename Index>
-__device__ __forceinline__ void insert_batch(Entry &list, int k, const float (&z)[N], Index idx) {
-  const int lane = threadIdx.x & 63;
-  float lv = -kInf;  // the last one taken; first none
-  int li = -1;
-  bool mine = true;  // my best has to be found anew
-  Entry best{-kInf, kNoIndex};
-  bool first = true;
-  for (int n = 0; n < k; ++n) {
-    if (mine) {
-      best = Entry{-kInf, kNoIndex};
+// The list: lane i holds the i-th best key so far.  Puts w (the same in every lane) in its place.
+__device__ __forceinline__ void insert(double &list, double w) {
+  // lane i's left neighbour; lane 0's is above everything
+  const double left = __hiloint2double(__builtin_amdgcn_update_dpp(0x7fe00000, __double2hiint(list), 0x138, 0xF, 0xF, false),
+                                       __builtin_amdgcn_update_dpp(0, __double2loint(list), 0x138, 0xF, 0xF, false));
+  list = fmax(list, fmin(left, w));
+}
+
+// The k-th largest of the lanes' values (k <= 64): the smallest of those that fewer than k exceed.
+__device__ __forceinline__ float kth_of_lanes(float v, int k) {
+  int over = 0;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float v = z[j] == z[j] ? z[j] : -kInf;
-        const int i = idx(j);
-        if (i != kNoIndex && (first || before(lv, li, v, i)) && before(v, i, best.v, best.i)) best = Entry{v, i};
+  for (int l = 0; l < 64; ++l) over += mfd::lane_f(v, l) > v;
+  return -wave_max(over < k ? -v : -kInf);
+}
+
+// Puts the keys of a batch that come before the list's entry k - 1 into the list.  best: the lane's largest logit.
+// Where many lanes have one (the first batch, above all), the k-th largest of the lanes' best is a bound below which
+// nothing can be among the k, and keeps the insertions to little more than k.
+template <int N, typename Index>
+__device__ __forceinline__ void take(double &list, int k, const float (&z)[N], float best, Index idx) {
+  double least = lane_d(list, k - 1);
+  if (__popcll(__ballot(best > value_of(least))) > 8) least = fmax(least, below(kth_of_lanes(best, k)));
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = idx(j);
+    const double key = i >= 0 ? key_of(z[j], i) : below(-kInf);
+    for (unsigned long long m = __ballot(key > least); m; m &= m - 1) {
+      const double w = lane_d(key, __ffsll((long long)m) - 1);
+      if (w > least) {
+        insert(list, w);
+        least = fmax(least, lane_d(list, k - 1));
       }
     }
-    const float v = wave_max(best.v);
-    const unsigned long long at = __ballot(best.v == v);
-    int i;
-    if (__popcll(at) == 1) i = __builtin_amdgcn_readlane(best.i, __ffsll((long long)at) - 1);
-    else i = wave_min(best.v == v ? best.i : kNoIndex);
-    const float tv = mfd::lane_f(list.v, k - 1);
-    const int ti = __builtin_amdgcn_readlane(list.i, k - 1);
-    if (i == kNoIndex || !before(v, i, tv, ti)) break;
-    const int pos = __popcll(__ballot(before(list.v, list.i, v, i)));
-    const float pv = __shfl_up(list.v, 1, 64);
-    const int pi = __shfl_up(list.i, 1, 64);
-    if (lane == pos) list = Entry{v, i};
-    else if (lane > pos) list = Entry{pv, pi};
-    lv = v;
-    li = i;
-    first = false;
-    mine = best.i == i;
   }
 }
 
 // One wave's share of a row: batches of 64 * U vectors, `step` batches apart, from element `at` up to `end`.
 template <typename T, bool TOP, int U>
-__device__ __forceinline__ void scan(const T *row, int at, int end, int step, int k, Acc &acc, Entry &list) {
+__device__ __forceinline__ void scan(const T *row, int at, int end, int step, int k, Acc &acc, double &list) {
   constexpr int VEC = El<T>::kVec, N = U * VEC;
   const int lane = threadIdx.x & 63;
+  bool full = false;
+  float last = -kInf;  // the logit of the list's last entry
   for (; at < end; at += step) {
     float z[N];
 #pragma unroll
@@ -119,38 +139,37 @@ __device__ __forceinline__ void scan(const T *row, int at, int end, int step, in
 #pragma unroll
       for (int i = 0; i < VEC; ++i) z[j * VEC + i] = v[i];
     }
-    float bm = z[0];
+    float bm = -kInf;
 #pragma unroll
-    for (int i = 1; i < N; ++i) bm = fmaxf(bm, z[i]);
-    bm = fmaxf(bm, -kInf);
+    for (int i = 0; i < N; ++i) bm = fmaxf(bm, z[i]);
     add(acc, z, bm);
-    if (TOP) {
-      const float tv = mfd::lane_f(list.v, k - 1);
-      const int ti = __builtin_amdgcn_readlane(list.i, k - 1);
-      // an equal logit of a later batch may have a lower index only where waves interleave: never within one wave
-      if (__ballot(bm > tv) != 0ull || ti == kNoIndex)
-        insert_batch(list, k, z, [&](int j) {
-          const int c = at + ((j / VEC) * 64 + lane) * VEC + j % VEC;
-          return c < end ? c : kNoIndex;
-        });
+    // a later batch of the same wave has larger indexes throughout, so an equal logit does not come before
+    if (TOP && (__ballot(bm > last) != 0ull || !full)) {
+      take(list, k, z, bm, [&](int j) {
+        const int c = at + ((j / VEC) * 64 + lane) * VEC + j % VEC;
+        return c < end ? c : -1;
+      });
+      const double least = lane_d(list, k - 1);
+      full = least > below(-kInf);
+      last = value_of(least);
     }
   }
 }
 
-// What a row's statistics say, written by one wave.
-__device__ __forceinline__ void finish(const LogProbArgs &a, int64_t r, const Acc &t, const Entry &list, int token,
+// What a row's statistics say: written by the group of lanes `l` = 0 .. that hold them and the list.
+__device__ __forceinline__ void finish(const LogProbArgs &a, int64_t r, int l, const Acc &t, double list, int token,
                                        float z) {
-  const int lane = threadIdx.x & 63;
   const bool none = t.m == -kInf && t.s == 0.f;  // nothing left in this row (a NaN makes s NaN)
   const float ls = logf(t.s), ref = ref_of(t.m);
-  if (lane == 0) {
+  if (l == 0) {
     a.lse[r] = none ? -kInf : ref + ls;
     a.entropy[r] = none ? 0.f : ls - kLn2 * (t.u / t.s);
     a.logp[r] = token < 0 ? 0.f : none ? -kInf : (z - ref) - ls;
   }
-  if (lane < a.top) {
-    a.top_ids[r * a.top + lane] = list.i;
-    a.top_logp[r * a.top + lane] = none ? -kInf : (list.v - ref) - ls;
+  if (l < a.top) {
+    const float v = value_of(list);
+    a.top_ids[r * a.top + l] = index_of(list);
+    a.top_logp[r * a.top + l] = none ? -kInf : (v - ref) - ls;
   }
 }
 
@@ -162,6 +181,103 @@ template <typename T> __device__ __forceinline__ int token_of(const LogProbArgs 
   return in ? t : -1;
 }
 
+__device__ __forceinline__ void exchange(double &a, double &b) {
+  const double m = fmax(a, b);
+  b = fmin(a, b);
+  a = m;
+}
+// Descending order of N keys in registers (odd-even merge sort).
+template <int N> __device__ __forceinline__ void sort_keys(double (&a)[N]) {
+#pragma unroll
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) exchange(a[i + j], a[i + j + k]);
+}
+
+// Rows of at most 256 logits: 16 lanes per row, 16 logits per lane, four rows per wave, so that the reductions
+// (inside rows of 16 lanes, without lane reads) and what follows them are shared by four rows.  The lanes sort the
+// TOP best of their keys; the row's best are then taken off the lanes' heads one at a time.
+template <typename T, int TOP>
+__global__ void __launch_bounds__(kThreadsLp) short_kernel(LogProbArgs a) {
+  constexpr int VEC = El<T>::kVec, E = 16, L = 16;
+  const int l = threadIdx.x & (L - 1);
+  const int64_t r0 = ((int64_t)blockIdx.x * kThreadsLp + threadIdx.x) / L, r = r0 < a.rows ? r0 : a.rows - 1;
+  const T *row = (const T *)a.logits + r * a.ld;
+  float zt;
+  const int token = token_of(a, r, row, &zt);
+  float z[E];
+#pragma unroll
+  for (int j = 0; j < E / VEC; ++j) {
+    const int c = (j * L + l) * VEC;
+    float v[VEC];
+    load_part(row + c, a.vocab - c, -kInf, v);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) z[j * VEC + i] = v[i];
+  }
+  float m = -kInf;
+#pragma unroll
+  for (int i = 0; i < E; ++i) m = fmaxf(m, z[i]);
+  m = fmaxf(m, dpp_f<0xB1>(m));
+  m = fmaxf(m, dpp_f<0x4E>(m));
+  m = fmaxf(m, dpp_f<0x141>(m));
+  m = fmaxf(m, dpp_f<0x140>(m));
+  const float ref = ref_of(m);
+  Acc acc{m, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float d = (z[i] - ref) * kLog2e, e = __builtin_amdgcn_exp2f(d);
+    acc.s += e;
+    acc.u += e * fmaxf(d, kFloor);
+  }
+  auto row_sum = [](float v) {
+    v += dpp_f<0xB1>(v);
+    v += dpp_f<0x4E>(v);
+    v += dpp_f<0x141>(v);
+    return v + dpp_f<0x140>(v);
+  };
+  acc.s = row_sum(acc.s);
+  acc.u = row_sum(acc.u);
+  double mine = 0.0;
+  if constexpr (TOP > 0) {
+    double best[TOP];
+#pragma unroll
+    for (int g = 0; g < E / TOP; ++g) {
+      double k[TOP];
+#pragma unroll
+      for (int i = 0; i < TOP; ++i) {
+        const int j = g * TOP + i, c = ((j / VEC) * L + l) * VEC + j % VEC;
+        k[i] = c < a.vocab ? key_of(z[j], c) : below(-kInf);
+      }
+      sort_keys(k);
+      if (g == 0) {
+#pragma unroll
+        for (int i = 0; i < TOP; ++i) best[i] = k[i];
+      } else {  // the best of two sorted lists: pair them end to end, then merge
+#pragma unroll
+        for (int i = 0; i < TOP; ++i) best[i] = fmax(best[i], k[TOP - 1 - i]);
+#pragma unroll
+        for (int h = TOP / 2; h >= 1; h /= 2)
+#pragma unroll
+          for (int i = 0; i < TOP; ++i)
+            if ((i & h) == 0) exchange(best[i], best[i + h]);
+      }
+    }
+    for (int n = 0; n < a.top; ++n) {
+      const double w = row16_max(best[0]);
+      if (l == n) mine = w;
+      const bool mine_goes = best[0] == w;
+#pragma unroll
+      for (int i = 0; i < TOP; ++i) best[i] = mine_goes ? (i + 1 < TOP ? best[i + 1] : below(-kInf)) : best[i];
+    }
+  }
+  if (r0 < a.rows) finish(a, r, l, acc, mine, token, zt);
+}
+
 // One wave per row.
 template <typename T, bool TOP, int U>
 __global__ void __launch_bounds__(kThreadsLp) rows_kernel(LogProbArgs a) {
@@ -171,20 +287,26 @@ __global__ void __launch_bounds__(kThreadsLp) rows_kernel(LogProbArgs a) {
   float z;
   const int token = token_of(a, r, row, &z);
   Acc acc{-kInf, 0.f, 0.f};
-  Entry list{-kInf, kNoIndex};
+  double list = below(-kInf);
   scan<T, TOP, U>(row, 0, a.vocab, 64 * U * El<T>::kVec, a.top, acc, list);
-  finish(a, r, wave_join(acc), list, token, z);
+  finish(a, r, threadIdx.x & 63, wave_join(acc), list, token, z);
 }
 
-// A part of a row as the workspace holds it: statistics, then the list.
-__host__ __device__ inline size_t part_floats(int top) { return 4 + 2 * (size_t)top; }
+// Rows in parts: the workspace holds the parts' statistics (m, s, u and a gap), then their lists.
+struct Parts {
+  float4 *stat;  // [rows][parts]
+  double *keys;  // [rows][parts][top]
+};
+__host__ __device__ inline Parts parts_at(unsigned char *ws, int64_t rows, int parts) {
+  return Parts{(float4 *)ws, (double *)(ws + (size_t)rows * parts * sizeof(float4))};
+}
 
-// One block per (row, part): its waves take the part's batches in turn.  One part: the row's results, else the
-// part's statistics and list go to the workspace.
+// One block per (row, part): its waves take the part's batches in turn and join what they found.  One part: the
+// row's results, else the part's statistics and list go to the workspace.
 template <typename T, bool TOP, int U>
 __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int parts, int per) {
   __shared__ Acc accs[kWaves];
-  __shared__ Entry lists[kWaves][kMaxTop];
+  __shared__ double lists[kWaves][kMaxTop], merged[kMaxTop];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t r = blockIdx.x / (unsigned)parts;
   const int p = blockIdx.x % (unsigned)parts;
@@ -192,72 +314,84 @@ __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int pa
   float z;
   const int token = token_of(a, r, row, &z);
   Acc acc{-kInf, 0.f, 0.f};
-  Entry list{-kInf, kNoIndex};
+  double list = below(-kInf);
   constexpr int kBatch = 64 * U * El<T>::kVec;
   scan<T, TOP, U>(row, p * per + wave * kBatch, min(a.vocab, (p + 1) * per), kWaves * kBatch, a.top, acc, list);
   acc = wave_join(acc);
   if (lane == 0) accs[wave] = acc;
-  if (TOP) lists[wave][lane] = list;
+  if (TOP) {
+    lists[wave][lane] = list;
+    if (wave == 0) merged[lane] = below(-kInf);
+  }
   __syncthreads();
+  if (TOP) {
+    // an entry's place is its place in its own list plus the entries of the others before it
+    int place[kWaves] = {};
+    int h = 64;
+    while (h > a.top) h >>= 1;
+    for (; h; h >>= 1) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        if (place[w] + h <= a.top && lists[w][place[w] + h - 1] > list) place[w] += h;
+    }
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) at += place[w];  // in its own list: the lane itself
+    if (lane < a.top && list > below(-kInf) && at < a.top) merged[at] = list;
+    __syncthreads();
+  }
   if (wave != 0) return;
   acc = wave_join(lane < kWaves ? accs[lane] : Acc{-kInf, 0.f, 0.f});
-  if (TOP) {
-    for (int w = 1; w < kWaves; ++w) {
-      const Entry e = lists[w][lane];
-      const float v[1] = {e.v};
-      insert_batch(list, a.top, v, [&](int) { return lane < a.top ? e.i : kNoIndex; });
-    }
-  }
+  if (TOP) list = merged[lane];
   if (parts == 1) {
-    finish(a, r, acc, list, token, z);
+    finish(a, r, lane, acc, list, token, z);
     return;
   }
-  float *out = (float *)a.ws + (size_t)blockIdx.x * part_floats(a.top);
-  if (lane == 0) {
-    out[0] = acc.m;
-    out[1] = acc.s;
-    out[2] = acc.u;
-  }
-  if (lane < a.top) {
-    out[4 + lane] = list.v;
-    ((int *)out)[4 + a.top + lane] = list.i;
-  }
+  const Parts o = parts_at(a.ws, a.rows, parts);
+  if (lane == 0) o.stat[blockIdx.x] = make_float4(acc.m, acc.s, acc.u, 0.f);
+  if (lane < a.top) o.keys[(size_t)blockIdx.x * a.top + lane] = list;
 }
 
-// Joins the parts of a row: one wave per row.
+// Joins the parts of a row (at most 64): one wave per row.
 template <typename T, bool TOP> __global__ void __launch_bounds__(64) join_kernel(LogProbArgs a, int parts) {
   const int lane = threadIdx.x;
   const int64_t r = blockIdx.x;
+  const Parts in = parts_at(a.ws, a.rows, parts);
   float z;
   const int token = token_of(a, r, (const T *)a.logits + r * a.ld, &z);
-  const size_t stride = part_floats(a.top);
-  const float *in = (const float *)a.ws + (size_t)r * parts * stride;
   Acc acc{-kInf, 0.f, 0.f};
-  for (int p = lane; p < parts; p += 64) {
-    const Acc b{in[p * stride], in[p * stride + 1], in[p * stride + 2]};
-    const float m = fmaxf(acc.m, b.m), ref = ref_of(m);
-    Acc c = b;
-    rescale(acc, ref);
-    rescale(c, ref);
-    acc = Acc{m, acc.s + c.s, acc.u + c.u};
+  double least = below(-kInf), list = least;
+  if (lane < parts) {
+    const float4 v = in.stat[r * parts + lane];
+    acc = Acc{v.x, v.y, v.z};
+    if (TOP) least = in.keys[(r * parts + lane) * a.top + a.top - 1];
   }
   acc = wave_join(acc);
-  Entry list{-kInf, kNoIndex};
   if (TOP) {
-    for (int c = lane; c - lane < parts * a.top; c += 64) {
-      const bool in_list = c < parts * a.top;
-      const int p = in_list ? c / a.top : 0, e = in_list ? c % a.top : 0;
-      const float v[1] = {in_list ? in[p * stride + 4 + e] : -kInf};
-      const int i = in_list ? ((const int *)in)[p * stride + 4 + a.top + e] : kNoIndex;
-      insert_batch(list, a.top, v, [&](int) { return i; });
+    least = wave_max_d(least);  // a part has k keys from here on
+    const double *keys = in.keys + r * parts * a.top;
+    const int n = parts * a.top;
+    for (int c0 = 0; c0 < n; c0 += 256) {
+      double k[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] = c0 + j * 64 + lane < n ? keys[c0 + j * 64 + lane] : below(-kInf);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        for (unsigned long long m = __ballot(k[j] >= least && k[j] > below(-kInf)); m; m &= m - 1) {
+          const double w = lane_d(k[j], __ffsll((long long)m) - 1);
+          if (w >= least) {
+            insert(list, w);
+            least = fmax(least, lane_d(list, a.top - 1));
+          }
+        }
     }
   }
-  finish(a, r, acc, list, token, z);
+  finish(a, r, lane, acc, list, token, z);
 }
 
-// Elements of a batch of one wave (U = 4), and the parts a row is cut into.
+// Elements of a batch of one wave, and the parts a row is cut into.
 template <typename T> constexpr int batch_of(int U) { return 64 * U * El<T>::kVec; }
-constexpr int kMaxParts = 256;
+constexpr int kMaxParts = 64;  // the join holds one per lane
 int parts_of(int64_t rows, int vocab, int batch) {
   // a part is at least one batch for each of a block's waves; parts are made only where the rows alone do not
   // fill the device (256 compute units with four blocks each)
@@ -269,15 +403,23 @@ int parts_of(int64_t rows, int vocab, int batch) {
 
 template <typename T, bool TOP> hipError_t run(const LogProbArgs &a, bool in_parts, hipStream_t s) {
   const int batch = batch_of<T>(4);
+  const dim3 block(kThreadsLp);
+  if (a.vocab <= 256 && a.top <= 8) {
+    const dim3 grid((unsigned)((a.rows + 15) / 16));
+    if (!TOP) hipLaunchKernelGGL((short_kernel<T, 0>), grid, block, 0, s, a);
+    else if (a.top <= 4) hipLaunchKernelGGL((short_kernel<T, TOP ? 4 : 0>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((short_kernel<T, TOP ? 8 : 0>), grid, block, 0, s, a);
+    return hipGetLastError();
+  }
   if (a.vocab <= batch) {
     const dim3 grid((unsigned)((a.rows + kWaves - 1) / kWaves));
-    if (a.vocab <= batch_of<T>(1)) hipLaunchKernelGGL((rows_kernel<T, TOP, 1>), grid, dim3(kThreadsLp), 0, s, a);
-    else hipLaunchKernelGGL((rows_kernel<T, TOP, 4>), grid, dim3(kThreadsLp), 0, s, a);
+    if (a.vocab <= batch_of<T>(1)) hipLaunchKernelGGL((rows_kernel<T, TOP, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((rows_kernel<T, TOP, 4>), grid, block, 0, s, a);
     return hipGetLastError();
   }
   const int parts = in_parts ? parts_of(a.rows, a.vocab, batch) : 1;
-  const int per = (int)(((int64_t)a.vocab + parts - 1) / parts);
-  hipLaunchKernelGGL((parts_kernel<T, TOP, 4>), dim3((unsigned)(a.rows * parts)), dim3(kThreadsLp), 0, s, a, parts, per);
+  const int per = (int)(((int64_t)a.vocab + parts - 1) / parts + 63) / 64 * 64;
+  hipLaunchKernelGGL((parts_kernel<T, TOP, 4>), dim3((unsigned)(a.rows * parts)), block, 0, s, a, parts, per);
   if (parts > 1) hipLaunchKernelGGL((join_kernel<T, TOP>), dim3((unsigned)a.rows), dim3(64), 0, s, a, parts);
   return hipGetLastError();
 }
@@ -337,7 +479,7 @@ size_t log_probs_bytes(int64_t rows, int vocab, int top, int dtype) {
   const int batch = dtype == FWG_BF16 ? lpr::batch_of<uint16_t>(4) : lpr::batch_of<float>(4);
   if (rows <= 0 || vocab <= batch) return 0;
   const int parts = lpr::parts_of(rows, vocab, batch);
-  return parts == 1 ? 0 : (size_t)rows * parts * lpr::part_floats(top) * sizeof(float);
+  return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(float4) + top * sizeof(double));
 }
 
 hipError_t launch_log_probs(const LogProbArgs &a, int dtype, bool in_parts, hipStream_t s) {
