@@ -8,7 +8,7 @@
 //
 // The k alternatives are a list with one entry per lane in order (logit descending, index ascending).  A batch
 // whose largest logit does not pass the list's last entry costs one comparison per lane; otherwise the elements
-// that pass it are inserted one at a time.
+// that pass it are joined with the list.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -22,6 +22,7 @@ namespace lpr {
 using namespace opd;
 
 constexpr int kWaves = 4, kThreadsLp = 64 * kWaves;
+constexpr float kMax = 3.4028234663852886e38f;
 constexpr float kFloor = -200.f;  // 2^-200 is zero in float32: products with it stay zero and finite
 
 struct Acc {
@@ -73,61 +74,171 @@ __device__ __forceinline__ double lane_d(double v, int l) {
 template <int CTRL> __device__ __forceinline__ double dpp_d(double v) {
   return __hiloint2double(dpp_i<CTRL>(__double2hiint(v)), dpp_i<CTRL>(__double2loint(v)));
 }
-// Largest key of each row of 16 lanes, in all of its lanes; and of the wavefront.
+// Largest key of each row of 16 lanes, in all of its lanes.
 __device__ __forceinline__ double row16_max(double v) {
   v = fmax(v, dpp_d<0xB1>(v));
   v = fmax(v, dpp_d<0x4E>(v));
   v = fmax(v, dpp_d<0x141>(v));
   return fmax(v, dpp_d<0x140>(v));
 }
-__device__ __forceinline__ double wave_max_d(double v) {
-  v = row16_max(v);
-  return fmax(fmax(lane_d(v, 0), lane_d(v, 16)), fmax(lane_d(v, 32), lane_d(v, 48)));
-}
 
-// The list: lane i holds the i-th best key so far.  Puts w (the same in every lane) in its place.
-__device__ __forceinline__ void insert(double &list, double w) {
-  // lane i's left neighbour; lane 0's is above everything
-  const double left = __hiloint2double(__builtin_amdgcn_update_dpp(0x7fe00000, __double2hiint(list), 0x138, 0xF, 0xF, false),
-                                       __builtin_amdgcn_update_dpp(0, __double2loint(list), 0x138, 0xF, 0xF, false));
-  list = fmax(list, fmin(left, w));
-}
+// What a wave keeps in LDS to select: candidates (logit bits, index), and the two sides of a merge.
+constexpr int kSlots = 256;
+struct Select {
+  int2 slot[kSlots];
+  double cand[64], place[kMaxTop];
+};
+// A wave's LDS accesses are in order; this keeps the compiler to the order of the source.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// The k-th largest of the lanes' values (k <= 64): the smallest of those that fewer than k exceed.
-__device__ __forceinline__ float kth_of_lanes(float v, int k) {
-  int over = 0;
+// Floats as whole numbers of the same order, and back (no NaN).
+__device__ __forceinline__ int ordered(float v) {
+  const int b = __float_as_int(v);
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float from_ordered(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7fffffff)); }
+
+// A bound that at least k, and where values differ at most 2 k, of the lanes' 64 U values reach (k <= 64, and every
+// lane has values: -inf at least).  Bisection over the values in order; a count takes a ballot per value.
+template <int U> __device__ __forceinline__ float bound_of(const float (&v)[U], int k) {
+  float most = v[0];
 #pragma unroll
-  for (int l = 0; l < 64; ++l) over += mfd::lane_f(v, l) > v;
-  return -wave_max(over < k ? -v : -kInf);
-}
-
-// Puts the keys of a batch that come before the list's entry k - 1 into the list.  best: the lane's largest logit.
-// Where many lanes have one (the first batch, above all), the k-th largest of the lanes' best is a bound below which
-// nothing can be among the k, and keeps the insertions to little more than k.
-template <int N, typename Index>
-__device__ __forceinline__ void take(double &list, int k, const float (&z)[N], float best, Index idx) {
-  double least = lane_d(list, k - 1);
-  if (__popcll(__ballot(best > value_of(least))) > 8) least = fmax(least, below(kth_of_lanes(best, k)));
+  for (int u = 1; u < U; ++u) most = fmaxf(most, v[u]);
+  int lo = ordered(-wave_max(-most)), hi = ordered(wave_max(most));  // all 64 lanes reach lo
+  while (lo < hi) {
+    const int mid = (int)(((long long)lo + hi + 1) >> 1);
+    const float t = from_ordered(mid);
+    int n = 0;
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int i = idx(j);
-    const double key = i >= 0 ? key_of(z[j], i) : below(-kInf);
-    for (unsigned long long m = __ballot(key > least); m; m &= m - 1) {
-      const double w = lane_d(key, __ffsll((long long)m) - 1);
-      if (w > least) {
-        insert(list, w);
-        least = fmax(least, lane_d(list, k - 1));
-      }
-    }
+    for (int u = 0; u < U; ++u) n += __popcll(__ballot(v[u] >= t));
+    if (n >= k) lo = mid;
+    else hi = mid - 1;
+    if (n >= k && n <= 2 * k) break;
   }
+  return from_ordered(lo);
+}
+
+// The list: lane i < k holds the i-th best key so far (below(-inf): none).  Joins it with candidates, at most one
+// per lane, in the first n lanes: everybody's place is the number of keys before it, counted over keys that all
+// lanes read at once.
+__device__ __forceinline__ void merge(double &list, int k, double cand, int n, Select &s) {
+  const int lane = threadIdx.x & 63;
+  const double none = below(-kInf);
+  int pc = 0, pl = lane;
+  s.cand[lane] = cand;
+  s.place[lane] = list;
+  in_order();
+#pragma unroll 1
+  for (int j = 0; j < n; j += 8)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double c = s.cand[j + i];
+      pc += c > cand;
+      pl += c > list;
+    }
+  const int held = __popcll(__ballot(list > none));
+#pragma unroll 1
+  for (int j = 0; j < held; j += 8)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pc += s.place[j + i] > cand;
+  in_order();
+  s.place[lane] = none;
+  in_order();
+  if (cand > none && pc < k) s.place[pc] = cand;
+  if (list > none && pl < k) s.place[pl] = list;
+  in_order();
+  list = s.place[lane];
+  in_order();
+}
+
+// Joins the list with the n <= kSlots candidates of the slots.
+__device__ __forceinline__ void merge_slots(double &list, int k, int n, Select &s) {
+  const int lane = threadIdx.x & 63;
+  in_order();
+#pragma unroll 1
+  for (int o = 0; o < n; o += 64) {
+    double cand = below(-kInf);
+    if (o + lane < n) {
+      const int2 v = s.slot[o + lane];
+      cand = key_of(__int_as_float(v.x), v.y);
+    }
+    merge(list, k, cand, min(64, n - o), s);
+  }
+}
+
+// Appends an element of each lane that wants to; n counts them, also beyond the slots.
+__device__ __forceinline__ void append(float z, int i, bool want, int &n, Select &s) {
+  const unsigned long long m = __ballot(want);
+  if (m == 0ull) return;
+  const int at = n + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
+  if (want && at < kSlots) s.slot[at] = make_int2(__float_as_int(z), i);
+  n += __popcll(m);
+}
+
+// Puts the elements of a batch (U vectors per lane, at .. min(end, at + 64 U VEC) of the row) that come before the
+// list's entry k - 1 into the list.  best: the largest of each vector.  Where many lanes have candidates (the first
+// batch, above all), a bound that k vectors' best reach leaves out what cannot be among the k, and little more than
+// those pass it.  Where more than the slots pass (many equal logits, rising rows) the elements are read again, 64 at
+// a time.
+template <typename T, int U>
+__device__ __forceinline__ void take(double &list, int k, const float (&batch)[U * El<T>::kVec], const float (&best)[U],
+                                     float most, const T *row, int at, int end, Select &s) {
+  constexpr int VEC = El<T>::kVec, N = U * VEC;
+  const int lane = threadIdx.x & 63;
+  float least = value_of(lane_d(list, k - 1));
+  if (__popcll(__ballot(most > least)) > 8) least = fmaxf(least, bound_of(best, k));
+  least = fmaxf(least, -kMax);
+  int n = 0, c = at + lane * VEC;
+  float z[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) z[i] = batch[i];
+#pragma unroll 1
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) append(z[i], c + i, z[i] >= least, n, s);
+#pragma unroll
+    for (int i = 0; i < N - VEC; ++i) z[i] = z[i + VEC];  // a loop over registers: move, not index
+    c += 64 * VEC;
+  }
+  const bool fits = n <= kSlots;
+  int c0 = at;
+  const int c1 = min(end, at + 64 * N);
+  do {
+    if (!fits) {
+      n = 0;
+      const double key = c0 + lane < c1 ? key_of(to_f(row[c0 + lane]), c0 + lane) : below(-kInf);
+      append(value_of(key), c0 + lane, key > lane_d(list, k - 1) && value_of(key) >= -kMax, n, s);
+      c0 += 64;
+    }
+    merge_slots(list, k, n, s);
+  } while (!fits && c0 < c1);
+}
+
+// Logits of -inf (and NaN, which ranks with them) are no candidates above: rows have them by the thousand.  Where
+// fewer than k others were found, the lowest tokens of them fill the list; 2 k tokens of the row hold enough.
+template <typename T> __device__ __forceinline__ void fill(double &list, int k, const T *row, int vocab, Select &s) {
+  const int lane = threadIdx.x & 63;
+  int n = __popcll(__ballot(lane < k && list > below(-kInf)));
+  if (n >= k) return;
+  in_order();
+  s.place[lane] = list;
+#pragma unroll 1
+  for (int c0 = 0; n < k && c0 < vocab; c0 += 64) {
+    const bool out = c0 + lane < vocab && !(to_f(row[c0 + lane]) > -kInf);
+    const unsigned long long m = __ballot(out);
+    const int at = n + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
+    if (out && at < k) s.place[at] = key_of(-kInf, c0 + lane);
+    n += __popcll(m);
+  }
+  in_order();
+  list = s.place[lane];
 }
 
 // One wave's share of a row: batches of 64 * U vectors, `step` batches apart, from element `at` up to `end`.
 template <typename T, bool TOP, int U>
-__device__ __forceinline__ void scan(const T *row, int at, int end, int step, int k, Acc &acc, double &list) {
+__device__ __forceinline__ void scan(const T *row, int at, int end, int step, int k, Acc &acc, double &list, Select *sel) {
   constexpr int VEC = El<T>::kVec, N = U * VEC;
   const int lane = threadIdx.x & 63;
-  bool full = false;
   float last = -kInf;  // the logit of the list's last entry
   for (; at < end; at += step) {
     float z[N];
@@ -139,19 +250,19 @@ __device__ __forceinline__ void scan(const T *row, int at, int end, int step, in
 #pragma unroll
       for (int i = 0; i < VEC; ++i) z[j * VEC + i] = v[i];
     }
-    float bm = -kInf;
+    float best[U], bm = -kInf;
 #pragma unroll
-    for (int i = 0; i < N; ++i) bm = fmaxf(bm, z[i]);
+    for (int j = 0; j < U; ++j) {
+      best[j] = -kInf;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) best[j] = fmaxf(best[j], z[j * VEC + i]);
+      bm = fmaxf(bm, best[j]);
+    }
     add(acc, z, bm);
     // a later batch of the same wave has larger indexes throughout, so an equal logit does not come before
-    if (TOP && (__ballot(bm > last) != 0ull || !full)) {
-      take(list, k, z, bm, [&](int j) {
-        const int c = at + ((j / VEC) * 64 + lane) * VEC + j % VEC;
-        return c < end ? c : -1;
-      });
-      const double least = lane_d(list, k - 1);
-      full = least > below(-kInf);
-      last = value_of(least);
+    if (TOP && __ballot(bm > last) != 0ull) {
+      take<T, U>(list, k, z, best, bm, row, at, end, *sel);
+      last = value_of(lane_d(list, k - 1));
     }
   }
 }
@@ -160,7 +271,7 @@ __device__ __forceinline__ void scan(const T *row, int at, int end, int step, in
 __device__ __forceinline__ void finish(const LogProbArgs &a, int64_t r, int l, const Acc &t, double list, int token,
                                        float z) {
   const bool none = t.m == -kInf && t.s == 0.f;  // nothing left in this row (a NaN makes s NaN)
-  const float ls = logf(t.s), ref = ref_of(t.m);
+  const float ls = kLn2 * __builtin_amdgcn_logf(t.s), ref = ref_of(t.m);  // t.s >= 1, or 0
   if (l == 0) {
     a.lse[r] = none ? -kInf : ref + ls;
     a.entropy[r] = none ? 0.f : ls - kLn2 * (t.u / t.s);
@@ -282,13 +393,15 @@ __global__ void __launch_bounds__(kThreadsLp) short_kernel(LogProbArgs a) {
 template <typename T, bool TOP, int U>
 __global__ void __launch_bounds__(kThreadsLp) rows_kernel(LogProbArgs a) {
   const int64_t r = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  __shared__ Select sel[TOP ? kWaves : 1];
   if (r >= a.rows) return;
   const T *row = (const T *)a.logits + r * a.ld;
   float z;
   const int token = token_of(a, r, row, &z);
   Acc acc{-kInf, 0.f, 0.f};
   double list = below(-kInf);
-  scan<T, TOP, U>(row, 0, a.vocab, 64 * U * El<T>::kVec, a.top, acc, list);
+  scan<T, TOP, U>(row, 0, a.vocab, 64 * U * El<T>::kVec, a.top, acc, list, &sel[TOP ? threadIdx.x >> 6 : 0]);
+  if (TOP) fill(list, a.top, row, a.vocab, sel[TOP ? threadIdx.x >> 6 : 0]);
   finish(a, r, threadIdx.x & 63, wave_join(acc), list, token, z);
 }
 
@@ -306,7 +419,8 @@ __host__ __device__ inline Parts parts_at(unsigned char *ws, int64_t rows, int p
 template <typename T, bool TOP, int U>
 __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int parts, int per) {
   __shared__ Acc accs[kWaves];
-  __shared__ double lists[kWaves][kMaxTop], merged[kMaxTop];
+  __shared__ Select sel[TOP ? kWaves : 1];
+  __shared__ double merged[kMaxTop];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t r = blockIdx.x / (unsigned)parts;
   const int p = blockIdx.x % (unsigned)parts;
@@ -316,11 +430,12 @@ __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int pa
   Acc acc{-kInf, 0.f, 0.f};
   double list = below(-kInf);
   constexpr int kBatch = 64 * U * El<T>::kVec;
-  scan<T, TOP, U>(row, p * per + wave * kBatch, min(a.vocab, (p + 1) * per), kWaves * kBatch, a.top, acc, list);
+  scan<T, TOP, U>(row, p * per + wave * kBatch, min(a.vocab, (p + 1) * per), kWaves * kBatch, a.top, acc, list,
+                  &sel[TOP ? wave : 0]);
   acc = wave_join(acc);
   if (lane == 0) accs[wave] = acc;
   if (TOP) {
-    lists[wave][lane] = list;
+    sel[wave].place[lane] = list;
     if (wave == 0) merged[lane] = below(-kInf);
   }
   __syncthreads();
@@ -332,7 +447,7 @@ __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int pa
     for (; h; h >>= 1) {
 #pragma unroll
       for (int w = 0; w < kWaves; ++w)
-        if (place[w] + h <= a.top && lists[w][place[w] + h - 1] > list) place[w] += h;
+        if (place[w] + h <= a.top && sel[w].place[place[w] + h - 1] > list) place[w] += h;
     }
     int at = 0;
 #pragma unroll
@@ -344,6 +459,7 @@ __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int pa
   acc = wave_join(lane < kWaves ? accs[lane] : Acc{-kInf, 0.f, 0.f});
   if (TOP) list = merged[lane];
   if (parts == 1) {
+    if (TOP) fill(list, a.top, row, a.vocab, sel[0]);
     finish(a, r, lane, acc, list, token, z);
     return;
   }
@@ -354,37 +470,40 @@ __global__ void __launch_bounds__(kThreadsLp) parts_kernel(LogProbArgs a, int pa
 
 // Joins the parts of a row (at most 64): one wave per row.
 template <typename T, bool TOP> __global__ void __launch_bounds__(64) join_kernel(LogProbArgs a, int parts) {
+  __shared__ Select sel;
   const int lane = threadIdx.x;
   const int64_t r = blockIdx.x;
   const Parts in = parts_at(a.ws, a.rows, parts);
   float z;
   const int token = token_of(a, r, (const T *)a.logits + r * a.ld, &z);
   Acc acc{-kInf, 0.f, 0.f};
-  double least = below(-kInf), list = least;
+  double list = below(-kInf);
   if (lane < parts) {
     const float4 v = in.stat[r * parts + lane];
     acc = Acc{v.x, v.y, v.z};
-    if (TOP) least = in.keys[(r * parts + lane) * a.top + a.top - 1];
   }
   acc = wave_join(acc);
   if (TOP) {
-    least = wave_max_d(least);  // a part has k keys from here on
+    // a bound from the heads of the lists: one key per lane
+    const int e = lane / parts;
+    float head[1] = {-kInf};
+    if (e < a.top && (e + 1) * parts <= 64) head[0] = value_of(in.keys[(r * parts + lane % parts) * a.top + e]);
+    float least = bound_of(head, a.top);
     const double *keys = in.keys + r * parts * a.top;
     const int n = parts * a.top;
-    for (int c0 = 0; c0 < n; c0 += 256) {
-      double k[4];
+#pragma unroll 1
+    for (int c0 = 0; c0 < n; c0 += kSlots) {
+      double key[kSlots / 64];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[j] = c0 + j * 64 + lane < n ? keys[c0 + j * 64 + lane] : below(-kInf);
+      for (int j = 0; j < kSlots / 64; ++j) key[j] = c0 + j * 64 + lane < n ? keys[c0 + j * 64 + lane] : below(-kInf);
+      int found = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        for (unsigned long long m = __ballot(k[j] >= least && k[j] > below(-kInf)); m; m &= m - 1) {
-          const double w = lane_d(k[j], __ffsll((long long)m) - 1);
-          if (w >= least) {
-            insert(list, w);
-            least = fmax(least, lane_d(list, a.top - 1));
-          }
-        }
+      for (int j = 0; j < kSlots / 64; ++j)
+        append(value_of(key[j]), index_of(key[j]), value_of(key[j]) >= least && key[j] > below(-kInf), found, sel);
+      merge_slots(list, a.top, found, sel);
+      least = fmaxf(least, value_of(lane_d(list, a.top - 1)));
     }
+    fill(list, a.top, (const T *)a.logits + r * a.ld, a.vocab, sel);
   }
   finish(a, r, lane, acc, list, token, z);
 }

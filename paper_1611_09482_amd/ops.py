@@ -12,6 +12,7 @@ allocator.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -29,27 +30,27 @@ def _library():
     return _lib
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+_device = torch.cuda.current_device
+_stream = torch._C._cuda_getCurrentRawStream  # of a device: what torch.cuda.current_stream() wraps, without its object
 
 
-def _on_device(name: str, t) -> None:
+def _refuse(name: str, t, device: int):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} is not a tensor")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}: the call runs on the current device, "
-                         f"cuda:{torch.cuda.current_device()}")
+    raise ValueError(f"{name} is on {t.device}: the call runs on the current device, cuda:{device}")
 
 
-def _typed(name: str, t, dtype) -> None:
-    _on_device(name, t)
+def _typed(name: str, t, dtype, device: int) -> None:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _refuse(name, t, device)
     if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}: {dtype} is wanted")
 
 
-def _matrix(name: str, t, out: bool = False):
+def _matrix(name: str, t, device: int, out: bool = False):
     """(element type, rows, width, stride) of a float32 or bfloat16 tensor seen as rows."""
-    _on_device(name, t)
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _refuse(name, t, device)
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise TypeError(f"{name} is {t.dtype}: float32 or bfloat16 is wanted")
@@ -58,21 +59,21 @@ def _matrix(name: str, t, out: bool = False):
 
 def _rows(name: str, t, out: bool = False):
     """(rows, width, stride) of a tensor seen as rows of its last dimension."""
-    shape = t.shape
+    shape, strides = t.shape, t.stride()
     if not shape:
         raise ValueError(f"{name} has no dimensions: rows are wanted")
     width = shape[-1]
-    if width > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: the elements of a row have to be consecutive (stride {t.stride(-1)})")
-    if t.dim() == 2:
-        rows, stride = shape[0], t.stride(0)
+    if width > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row have to be consecutive (stride {strides[-1]})")
+    if len(shape) == 2:
+        rows, stride = shape[0], strides[0]
     else:
         rows, stride = 1, width
-        for n, s in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
+        for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
             if n == 1:
                 continue
             if rows > 1 and s != rows * stride:
-                raise ValueError(f"{name}: the rows of shape {tuple(shape)}, strides {t.stride()} do not lie evenly apart")
+                raise ValueError(f"{name}: the rows of shape {tuple(shape)}, strides {strides} do not lie evenly apart")
             if rows == 1:
                 stride = s
             rows *= n
@@ -83,9 +84,12 @@ def _rows(name: str, t, out: bool = False):
     return rows, width, stride
 
 
-def _vector(name: str, t, n: int, dtype) -> int:
+def _vector(name: str, t, n: int, dtype, device: int) -> int:
     """Address of `n` consecutive elements."""
-    _typed(name, t, dtype)
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _refuse(name, t, device)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}: {dtype} is wanted")
     if t.numel() != n:
         raise ValueError(f"{name} has {t.numel()} elements: {n} are wanted")
     if not t.is_contiguous():
@@ -93,23 +97,25 @@ def _vector(name: str, t, n: int, dtype) -> int:
     return t.data_ptr()
 
 
-def _same(name: str, got: int, want: int, what: str) -> None:
-    if got != want:
-        raise ValueError(f"{name} has {got} {what}: {want} are wanted")
-
-
 def _shaped(name: str, t, shape) -> None:
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is wanted")
+
+
+def _flat(name: str, t) -> None:
+    if t.dim() != 2:
+        raise ValueError(f"{name} has {t.dim()} dimensions: 2 are wanted")
 
 
 def _workspace(need: int):
     return torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
 
 
-def _bytes(size, *args) -> int:
+@functools.lru_cache(maxsize=1024)
+def _bytes(call: str, *sizes) -> int:
+    """Workspace bytes: a pure function of the sizes."""
     n = ctypes.c_size_t(0)
-    _check(size(*args, ctypes.byref(n)))
+    _check(getattr(_library(), call)(*sizes, ctypes.byref(n)))
     return n.value
 
 
@@ -117,17 +123,18 @@ def embed(table, tokens, scale: float = 1.0, out=None):
     """scale * table[tokens].  table: float32 or bfloat16 [vocab][channels]; tokens: int32, any shape, contiguous;
     a token outside [0, vocab) is padding and gives a zero row.  out: [*tokens.shape][channels], float32 or bfloat16
     (default: of the table's type)."""
-    kind, vocab, channels, stride = _matrix("table", table)
-    _same("table", table.dim(), 2, "dimensions")
+    dev = _device()
+    kind, vocab, channels, stride = _matrix("table", table, dev)
+    _flat("table", table)
     n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
-    ids = _vector("tokens", tokens, n, torch.int32)
+    ids = _vector("tokens", tokens, n, torch.int32, dev)
     shape = tokens.shape + (channels,)
     if out is None:
         out = torch.empty(shape, dtype=table.dtype, device=table.device)
-    okind, _, _, ostride = _matrix("out", out, True)
+    okind, _, _, ostride = _matrix("out", out, dev, True)
     _shaped("out", out, shape)
     _check(_library().fwg_embed(kind, okind, n, vocab, channels, table.data_ptr(), stride, ids, scale, out.data_ptr(),
-                                ostride, _stream()))
+                                ostride, _stream(dev)))
     return out
 
 
@@ -136,19 +143,19 @@ def embed_grad(grad, tokens, vocab: int, scale: float = 1.0, out=None):
     v), zero where there is none.  grad: float32 or bfloat16 [*tokens.shape][channels] (rows may be expanded); out:
     float32 (default) or bfloat16 [vocab][channels].  Sums in float32 in an order that depends on the tokens only:
     the same bits every time."""
-    kind, rows, channels, stride = _matrix("grad", grad)
+    dev = _device()
+    kind, rows, channels, stride = _matrix("grad", grad, dev)
     n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
-    ids = _vector("tokens", tokens, n, torch.int32)
+    ids = _vector("tokens", tokens, n, torch.int32, dev)
     _shaped("grad", grad, tokens.shape + (channels,))
+    need = _bytes("fwg_embed_grad_workspace", n, vocab, channels)
     if out is None:
         out = torch.empty((vocab, channels), dtype=torch.float32, device=grad.device)
-    okind, _, _, ostride = _matrix("out", out, True)
+    okind, _, _, ostride = _matrix("out", out, dev, True)
     _shaped("out", out, (vocab, channels))
-    lib = _library()
-    need = _bytes(lib.fwg_embed_grad_workspace, n, vocab, channels)
     ws = _workspace(need)
-    _check(lib.fwg_embed_grad(kind, okind, n, vocab, channels, grad.data_ptr(), stride, ids, scale, out.data_ptr(),
-                              ostride, None if ws is None else ws.data_ptr(), need, _stream()))
+    _check(_library().fwg_embed_grad(kind, okind, n, vocab, channels, grad.data_ptr(), stride, ids, scale, out.data_ptr(),
+                              ostride, None if ws is None else ws.data_ptr(), need, _stream(dev)))
     return out
 
 
@@ -170,16 +177,17 @@ class NormQuant(NamedTuple):
 def quant_rows(x, out=None) -> QuantRows:
     """Rows in 8 bits with a scale each: scale = max|x| / 127, q = x / scale to the nearest (ties to even).  For
     weights [outputs][inner] these are matmul_quant's w and w_scale."""
-    kind, rows, width, stride = _matrix("x", x)
+    dev = _device()
+    kind, rows, width, stride = _matrix("x", x, dev)
     if out is None:
         out = QuantRows(torch.empty(x.shape, dtype=torch.int8, device=x.device),
                         torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device))
     q, scale = out
-    _typed("out.q", q, torch.int8)
+    _typed("out.q", q, torch.int8, dev)
     _shaped("out.q", q, x.shape)
     _check(_library().fwg_quant_rows(kind, rows, width, x.data_ptr(), stride, q.data_ptr(),
-                                     _rows("out.q", q, True)[2], _vector("out.scale", scale, rows, torch.float32),
-                                     _stream()))
+                                     _rows("out.q", q, True)[2], _vector("out.scale", scale, rows, torch.float32, dev),
+                                     _stream(dev)))
     return out if isinstance(out, QuantRows) else QuantRows(*out)
 
 
@@ -188,10 +196,11 @@ def norm_quant(x, gain=None, residual=None, eps: float = 1e-6, values: bool = Fa
     float32 or bfloat16 [..., channels]; gain: float32 [channels].  Results: q, scale, `summed` (h, rounded to x's
     type; with a residual only) and, where values is true, `values` (q * scale in bfloat16).  out: a NormQuant or
     the four tensors (None: not wanted); out's `summed` may be x or residual itself."""
-    kind, rows, width, stride = _matrix("x", x)
+    dev = _device()
+    kind, rows, width, stride = _matrix("x", x, dev)
     rp, rstride = None, 0
     if residual is not None:
-        _typed("residual", residual, x.dtype)
+        _typed("residual", residual, x.dtype, dev)
         _shaped("residual", residual, x.shape)
         rp, rstride = residual.data_ptr(), _rows("residual", residual)[2]
     if out is None:
@@ -200,21 +209,21 @@ def norm_quant(x, gain=None, residual=None, eps: float = 1e-6, values: bool = Fa
                         None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device),
                         torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
     q, scale, summed, vals = out
-    _typed("out.q", q, torch.int8)
+    _typed("out.q", q, torch.int8, dev)
     _shaped("out.q", q, x.shape)
     sp, sstride, vp, vstride = None, 0, None, 0
     if summed is not None:
-        _typed("out.summed", summed, x.dtype)
+        _typed("out.summed", summed, x.dtype, dev)
         _shaped("out.summed", summed, x.shape)
         sp, sstride = summed.data_ptr(), _rows("out.summed", summed, True)[2]
     if vals is not None:
-        _typed("out.values", vals, torch.bfloat16)
+        _typed("out.values", vals, torch.bfloat16, dev)
         _shaped("out.values", vals, x.shape)
         vp, vstride = vals.data_ptr(), _rows("out.values", vals, True)[2]
     _check(_library().fwg_norm_quant(kind, rows, width, x.data_ptr(), stride, rp, rstride,
-                                     None if gain is None else _vector("gain", gain, width, torch.float32), eps, sp,
+                                     None if gain is None else _vector("gain", gain, width, torch.float32, dev), eps, sp,
                                      sstride, q.data_ptr(), _rows("out.q", q, True)[2],
-                                     _vector("out.scale", scale, rows, torch.float32), vp, vstride, _stream()))
+                                     _vector("out.scale", scale, rows, torch.float32, dev), vp, vstride, _stream(dev)))
     return out if isinstance(out, NormQuant) else NormQuant(*out)
 
 
@@ -222,25 +231,26 @@ def matmul_quant(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=No
     """(x @ w.T) * x_scale[:, None] * w_scale + bias, the product of the 8-bit integers exact.  x: int8
     [..., inner] with x_scale float32 [...]; w: int8 [outputs][inner] with w_scale float32 [outputs]; bias: float32
     [outputs].  out: [..., outputs] of dtype (float32 or bfloat16)."""
-    _typed("x", x, torch.int8)
-    _typed("w", w, torch.int8)
+    dev = _device()
+    _typed("x", x, torch.int8, dev)
+    _typed("w", w, torch.int8, dev)
     rows, inner, stride = _rows("x", x)
-    _same("w", w.dim(), 2, "dimensions")
+    _flat("w", w)
     outputs, winner, wstride = _rows("w", w)
-    _same("w", winner, inner, "inner elements")
+    if winner != inner:
+        raise ValueError(f"w has {winner} inner elements: {inner} are wanted")
     shape = x.shape[:-1] + (outputs,)
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=x.device)
-    okind, _, _, ostride = _matrix("out", out, True)
+    okind, _, _, ostride = _matrix("out", out, dev, True)
     _shaped("out", out, shape)
-    lib = _library()
-    need = _bytes(lib.fwg_matmul_quant_workspace, rows, outputs, inner)
+    need = _bytes("fwg_matmul_quant_workspace", rows, outputs, inner)
     ws = _workspace(need)
-    _check(lib.fwg_matmul_quant(okind, rows, outputs, inner, x.data_ptr(), stride,
-                                _vector("x_scale", x_scale, rows, torch.float32), w.data_ptr(), wstride,
-                                _vector("w_scale", w_scale, outputs, torch.float32),
-                                None if bias is None else _vector("bias", bias, outputs, torch.float32),
-                                out.data_ptr(), ostride, None if ws is None else ws.data_ptr(), need, _stream()))
+    _check(_library().fwg_matmul_quant(okind, rows, outputs, inner, x.data_ptr(), stride,
+                                _vector("x_scale", x_scale, rows, torch.float32, dev), w.data_ptr(), wstride,
+                                _vector("w_scale", w_scale, outputs, torch.float32, dev),
+                                None if bias is None else _vector("bias", bias, outputs, torch.float32, dev),
+                                out.data_ptr(), ostride, None if ws is None else ws.data_ptr(), need, _stream(dev)))
     return out
 
 
@@ -258,26 +268,26 @@ def log_probs(logits, tokens, top: int = 0, out=None) -> LogProbs:
     """Log probabilities of tokens (int32 [...]) under logits (float32 or bfloat16 [..., vocab]), with entropy, log
     sum exp and the `top` (at most 64) most probable tokens, equal logits in the order of the tokens.  -inf masks
     a token; a token outside [0, vocab) is padding and has log probability 0."""
-    kind, rows, vocab, stride = _matrix("logits", logits)
+    dev = _device()
+    kind, rows, vocab, stride = _matrix("logits", logits, dev)
     lead = logits.shape[:-1]
-    ids = _vector("tokens", tokens, rows, torch.int32)
+    ids = _vector("tokens", tokens, rows, torch.int32, dev)
     _shaped("tokens", tokens, lead)
+    need = _bytes("fwg_log_probs_workspace", kind, rows, vocab, top)
     if out is None:
         def new(dtype, *more):
             return torch.empty(lead + more, dtype=dtype, device=logits.device)
         out = LogProbs(new(torch.float32), new(torch.float32), new(torch.float32), new(torch.int32, top),
                        new(torch.float32, top))
     logp, entropy, lse, top_ids, top_logp = out
-    lib = _library()
-    need = _bytes(lib.fwg_log_probs_workspace, kind, rows, vocab, top)
     ws = _workspace(need)
-    _check(lib.fwg_log_probs(kind, rows, vocab, logits.data_ptr(), stride, ids, top,
-                             _vector("out.logp", logp, rows, torch.float32),
-                             _vector("out.entropy", entropy, rows, torch.float32),
-                             _vector("out.lse", lse, rows, torch.float32),
-                             _vector("out.top_ids", top_ids, rows * top, torch.int32),
-                             _vector("out.top_logp", top_logp, rows * top, torch.float32),
-                             None if ws is None else ws.data_ptr(), need, _stream()))
+    _check(_library().fwg_log_probs(kind, rows, vocab, logits.data_ptr(), stride, ids, top,
+                             _vector("out.logp", logp, rows, torch.float32, dev),
+                             _vector("out.entropy", entropy, rows, torch.float32, dev),
+                             _vector("out.lse", lse, rows, torch.float32, dev),
+                             _vector("out.top_ids", top_ids, rows * top, torch.int32, dev),
+                             _vector("out.top_logp", top_logp, rows * top, torch.float32, dev),
+                             None if ws is None else ws.data_ptr(), need, _stream(dev)))
     return out if isinstance(out, LogProbs) else LogProbs(*out)
 
 
@@ -285,18 +295,19 @@ def log_probs_grad(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, o
     """The gradient of log_probs() with respect to the logits, from the gradients of logp and (optional) entropy;
     lse and entropy as log_probs() returned them (entropy may be None without grad_entropy).  out: of the logits'
     shape and type; may be the logits themselves."""
-    kind, rows, vocab, stride = _matrix("logits", logits)
-    ids = _vector("tokens", tokens, rows, torch.int32)
+    dev = _device()
+    kind, rows, vocab, stride = _matrix("logits", logits, dev)
+    ids = _vector("tokens", tokens, rows, torch.int32, dev)
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _typed("out", out, logits.dtype)
+    _typed("out", out, logits.dtype, dev)
     _shaped("out", out, logits.shape)
     if grad_entropy is not None and entropy is None:
         raise ValueError("grad_entropy is given without entropy")
     _check(_library().fwg_log_probs_grad(
-        kind, rows, vocab, logits.data_ptr(), stride, ids, _vector("lse", lse, rows, torch.float32),
-        None if entropy is None else _vector("entropy", entropy, rows, torch.float32),
-        _vector("grad_logp", grad_logp, rows, torch.float32),
-        None if grad_entropy is None else _vector("grad_entropy", grad_entropy, rows, torch.float32),
-        out.data_ptr(), _rows("out", out, True)[2], _stream()))
+        kind, rows, vocab, logits.data_ptr(), stride, ids, _vector("lse", lse, rows, torch.float32, dev),
+        None if entropy is None else _vector("entropy", entropy, rows, torch.float32, dev),
+        _vector("grad_logp", grad_logp, rows, torch.float32, dev),
+        None if grad_entropy is None else _vector("grad_entropy", grad_entropy, rows, torch.float32, dev),
+        out.data_ptr(), _rows("out", out, True)[2], _stream(dev)))
     return out

@@ -135,7 +135,7 @@ def test_tensor_checks_without_a_device():
         pytest.skip("the messages below are those of a machine without a GPU")
     x = torch.zeros((2, 4))
     with pytest.raises(TypeError):
-        ops._matrix("x", [1, 2])
+        ops._matrix("x", [1, 2], 0)
     for bad in (torch.zeros((2, 4, 3)).transpose(1, 2), torch.zeros(())):
         with pytest.raises(ValueError):
             ops._rows("x", bad)
