@@ -102,53 +102,69 @@ template <typename TO> __global__ void __launch_bounds__(256) tile_kernel(Matmul
 // through registers; else they pass through registers, which takes them at any address.
 constexpr int HT = 256, HK = 128, kHugeThreads = 512;
 constexpr int kStageBytes = 2 * HT * HK;
-constexpr int kHugeLds = 2 * kStageBytes + 3 * HT * (int)sizeof(float);
+constexpr int kHugeLds = 2 * kStageBytes + 2 * 3 * HT * (int)sizeof(float);
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ int piece_of(int row, int piece) { return piece ^ ((row >> 1) & 7); }
 
+// From memory to LDS without registers: lane l's bytes land at the (uniform) address + 16 l, or 4 l.
+__device__ __forceinline__ void copy_16(const int8_t *g, int8_t *l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
+                                   (__attribute__((address_space(3))) void *)l, 16, 0, 0);
+}
+__device__ __forceinline__ void copy_4(const float *g, float *l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
+                                   (__attribute__((address_space(3))) void *)l, 4, 0, 0);
+}
+
 template <typename TO, bool ALIGNED>
 __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int tiles_m, int tiles_n) {
   extern __shared__ __align__(1024) int8_t smem[];
+  float *const scales = (float *)(smem + 2 * kStageBytes);  // [2]: w_scale, bias, x_scale of the tile
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // each XCD (blocks go to the eight in turn) takes a contiguous share of the tiles, eight rows of tiles at a time
-  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8;
-  const int tile = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
-  if (tile >= tiles || (int)(blockIdx.x >> 3) >= share) return;
-  constexpr int G = 8;
-  const int band = tile / (G * tiles_n), in_band = tile - band * G * tiles_n;
-  const int high = min(G, tiles_m - band * G);
-  const int n0 = in_band / high * HT;
-  const int64_t m0 = (int64_t)(band * G + in_band % high) * HT;
-  const int wn = (wave >> 1) * 64, wm = (wave & 1) * 128;
+  const int wn = (wave >> 1) * 64, wm = (wave & 1) * 128, row = lane & 31, half = lane >> 5;
+  // Each XCD (blocks go to the eight in turn) takes a contiguous share of the tiles, eight rows of tiles at a time;
+  // its blocks go through the share together.
+  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = gridDim.x >> 3;
+  int tile = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
+  const int end = min(tiles, (int)(blockIdx.x & 7) * share + share);
+  if (tile >= end) return;
 
-  // a wave copies 32 rows of each operand, 8 rows of 8 pieces at a time; rows past the end are the last one again
-  auto from_w = [&](int r) { return a.w + (int64_t)min(n0 + r, a.N - 1) * a.ld_w; };
-  auto from_x = [&](int r) { return a.x + (m0 + r < a.M ? m0 + r : a.M - 1) * a.ld_x; };
-  const int8_t *gw[4], *gx[4];
+  // Copies: a wave brings 32 rows of each operand, 8 rows of 8 pieces at a time; rows past the end are the last one.
+  int n0;
+  int64_t m0;
+  const int8_t *bw, *bx;  // the tile's first rows
+  unsigned ow[4], ox[4];  // this lane's pieces from there (rows_fit: below 2^31)
+  auto go_to = [&](int t) {
+    constexpr int G = 8;
+    const int band = t / (G * tiles_n), in_band = t - band * G * tiles_n, high = min(G, tiles_m - band * G);
+    n0 = in_band / high * HT;
+    m0 = (int64_t)(band * G + in_band % high) * HT;
+    bw = a.w + n0 * a.ld_w;
+    bx = a.x + m0 * a.ld_x;
+    const int rows_w = min(HT, a.N - n0), rows_x = (int)min((int64_t)HT, a.M - m0);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = wave * 32 + i * 8 + (lane >> 3), p = piece_of(r, lane & 7) * 16;
-    gw[i] = from_w(r) + p;
-    gx[i] = from_x(r) + p;
-  }
+    for (int i = 0; i < 4; ++i) {
+      const int r = wave * 32 + i * 8 + (lane >> 3), p = piece_of(r, lane & 7) * 16;
+      ow[i] = (unsigned)min(r, rows_w - 1) * (unsigned)a.ld_w + p;
+      ox[i] = (unsigned)min(r, rows_x - 1) * (unsigned)a.ld_x + p;
+    }
+  };
   auto copy = [&](int k0, int buf) {
     int8_t *w = smem + buf * kStageBytes + wave * 32 * HK, *x = w + HT * HK;
     if (k0 + HK <= a.K) {
       if constexpr (ALIGNED) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gw[i] + k0),
-                                           (__attribute__((address_space(3))) void *)(w + i * 8 * HK), 16, 0, 0);
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gx[i] + k0),
-                                           (__attribute__((address_space(3))) void *)(x + i * 8 * HK), 16, 0, 0);
+          copy_16(bw + k0 + ow[i], w + i * 8 * HK);
+          copy_16(bx + k0 + ox[i], x + i * 8 * HK);
         }
       } else {
         i32x4 vw[4], vx[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          vw[i] = *(const i32x4_b *)(gw[i] + k0);
-          vx[i] = *(const i32x4_b *)(gx[i] + k0);
+          vw[i] = *(const i32x4_b *)(bw + k0 + ow[i]);
+          vx[i] = *(const i32x4_b *)(bx + k0 + ox[i]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -160,14 +176,26 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
 #pragma unroll 1
       for (int i = 0; i < 4; ++i) {
         const int r = wave * 32 + i * 8 + (lane >> 3), k = k0 + piece_of(r, lane & 7) * 16;
-        *(i32x4 *)(w + i * 8 * HK + lane * 16) = load16(from_w(r), k, a.K, true);
-        *(i32x4 *)(x + i * 8 * HK + lane * 16) = load16(from_x(r), k, a.K, true);
+        const int rw = min(r, a.N - 1 - n0), rx = (int)min((int64_t)r, a.M - 1 - m0);
+        *(i32x4 *)(w + i * 8 * HK + lane * 16) = load16(bw + rw * a.ld_w, k, a.K, true);
+        *(i32x4 *)(x + i * 8 * HK + lane * 16) = load16(bx + rx * a.ld_x, k, a.K, true);
       }
     }
   };
-  i32x16 acc[2][4] = {};
-  const int row = lane & 31, half = lane >> 5;
+  auto copy_scales = [&](int which) {  // waves 0 .. 3: 64 channels each, 4 .. 7: 64 rows each
+    float *to = scales + which * 3 * HT;
+    const int o = (wave & 3) * 64, n = min(n0 + o + lane, a.N - 1);
+    const int64_t m = m0 + o + lane;
+    if (wave < 4) {
+      copy_4(a.w_scale + n, to + o);
+      if (a.bias) copy_4(a.bias + n, to + HT + o);
+    } else {
+      copy_4(a.x_scale + (m < a.M ? m : a.M - 1), to + 2 * HT + o);
+    }
+  };
+
   // the operands of one k-step (32 bytes), read while the step before is multiplied
+  i32x16 acc[2][4] = {};
   i32x4 fw[2][2], fx[2][4];
   auto read = [&](int buf, int k, int slot) {
     const int8_t *w = smem + buf * kStageBytes + (wn + row) * HK, *x = smem + buf * kStageBytes + HT * HK + (wm + row) * HK;
@@ -193,81 +221,107 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
   };
-  copy(0, 0);
-  // the tile's scales and biases: w_scale, bias, x_scale
-  float *scales = (float *)(smem + 2 * kStageBytes);
-  if (threadIdx.x < HT) {
-    const int n = min(n0 + (int)threadIdx.x, a.N - 1);
-    scales[threadIdx.x] = a.w_scale[n];
-    scales[HT + threadIdx.x] = a.bias ? a.bias[n] : 0.f;
-  } else {
-    const int64_t m = m0 + threadIdx.x - HT;
-    scales[HT + threadIdx.x] = a.x_scale[m < a.M ? m : a.M - 1];
-  }
-  __syncthreads();
-  read(0, 0, 0);
-  int buf = 0;
-  for (int k0 = 0; k0 < a.K; k0 += HK) {
-    if (k0 + HK < a.K) copy(k0 + HK, buf ^ 1);
+
+  // Results: a wave's 64 outputs x 128 rows pass through 8 KB of LDS (of the stage that was multiplied last), so that
+  // they go out in whole 128-byte lines: 64 rows of 128 bytes at a time (64 bf16, or 32 float32), pieces of 16 bytes
+  // permuted by the row.
+  auto write = [&](int8_t *mine, const float *sc, int n_at, int64_t m_at) {
+    constexpr int kTiles = sizeof(TO) == 2 ? 2 : 1;  // 32-output tiles of a line
+    constexpr int E = 16 / sizeof(TO);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      read(buf, k + 1, (k + 1) & 1);
-      multiply(k & 1);
-      interleave();
-    }
-    __syncthreads();
-    buf ^= 1;
-    read(buf, 0, 0);  // after the last stage: unused
-    multiply(1);
-    interleave();
-  }
-  __syncthreads();
-  // The results of a wave pass through its eighth of the LDS, so that rows go out in whole 128-byte lines: as rows of
-  // 128 bytes (64 bf16, or 32 float32 at a time), pieces of 16 bytes permuted by the row.
-  constexpr int kTiles = sizeof(TO) == 2 ? 2 : 1;  // 32-output tiles of a line
-  int8_t *mine = smem + wave * (2 * kStageBytes / 8);
+    for (int i0 = 0; i0 < 2; i0 += kTiles) {
 #pragma unroll
-  for (int i0 = 0; i0 < 2; i0 += kTiles) {
-    if (i0) in_order();
+      for (int j0 = 0; j0 < 4; j0 += 2) {
+        in_order();
 #pragma unroll
-    for (int ii = 0; ii < kTiles; ++ii) {
-      const int i = i0 + ii;
+        for (int ii = 0; ii < kTiles; ++ii) {
+          const int i = i0 + ii;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int n = wn + i * 32 + g * 8 + half * 4;
-        const f32x4 ws = *(const f32x4 *)(scales + n), b = *(const f32x4 *)(scales + HT + n);
+          for (int g = 0; g < 4; ++g) {
+            const int n = wn + i * 32 + g * 8 + half * 4;
+            const f32x4 ws = *(const f32x4 *)(sc + n), b = *(const f32x4 *)(sc + HT + n);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float sx = scales[2 * HT + wm + j * 32 + row];
-          float v[4];
+            for (int jj = 0; jj < 2; ++jj) {
+              const float sx = sc[2 * HT + wm + (j0 + jj) * 32 + row];
+              float v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = (float)acc[i][j][4 * g + e] * sx * ws[e];
-            if (a.bias) v[e] += b[e];
+              for (int e = 0; e < 4; ++e) {
+                v[e] = (float)acc[i][j0 + jj][4 * g + e] * sx * ws[e];
+                if (a.bias) v[e] += b[e];
+              }
+              const int at = (ii * 32 + g * 8 + half * 4) * (int)sizeof(TO), r = jj * 32 + row;
+              store((TO *)(mine + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15)), v);
+            }
           }
-          const int at = (ii * 32 + g * 8 + half * 4) * (int)sizeof(TO), r = j * 32 + row;
-          store((TO *)(mine + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15)), v);
+        }
+        in_order();
+        const int n = n_at + wn + i0 * 32 + (lane & 7) * E;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int r = q * 8 + (lane >> 3);
+          const int64_t m = m_at + wm + j0 * 32 + r;
+          const int8_t *line = mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4);
+          if (m >= a.M) continue;
+          TO *out = (TO *)a.out + m * a.ld_o + n;
+          if (n + E <= a.N) {
+            *(u32x4_el *)out = *(const u32x4 *)line;
+          } else {
+            for (int k = 0; k < E; ++k)
+              if (n + k < a.N) out[k] = ((const TO *)line)[k];
+          }
         }
       }
     }
-    in_order();
-    constexpr int E = 16 / sizeof(TO);
-    const int n = n0 + wn + i0 * 32 + (lane & 7) * E;
+  };
+
+  go_to(tile);
+  copy(0, 0);
+  copy_scales(0);
+  __syncthreads();
+  int buf = 0, which = 0;
+  while (true) {
+    const int n_at = n0, next = tile + stride;
+    const int64_t m_at = m0;
+    read(buf, 0, 0);
+    auto three_steps = [&] {
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const int r = q * 8 + (lane >> 3);
-      const int64_t m = m0 + wm + r;
-      const u32x4 v = *(const u32x4 *)(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-      if (m >= a.M) continue;
-      TO *out = (TO *)a.out + m * a.ld_o + n;
-      if (n + E <= a.N) {
-        *(u32x4_el *)out = v;
-      } else {
-        const TO *e = (const TO *)(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-        for (int k = 0; k < E; ++k)
-          if (n + k < a.N) out[k] = e[k];
+      for (int k = 0; k < 3; ++k) {
+        read(buf, k + 1, (k + 1) & 1);
+        multiply(k & 1);
+        interleave();
       }
+      __syncthreads();  // the next stage has arrived, and this one has been read
+    };
+    int k0 = 0;
+    for (; k0 + HK < a.K; k0 += HK) {
+      copy(k0 + HK, buf ^ 1);
+      three_steps();
+      buf ^= 1;
+      read(buf, 0, 0);
+      multiply(1);
+      interleave();
     }
+    // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
+    if (next < end) {
+      go_to(next);
+      copy(0, buf ^ 1);
+      copy_scales(which ^ 1);
+    }
+    three_steps();
+    multiply(1);
+    write(smem + buf * kStageBytes + wave * (kStageBytes / 8), scales + which * 3 * HT, n_at, m_at);
+    if (next >= end) break;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = i32x16{};
+    tile = next;
+    buf ^= 1;
+    which ^= 1;
+    // the LDS just used may be copied over now; the results on their way out are not waited for
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   }
 }
 
@@ -276,14 +330,16 @@ template <typename TO, bool ALIGNED> hipError_t run_huge(const MatmulArgs &a, hi
                                                     hipFuncAttributeMaxDynamicSharedMemorySize, kHugeLds);
   if (set != hipSuccess) return set;
   const int tm = (int)((a.M + HT - 1) / HT), tn = (a.N + HT - 1) / HT;
-  const unsigned grid = (unsigned)(((int64_t)tm * tn + 7) / 8 * 8);
+  const int64_t blocks = ((int64_t)tm * tn + 7) / 8 * 8;
+  const unsigned grid = blocks < 256 ? (unsigned)blocks : 256;  // one per compute unit: they fill its LDS
   hipLaunchKernelGGL((huge_kernel<TO, ALIGNED>), dim3(grid), dim3(kHugeThreads), kHugeLds, s, a, tm, tn);
   return hipGetLastError();
 }
 
 template <typename TO> hipError_t run(const MatmulArgs &a, hipStream_t s) {
   const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
-  if ((a.M + HT - 1) / HT * ((a.N + HT - 1) / HT) >= 128)
+  const bool rows_fit = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
+  if (rows_fit && (a.M + HT - 1) / HT * ((a.N + HT - 1) / HT) >= 128)
     return aligned ? run_huge<TO, true>(a, s) : run_huge<TO, false>(a, s);
   hipLaunchKernelGGL((tile_kernel<TO>), dim3((a.N + BN - 1) / BN, (unsigned)((a.M + BM - 1) / BM)), dim3(256), 0, s, a);
   return hipGetLastError();
