@@ -8,6 +8,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fwg.h"
 #include "fwg_ops.h"
 #include "fwg_ops_dev.h"
@@ -27,10 +29,10 @@ __device__ __forceinline__ i32x4 mma(const i32x4 &a, const i32x4 &b, const i32x4
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
-// 16 bytes of a row from byte k on; bytes from K on and absent rows are 0.
-__device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K, bool exists) {
+// 16 bytes of a row from byte k on; bytes from K on are 0.
+__device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K) {
   i32x4 v = {0, 0, 0, 0};
-  if (!exists || k >= K) return v;
+  if (k >= K) return v;
   if (k + 16 <= K) return *(const i32x4_b *)(row + k);
   if (K >= 16) {  // the row's last 16 bytes, shifted down
     const unsigned __int128 last = __builtin_bit_cast(unsigned __int128, (i32x4)*(const i32x4_b *)(row + K - 16));
@@ -42,70 +44,25 @@ __device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K, bool ex
   return __builtin_bit_cast(i32x4, part);
 }
 
-// Four outputs n .. n + 3 of row m.
-template <typename TO>
-__device__ __forceinline__ void epilogue(const MatmulArgs &a, int64_t m, int n, const i32x4 &c) {
-  if (m >= a.M || n >= a.N) return;
-  const float sx = a.x_scale[m];
-  const int have = a.N - n;
-  float v[4], ws[4], b[4];
-  load_part(a.w_scale + n, have, 0.f, ws);
-  if (a.bias) load_part(a.bias + n, have, 0.f, b);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = (float)c[i] * sx * ws[i];
-    if (a.bias) v[i] += b[i];
-  }
-  store_part((TO *)a.out + m * a.ld_o + n, have, v);
-}
-
-// 128 outputs x 128 rows per block of four waves, 64 bytes of k at a time through LDS.
-constexpr int BM = 128, BN = 128, BK = 64, PAD = 16;
-template <typename TO> __global__ void __launch_bounds__(256) tile_kernel(MatmulArgs a) {
-  __shared__ __align__(16) int8_t sw[BN][BK + PAD], sx[BM][BK + PAD];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int n0 = blockIdx.x * BN;
-  const int64_t m0 = (int64_t)blockIdx.y * BM;
-  const int wn = (wave & 1) * 64, wm = (wave >> 1) * 64;
-  i32x4 acc[4][4] = {};
-  for (int k0 = 0; k0 < a.K; k0 += BK) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int p = i * 256 + t, r = p >> 2, k = (p & 3) * 16;
-      *(i32x4 *)&sw[r][k] = load16(a.w + (int64_t)(n0 + r) * a.ld_w, k0 + k, a.K, n0 + r < a.N);
-      *(i32x4 *)&sx[r][k] = load16(a.x + (m0 + r) * a.ld_x, k0 + k, a.K, m0 + r < a.M);
-    }
-    __syncthreads();
-    i32x4 fw[4], fx[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      fw[i] = *(const i32x4 *)&sw[wn + 16 * i + (lane & 15)][(lane >> 4) * 16];
-      fx[i] = *(const i32x4 *)&sx[wm + 16 * i + (lane & 15)][(lane >> 4) * 16];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = mma(fw[i], fx[j], acc[i][j]);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      epilogue<TO>(a, m0 + wm + 16 * j + (lane & 15), n0 + wn + 16 * i + (lane >> 4) * 4, acc[i][j]);
-}
-
-// 256 outputs x 256 rows per block of eight waves, 128 bytes of k per stage, two stages in LDS (128 KB): one is filled
-// while the other is multiplied.  A wave multiplies 64 outputs x 128 rows (v_mfma_i32_32x32x32_i8).  A stage's rows are
-// 128 bytes; the 16-byte pieces of row r lie permuted by (r >> 1) & 7, so that the 32 rows that an instruction reads
-// at one k spread over the banks.  ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without passing
-// through registers; else they pass through registers, which takes them at any address.
-constexpr int HT = 256, HK = 128, kHugeThreads = 512;
-constexpr int kStageBytes = 2 * HT * HK;
-constexpr int kHugeLds = 2 * kStageBytes + 2 * 3 * HT * (int)sizeof(float);
+// Tiles of T outputs x T rows (256: eight waves; 128: four), 128 bytes of k per stage, two stages in LDS: one is filled
+// while the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows (v_mfma_i32_32x32x32_i8).  A stage's rows
+// are 128 bytes; the 16-byte pieces of row r lie permuted by (r >> 1) & 7, so that the 32 rows that an instruction
+// reads at one k spread over the banks.  ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without
+// passing through registers; else they pass through registers, which takes them at any address.  TO = int: sums of a
+// part of k go to the workspace as they are.
+constexpr int HK = 128;
+template <int T> struct Tile {
+  static constexpr int kWaves = T / 32, kThreads = 64 * kWaves, kWM = T / 2, kJ = kWM / 32;
+  static constexpr int kStage = 2 * T * HK;                               // bytes of a stage: weights, then rows
+  static constexpr int kLds = 2 * kStage + 2 * 3 * T * (int)sizeof(float);  // two stages, two tiles' scales
+};
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ int piece_of(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+
+struct Cut {
+  int tiles_m, tiles_n, splits, per;  // k is cut into `splits` parts of `per` bytes (a multiple of HK)
+};
 
 // From memory to LDS without registers: lane l's bytes land at the (uniform) address + 16 l, or 4 l.
 __device__ __forceinline__ void copy_16(const int8_t *g, int8_t *l) {
@@ -117,12 +74,17 @@ __device__ __forceinline__ void copy_4(const float *g, float *l) {
                                    (__attribute__((address_space(3))) void *)l, 4, 0, 0);
 }
 
-template <typename TO, bool ALIGNED>
-__global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int tiles_m, int tiles_n) {
+template <typename TO, bool ALIGNED, int T>
+__global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulArgs a, Cut cut) {
+  constexpr int J = Tile<T>::kJ, kStage = Tile<T>::kStage;
+  constexpr bool kSums = std::is_same<TO, int>::value;
   extern __shared__ __align__(1024) int8_t smem[];
-  float *const scales = (float *)(smem + 2 * kStageBytes);  // [2]: w_scale, bias, x_scale of the tile
+  float *const scales = (float *)(smem + 2 * kStage);  // [2]: w_scale, bias, x_scale of the tile
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wn = (wave >> 1) * 64, wm = (wave & 1) * 128, row = lane & 31, half = lane >> 5;
+  const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T>::kWM, row = lane & 31, half = lane >> 5;
+  const int tiles_m = cut.tiles_m, tiles_n = cut.tiles_n;
+  const int k_at = (int)blockIdx.y * cut.per, k_end = min(a.K, k_at + cut.per);
+  TO *const result = (TO *)a.out + (kSums ? (int64_t)blockIdx.y * a.M * a.ld_o : 0);
   // Each XCD (blocks go to the eight in turn) takes a contiguous share of the tiles, eight rows of tiles at a time;
   // its blocks go through the share together.
   const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = gridDim.x >> 3;
@@ -133,25 +95,30 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
   // Copies: a wave brings 32 rows of each operand, 8 rows of 8 pieces at a time; rows past the end are the last one.
   int n0;
   int64_t m0;
-  const int8_t *bw, *bx;  // the tile's first rows
-  unsigned ow[4], ox[4];  // this lane's pieces from there (rows_fit: below 2^31)
+  const int8_t *bw, *bx;                    // the tile's first rows
+  int rows_w, rows_x;
+  unsigned ow[4], ox[4];                    // ALIGNED: this lane's pieces from there (below 2^31)
+  const int cr = wave * 32 + (lane >> 3);   // the first of the lane's rows; the others follow 8 apart
   auto go_to = [&](int t) {
     constexpr int G = 8;
     const int band = t / (G * tiles_n), in_band = t - band * G * tiles_n, high = min(G, tiles_m - band * G);
-    n0 = in_band / high * HT;
-    m0 = (int64_t)(band * G + in_band % high) * HT;
+    n0 = in_band / high * T;
+    m0 = (int64_t)(band * G + in_band % high) * T;
     bw = a.w + n0 * a.ld_w;
     bx = a.x + m0 * a.ld_x;
-    const int rows_w = min(HT, a.N - n0), rows_x = (int)min((int64_t)HT, a.M - m0);
+    rows_w = min(T, a.N - n0);
+    rows_x = (int)min((int64_t)T, a.M - m0);
+    if constexpr (ALIGNED) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = wave * 32 + i * 8 + (lane >> 3), p = piece_of(r, lane & 7) * 16;
-      ow[i] = (unsigned)min(r, rows_w - 1) * (unsigned)a.ld_w + p;
-      ox[i] = (unsigned)min(r, rows_x - 1) * (unsigned)a.ld_x + p;
+      for (int i = 0; i < 4; ++i) {
+        const int r = cr + i * 8, p = piece_of(r, lane & 7) * 16;
+        ow[i] = (unsigned)min(r, rows_w - 1) * (unsigned)a.ld_w + p;
+        ox[i] = (unsigned)min(r, rows_x - 1) * (unsigned)a.ld_x + p;
+      }
     }
   };
   auto copy = [&](int k0, int buf) {
-    int8_t *w = smem + buf * kStageBytes + wave * 32 * HK, *x = w + HT * HK;
+    int8_t *w = smem + buf * kStage + wave * 32 * HK, *x = w + T * HK;
     if (k0 + HK <= a.K) {
       if constexpr (ALIGNED) {
 #pragma unroll
@@ -163,8 +130,9 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
         i32x4 vw[4], vx[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          vw[i] = *(const i32x4_b *)(bw + k0 + ow[i]);
-          vx[i] = *(const i32x4_b *)(bx + k0 + ox[i]);
+          const int r = cr + i * 8, p = k0 + piece_of(r, lane & 7) * 16;
+          vw[i] = *(const i32x4_b *)(bw + min(r, rows_w - 1) * a.ld_w + p);
+          vx[i] = *(const i32x4_b *)(bx + min(r, rows_x - 1) * a.ld_x + p);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -175,39 +143,40 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
     } else {  // the last stage, where K ends inside it
 #pragma unroll 1
       for (int i = 0; i < 4; ++i) {
-        const int r = wave * 32 + i * 8 + (lane >> 3), k = k0 + piece_of(r, lane & 7) * 16;
-        const int rw = min(r, a.N - 1 - n0), rx = (int)min((int64_t)r, a.M - 1 - m0);
-        *(i32x4 *)(w + i * 8 * HK + lane * 16) = load16(bw + rw * a.ld_w, k, a.K, true);
-        *(i32x4 *)(x + i * 8 * HK + lane * 16) = load16(bx + rx * a.ld_x, k, a.K, true);
+        const int r = cr + i * 8, p = k0 + piece_of(r, lane & 7) * 16;
+        *(i32x4 *)(w + i * 8 * HK + lane * 16) = load16(bw + min(r, rows_w - 1) * a.ld_w, p, a.K);
+        *(i32x4 *)(x + i * 8 * HK + lane * 16) = load16(bx + min(r, rows_x - 1) * a.ld_x, p, a.K);
       }
     }
   };
-  auto copy_scales = [&](int which) {  // waves 0 .. 3: 64 channels each, 4 .. 7: 64 rows each
-    float *to = scales + which * 3 * HT;
-    const int o = (wave & 3) * 64, n = min(n0 + o + lane, a.N - 1);
+  auto copy_scales = [&](int which) {  // the first half of the waves: 64 channels each, the others: 64 rows each
+    if constexpr (kSums) return;
+    constexpr int kHalf = Tile<T>::kWaves / 2;
+    float *to = scales + which * 3 * T;
+    const int o = (wave % kHalf) * 64, n = min(n0 + o + lane, a.N - 1);
     const int64_t m = m0 + o + lane;
-    if (wave < 4) {
+    if (wave < kHalf) {
       copy_4(a.w_scale + n, to + o);
-      if (a.bias) copy_4(a.bias + n, to + HT + o);
+      if (a.bias) copy_4(a.bias + n, to + T + o);
     } else {
-      copy_4(a.x_scale + (m < a.M ? m : a.M - 1), to + 2 * HT + o);
+      copy_4(a.x_scale + (m < a.M ? m : a.M - 1), to + 2 * T + o);
     }
   };
 
   // the operands of one k-step (32 bytes), read while the step before is multiplied
-  i32x16 acc[2][4] = {};
-  i32x4 fw[2][2], fx[2][4];
+  i32x16 acc[2][J] = {};
+  i32x4 fw[2][2], fx[2][J];
   auto read = [&](int buf, int k, int slot) {
-    const int8_t *w = smem + buf * kStageBytes + (wn + row) * HK, *x = smem + buf * kStageBytes + HT * HK + (wm + row) * HK;
+    const int8_t *w = smem + buf * kStage + (wn + row) * HK, *x = smem + buf * kStage + T * HK + (wm + row) * HK;
     const int p = piece_of(row, 2 * k + half) * 16;  // wn, wm and 32 leave (r >> 1) & 7 as it is
 #pragma unroll
     for (int i = 0; i < 2; ++i) fw[slot][i] = *(const i32x4 *)(w + i * 32 * HK + p);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) fx[slot][j] = *(const i32x4 *)(x + j * 32 * HK + p);
+    for (int j = 0; j < J; ++j) fx[slot][j] = *(const i32x4 *)(x + j * 32 * HK + p);
   };
   auto multiply = [&](int slot) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[slot][i], fx[slot][j], acc[i][j], 0, 0, 0);
@@ -215,14 +184,14 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
   // one read between two products
   auto interleave = [] {
 #pragma unroll
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < min(2 + J, 2 * J); ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+    if constexpr (J > 2) __builtin_amdgcn_sched_group_barrier(0x008, J - 2, 0);
   };
 
-  // Results: a wave's 64 outputs x 128 rows pass through 8 KB of LDS (of the stage that was multiplied last), so that
+  // Results: a wave's 64 outputs x T / 2 rows pass through 8 KB of LDS (of the stage that was multiplied last), so that
   // they go out in whole 128-byte lines: 64 rows of 128 bytes at a time (64 bf16, or 32 float32), pieces of 16 bytes
   // permuted by the row.
   auto write = [&](int8_t *mine, const float *sc, int n_at, int64_t m_at) {
@@ -231,7 +200,7 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
 #pragma unroll
     for (int i0 = 0; i0 < 2; i0 += kTiles) {
 #pragma unroll
-      for (int j0 = 0; j0 < 4; j0 += 2) {
+      for (int j0 = 0; j0 < J; j0 += 2) {
         in_order();
 #pragma unroll
         for (int ii = 0; ii < kTiles; ++ii) {
@@ -239,18 +208,24 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int n = wn + i * 32 + g * 8 + half * 4;
-            const f32x4 ws = *(const f32x4 *)(sc + n), b = *(const f32x4 *)(sc + HT + n);
+            const f32x4 ws = *(const f32x4 *)(sc + n), b = *(const f32x4 *)(sc + T + n);
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
-              const float sx = sc[2 * HT + wm + (j0 + jj) * 32 + row];
-              float v[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                v[e] = (float)acc[i][j0 + jj][4 * g + e] * sx * ws[e];
-                if (a.bias) v[e] += b[e];
-              }
+              const float sx = sc[2 * T + wm + (j0 + jj) * 32 + row];
               const int at = (ii * 32 + g * 8 + half * 4) * (int)sizeof(TO), r = jj * 32 + row;
-              store((TO *)(mine + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15)), v);
+              int8_t *to = mine + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15);
+              if constexpr (kSums) {
+                *(i32x4 *)to = i32x4{acc[i][j0 + jj][4 * g], acc[i][j0 + jj][4 * g + 1], acc[i][j0 + jj][4 * g + 2],
+                                     acc[i][j0 + jj][4 * g + 3]};
+              } else {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  v[e] = (float)acc[i][j0 + jj][4 * g + e] * sx * ws[e];
+                  if (a.bias) v[e] += b[e];
+                }
+                store((TO *)to, v);
+              }
             }
           }
         }
@@ -262,7 +237,7 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
           const int64_t m = m_at + wm + j0 * 32 + r;
           const int8_t *line = mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4);
           if (m >= a.M) continue;
-          TO *out = (TO *)a.out + m * a.ld_o + n;
+          TO *out = result + m * a.ld_o + n;
           if (n + E <= a.N) {
             *(u32x4_el *)out = *(const u32x4 *)line;
           } else {
@@ -275,7 +250,7 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
   };
 
   go_to(tile);
-  copy(0, 0);
+  copy(k_at, 0);
   copy_scales(0);
   __syncthreads();
   int buf = 0, which = 0;
@@ -292,8 +267,7 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
       }
       __syncthreads();  // the next stage has arrived, and this one has been read
     };
-    int k0 = 0;
-    for (; k0 + HK < a.K; k0 += HK) {
+    for (int k0 = k_at; k0 + HK < k_end; k0 += HK) {
       copy(k0 + HK, buf ^ 1);
       three_steps();
       buf ^= 1;
@@ -304,17 +278,17 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
     // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
     if (next < end) {
       go_to(next);
-      copy(0, buf ^ 1);
+      copy(k_at, buf ^ 1);
       copy_scales(which ^ 1);
     }
     three_steps();
     multiply(1);
-    write(smem + buf * kStageBytes + wave * (kStageBytes / 8), scales + which * 3 * HT, n_at, m_at);
+    write(smem + buf * kStage + wave * 8192, scales + which * 3 * T, n_at, m_at);
     if (next >= end) break;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = i32x16{};
+      for (int j = 0; j < J; ++j) acc[i][j] = i32x16{};
     tile = next;
     buf ^= 1;
     which ^= 1;
@@ -325,29 +299,168 @@ __global__ void __launch_bounds__(kHugeThreads) huge_kernel(MatmulArgs a, int ti
   }
 }
 
-template <typename TO, bool ALIGNED> hipError_t run_huge(const MatmulArgs &a, hipStream_t s) {
-  static const hipError_t set = hipFuncSetAttribute((const void *)huge_kernel<TO, ALIGNED>,
-                                                    hipFuncAttributeMaxDynamicSharedMemorySize, kHugeLds);
+// Few rows (M <= 16 MT): the weights are read once, straight into registers, by as many waves as there are tiles of
+// 16 NT outputs x a quarter of k; the rows come from the caches.  The four waves of a block take 128 bytes of k in turn
+// (so a block reads 512 consecutive bytes of each weight row) and their sums meet in LDS.
+template <typename TO, int MT, int NT>
+__global__ void __launch_bounds__(256) rows_kernel(MatmulArgs a) {
+  constexpr int kUnits = MT * NT >= 8 ? 1 : MT * NT >= 4 ? 2 : 4;  // 128-byte pieces of k in flight per wave
+  __shared__ int sums[4][MT * 16][NT * 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, p = (lane >> 4) * 16;
+  const int n0 = blockIdx.x * (16 * NT);
+  const int8_t *w[NT], *x[MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) w[i] = a.w + (int64_t)min(n0 + i * 16 + r, a.N - 1) * a.ld_w;
+#pragma unroll
+  for (int j = 0; j < MT; ++j) x[j] = a.x + (int64_t)min(j * 16 + r, (int)a.M - 1) * a.ld_x;
+  i32x4 acc[NT][MT] = {};
+  int k = wave * 128;
+  for (; k + (kUnits - 1) * 512 + 128 <= a.K; k += kUnits * 512) {
+    i32x4 vw[kUnits][2][NT], vx[kUnits][2][MT];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) vw[u][h][i] = *(const i32x4_b *)(w[i] + k + u * 512 + h * 64 + p);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) vx[u][h][j] = *(const i32x4_b *)(x[j] + k + u * 512 + h * 64 + p);
+      }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < MT; ++j) acc[i][j] = mma(vw[u][h][i], vx[u][h][j], acc[i][j]);
+  }
+#pragma unroll 1
+  for (; k < a.K; k += 512) {
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+      i32x4 vw[NT], vx[MT];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) vw[i] = load16(w[i], k + h * 64 + p, a.K);
+#pragma unroll
+      for (int j = 0; j < MT; ++j) vx[j] = load16(x[j], k + h * 64 + p, a.K);
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = mma(vw[i], vx[j], acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) *(i32x4 *)&sums[wave][j * 16 + r][i * 16 + (lane >> 4) * 4] = acc[i][j];
+  __syncthreads();
+  for (int t = threadIdx.x; t < MT * NT * 256; t += 256) {
+    const int m = t / (16 * NT), c = t % (16 * NT), n = n0 + c;
+    if (m >= a.M || n >= a.N) continue;
+    const int sum = sums[0][m][c] + sums[1][m][c] + sums[2][m][c] + sums[3][m][c];
+    float v = (float)sum * a.x_scale[m] * a.w_scale[n];
+    if (a.bias) v += a.bias[n];
+    put((TO *)a.out + m * a.ld_o + n, v);
+  }
+}
+
+// Adds the parts of k up: whole numbers, so their order does not matter.
+template <typename TO> __global__ void __launch_bounds__(256) add_kernel(MatmulArgs a, int splits) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = a.M * a.N;
+  if (i >= all) return;
+  const int *sums = (const int *)a.ws;
+  if (i + 4 <= all && a.N % 4 == 0) {
+    i32x4 c = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) c += *(const i32x4 *)(sums + s * all + i);
+    const int64_t m = i / a.N;
+    const int n = (int)(i - m * a.N);
+    const float sx = a.x_scale[m];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = (float)c[e] * sx * a.w_scale[n + e];
+      if (a.bias) v[e] += a.bias[n + e];
+    }
+    store((TO *)a.out + m * a.ld_o + n, v);
+    return;
+  }
+  for (int64_t e = i; e < i + 4 && e < all; ++e) {
+    int c = 0;
+    for (int s = 0; s < splits; ++s) c += sums[s * all + e];
+    const int64_t m = e / a.N;
+    const int n = (int)(e - m * a.N);
+    float v = (float)c * a.x_scale[m] * a.w_scale[n];
+    if (a.bias) v += a.bias[n];
+    put((TO *)a.out + m * a.ld_o + n, v);
+  }
+}
+
+constexpr int kRowsMost = 64;  // rows_kernel's
+// How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.
+int cut_of(int64_t M, int N, int K, Cut *c) {
+  const int64_t big = (M + 255) / 256 * ((N + 255) / 256);
+  const int side = big >= 192 ? 256 : 128;
+  c->tiles_m = (int)((M + side - 1) / side);
+  c->tiles_n = (N + side - 1) / side;
+  const int64_t tiles = (int64_t)c->tiles_m * c->tiles_n;
+  const int stages = (K + HK - 1) / HK;
+  int64_t splits = side == 256 ? 1 : 512 / tiles;
+  if (splits > stages / 4) splits = stages / 4;  // a part shorter than four stages costs more than it saves
+  if (splits < 1) splits = 1;
+  c->per = (int)((stages + splits - 1) / splits) * HK;
+  c->splits = (K + c->per - 1) / c->per;
+  return side;
+}
+
+template <typename TO, bool ALIGNED, int T> hipError_t run_tiles(const MatmulArgs &a, const Cut &c, hipStream_t s) {
+  static const hipError_t set = hipFuncSetAttribute((const void *)tile_kernel<TO, ALIGNED, T>,
+                                                    hipFuncAttributeMaxDynamicSharedMemorySize, Tile<T>::kLds);
   if (set != hipSuccess) return set;
-  const int tm = (int)((a.M + HT - 1) / HT), tn = (a.N + HT - 1) / HT;
-  const int64_t blocks = ((int64_t)tm * tn + 7) / 8 * 8;
-  const unsigned grid = blocks < 256 ? (unsigned)blocks : 256;  // one per compute unit: they fill its LDS
-  hipLaunchKernelGGL((huge_kernel<TO, ALIGNED>), dim3(grid), dim3(kHugeThreads), kHugeLds, s, a, tm, tn);
+  // a block goes through several tiles where there are more than the device holds (one of 256, or two of 128 per
+  // compute unit)
+  const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = T == 256 ? 256 : 512;
+  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, T>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)c.splits),
+                     dim3(Tile<T>::kThreads), Tile<T>::kLds, s, a, c);
+  return hipGetLastError();
+}
+
+template <typename TO, int T> hipError_t run_cut(const MatmulArgs &a, const Cut &c, hipStream_t s) {
+  const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
+  const bool near = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
+  return aligned && near ? run_tiles<TO, true, T>(a, c, s) : run_tiles<TO, false, T>(a, c, s);
+}
+
+template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((rows_kernel<TO, MT, NT>), dim3((a.N + 16 * NT - 1) / (16 * NT)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename TO> hipError_t run(const MatmulArgs &a, hipStream_t s) {
-  const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
-  const bool rows_fit = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
-  if (rows_fit && (a.M + HT - 1) / HT * ((a.N + HT - 1) / HT) >= 128)
-    return aligned ? run_huge<TO, true>(a, s) : run_huge<TO, false>(a, s);
-  hipLaunchKernelGGL((tile_kernel<TO>), dim3((a.N + BN - 1) / BN, (unsigned)((a.M + BM - 1) / BM)), dim3(256), 0, s, a);
+  if (a.M <= 16) return run_rows<TO, 1, 1>(a, s);
+  if (a.M <= 32) return a.N >= 8192 ? run_rows<TO, 2, 2>(a, s) : run_rows<TO, 2, 1>(a, s);
+  if (a.M <= kRowsMost) return a.N >= 16384 ? run_rows<TO, 4, 4>(a, s) : run_rows<TO, 4, 1>(a, s);
+  Cut c;
+  if (cut_of(a.M, a.N, a.K, &c) == 256) return run_cut<TO, 256>(a, c, s);
+  if (c.splits == 1) return run_cut<TO, 128>(a, c, s);
+  MatmulArgs b = a;
+  b.out = a.ws;
+  b.ld_o = a.N;
+  const hipError_t e = run_cut<int, 128>(b, c, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((add_kernel<TO>), dim3((unsigned)((a.M * a.N + 1023) / 1024)), dim3(256), 0, s, a, c.splits);
   return hipGetLastError();
 }
 
 }  // namespace mmq
 
-size_t matmul_quant_bytes(int64_t, int, int) { return 0; }
+size_t matmul_quant_bytes(int64_t rows, int outputs, int inner) {
+  if (rows <= mmq::kRowsMost) return 0;
+  mmq::Cut c;
+  const int side = mmq::cut_of(rows, outputs, inner, &c);
+  return side == 128 && c.splits > 1 ? (size_t)c.splits * rows * outputs * sizeof(int) : 0;
+}
 
 hipError_t launch_matmul_quant(const MatmulArgs &a, int out_dtype, hipStream_t s) {
   return out_dtype == FWG_BF16 ? mmq::run<uint16_t>(a, s) : mmq::run<float>(a, s);

@@ -338,6 +338,35 @@ def test_matmul_quant_large(M, N, K):
     check_matmul(bytes_(1, M, K), bytes_(2, N, K), None, 4, BF16)
 
 
+@pytest.mark.parametrize("M,N,K", [(4100, 8200, 200), (4099, 8193, 128), (130, 48001, 130), (257, 40000, 129)])
+def test_matmul_quant_several_tiles_per_block(M, N, K):
+    """More tiles than the device holds blocks, with ragged last ones, K of one and two stages and a byte more."""
+    x, w, b = bytes_(1, M, K), bytes_(2, N, K), randn(3, N)
+    check_matmul(x, w, b, 4, BF16)
+    check_matmul(odd_view(x), odd_view(w), None, 4, F32)
+
+
+@pytest.mark.parametrize("M,N,K", [(70, 90, 8192), (100, 300, 5001), (300, 515, 4097), (129, 129, 1100)])
+def test_matmul_quant_k_in_parts(M, N, K):
+    """Few tiles and a long sum: parts of k are summed apart and added."""
+    x, w, b = bytes_(1, M, K), bytes_(2, N, K), randn(3, N)
+    check_matmul(x, w, b, 4, F32)
+    check_matmul(x, w, None, 4, BF16)
+    check_matmul(odd_view(x, 2), odd_view(w), b, 4, F32)
+
+
+def test_matmul_quant_rows_far_apart():
+    """Rows megabytes apart: offsets inside a tile pass 2^31."""
+    K, far = 300, (1 << 23) + 16
+    x = torch.zeros((200, far), dtype=torch.int8, device="cuda")[:, :K]
+    x.copy_(bytes_(1, 200, K))
+    w = torch.zeros((260, far), dtype=torch.int8, device="cuda")[:, :K]
+    w.copy_(bytes_(2, 260, K))
+    check_matmul(x, w, randn(3, 260), 4, F32)
+    check_matmul(x[:9], w, None, 4, F32)
+    check_matmul(x[:50], w, None, 4, BF16)
+
+
 def test_matmul_quant_scales_not_finite():
     """A row or channel whose scale is NaN (a poisoned 8-bit row) poisons its own outputs only."""
     x, w = bytes_(1, 20, 64), bytes_(2, 30, 64)
