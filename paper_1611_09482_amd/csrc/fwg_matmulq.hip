@@ -301,10 +301,9 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulArgs a
 
 // Few rows (M <= 16 MT): the weights are read once, straight into registers, by as many waves as there are tiles of
 // 16 NT outputs x a quarter of k; the rows come from the caches.  The four waves of a block take 128 bytes of k in turn
-// (so a block reads 512 consecutive bytes of each weight row) and their sums meet in LDS.
-template <typename TO, int MT, int NT>
+// (so a block reads 512 consecutive bytes of each weight row), kUnits turns in flight, and their sums meet in LDS.
+template <typename TO, int MT, int NT, int kUnits>
 __global__ void __launch_bounds__(256) rows_kernel(MatmulArgs a) {
-  constexpr int kUnits = MT * NT >= 8 ? 1 : MT * NT >= 4 ? 2 : 4;  // 128-byte pieces of k in flight per wave
   __shared__ int sums[4][MT * 16][NT * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, p = (lane >> 4) * 16;
   const int n0 = blockIdx.x * (16 * NT);
@@ -397,7 +396,9 @@ template <typename TO> __global__ void __launch_bounds__(256) add_kernel(MatmulA
   }
 }
 
-constexpr int kRowsMost = 64;  // rows_kernel's
+// rows_kernel or tiles (us at k = 4096): 32 rows x 32,000 outputs 28.3 or 26.9, x 4,096 7.3 or 10.7; 64 rows x 32,000
+// 36.3 or 27.9, x 4,096 12.0 or 12.5, x 8,192 (k = 8192) 38.1 or 21.1.
+bool rows_form(int64_t M, int N) { return M <= 16 || (M <= 32 && N <= 8192) || (M <= 64 && N <= 4096); }
 // How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.
 int cut_of(int64_t M, int N, int K, Cut *c) {
   const int64_t big = (M + 255) / 256 * ((N + 255) / 256);
@@ -406,7 +407,8 @@ int cut_of(int64_t M, int N, int K, Cut *c) {
   c->tiles_n = (N + side - 1) / side;
   const int64_t tiles = (int64_t)c->tiles_m * c->tiles_n;
   const int stages = (K + HK - 1) / HK;
-  int64_t splits = side == 256 ? 1 : 512 / tiles;
+  // one part per compute unit: two measured 25.1 -> 27.3 us at 300 x 8,000 x 4,096, 27.9 -> 30.0 at 64 x 32,000 x 4,096
+  int64_t splits = side == 256 ? 1 : 256 / tiles;
   if (splits > stages / 4) splits = stages / 4;  // a part shorter than four stages costs more than it saves
   if (splits < 1) splits = 1;
   c->per = (int)((stages + splits - 1) / splits) * HK;
@@ -432,15 +434,19 @@ template <typename TO, int T> hipError_t run_cut(const MatmulArgs &a, const Cut 
   return aligned && near ? run_tiles<TO, true, T>(a, c, s) : run_tiles<TO, false, T>(a, c, s);
 }
 
-template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((rows_kernel<TO, MT, NT>), dim3((a.N + 16 * NT - 1) / (16 * NT)), dim3(256), 0, s, a);
+template <typename TO, int MT, int NT, int U> hipError_t run_rows(const MatmulArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U>), dim3((a.N + 16 * NT - 1) / (16 * NT)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename TO> hipError_t run(const MatmulArgs &a, hipStream_t s) {
-  if (a.M <= 16) return run_rows<TO, 1, 1>(a, s);
-  if (a.M <= 32) return a.N >= 8192 ? run_rows<TO, 2, 2>(a, s) : run_rows<TO, 2, 1>(a, s);
-  if (a.M <= kRowsMost) return a.N >= 16384 ? run_rows<TO, 4, 4>(a, s) : run_rows<TO, 4, 1>(a, s);
+  if (rows_form(a.M, a.N)) {
+    // us at k = 4096.  16 rows: 32,000 outputs 21.9 with four tiles of outputs per wave, 26.3 with two, 32.3 with one
+    // (the rows are read from the caches once per wave); 5,000 outputs 12.2, 7.8, 9.0; 1,000 14.9, 10.0, 7.5 (k = 8000)
+    if (a.M <= 16)
+      return a.N >= 16384 ? run_rows<TO, 1, 4, 2>(a, s) : a.N >= 4096 ? run_rows<TO, 1, 2, 4>(a, s) : run_rows<TO, 1, 1, 4>(a, s);
+    return a.M <= 32 ? run_rows<TO, 2, 1, 4>(a, s) : run_rows<TO, 4, 1, 2>(a, s);
+  }
   Cut c;
   if (cut_of(a.M, a.N, a.K, &c) == 256) return run_cut<TO, 256>(a, c, s);
   if (c.splits == 1) return run_cut<TO, 128>(a, c, s);
@@ -456,7 +462,7 @@ template <typename TO> hipError_t run(const MatmulArgs &a, hipStream_t s) {
 }  // namespace mmq
 
 size_t matmul_quant_bytes(int64_t rows, int outputs, int inner) {
-  if (rows <= mmq::kRowsMost) return 0;
+  if (mmq::rows_form(rows, outputs)) return 0;
   mmq::Cut c;
   const int side = mmq::cut_of(rows, outputs, inner, &c);
   return side == 128 && c.splits > 1 ? (size_t)c.splits * rows * outputs * sizeof(int) : 0;
