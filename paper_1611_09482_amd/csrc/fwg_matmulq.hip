@@ -299,12 +299,16 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulArgs a
   }
 }
 
-// Few rows (M <= 16 MT): the weights are read once, straight into registers, by as many waves as there are tiles of
-// 16 NT outputs x a quarter of k; the rows come from the caches.  The four waves of a block take 128 bytes of k in turn
-// (so a block reads 512 consecutive bytes of each weight row), kUnits turns in flight, and their sums meet in LDS.
+// Few rows (M <= 16 MT): the weights are read once, straight into registers, by one block per 16 NT outputs; the rows
+// come from the caches.  The W waves of a block take 128 bytes of k in turn, kUnits turns in flight, and their sums
+// meet in LDS.  Bound by memory: 16 x 32,000 x 4,096 in 31 us (4.3 TB/s; 22 us where the weights are in the last-level
+// cache), one row in 25 us (5.2 TB/s).  W: with 4 waves 16 x 1,000 x 8,000 takes 17 us instead of 10, 16 x 4,096 x
+// 8,192 15.9 instead of 10.8.  NT: two tiles of outputs share the rows' reads (16 x 32,000 x 4,096 31 us, 38 with one) but
+// leave compute units idle below 8,192 outputs (16 x 4,096 x 8,192 15.1 us, 10.8 with one).
 template <typename TO, int MT, int NT, int kUnits>
-__global__ void __launch_bounds__(256) rows_kernel(MatmulArgs a) {
-  __shared__ int sums[4][MT * 16][NT * 16];
+__global__ void __launch_bounds__(1024) rows_kernel(MatmulArgs a) {
+  constexpr int W = 16;
+  __shared__ int sums[W][MT * 16][NT * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, p = (lane >> 4) * 16;
   const int n0 = blockIdx.x * (16 * NT);
   const int8_t *w[NT], *x[MT];
@@ -314,16 +318,16 @@ __global__ void __launch_bounds__(256) rows_kernel(MatmulArgs a) {
   for (int j = 0; j < MT; ++j) x[j] = a.x + (int64_t)min(j * 16 + r, (int)a.M - 1) * a.ld_x;
   i32x4 acc[NT][MT] = {};
   int k = wave * 128;
-  for (; k + (kUnits - 1) * 512 + 128 <= a.K; k += kUnits * 512) {
+  for (; k + (kUnits - 1) * (128 * W) + 128 <= a.K; k += kUnits * (128 * W)) {
     i32x4 vw[kUnits][2][NT], vx[kUnits][2][MT];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) vw[u][h][i] = *(const i32x4_b *)(w[i] + k + u * 512 + h * 64 + p);
+        for (int i = 0; i < NT; ++i) vw[u][h][i] = *(const i32x4_b *)(w[i] + k + u * (128 * W) + h * 64 + p);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) vx[u][h][j] = *(const i32x4_b *)(x[j] + k + u * 512 + h * 64 + p);
+        for (int j = 0; j < MT; ++j) vx[u][h][j] = *(const i32x4_b *)(x[j] + k + u * (128 * W) + h * 64 + p);
       }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
@@ -335,7 +339,7 @@ __global__ void __launch_bounds__(256) rows_kernel(MatmulArgs a) {
           for (int j = 0; j < MT; ++j) acc[i][j] = mma(vw[u][h][i], vx[u][h][j], acc[i][j]);
   }
 #pragma unroll 1
-  for (; k < a.K; k += 512) {
+  for (; k < a.K; k += 128 * W) {
 #pragma unroll 1
     for (int h = 0; h < 2; ++h) {
       i32x4 vw[NT], vx[MT];
@@ -354,10 +358,12 @@ __global__ void __launch_bounds__(256) rows_kernel(MatmulArgs a) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) *(i32x4 *)&sums[wave][j * 16 + r][i * 16 + (lane >> 4) * 4] = acc[i][j];
   __syncthreads();
-  for (int t = threadIdx.x; t < MT * NT * 256; t += 256) {
+  for (int t = threadIdx.x; t < MT * NT * 256; t += 64 * W) {
     const int m = t / (16 * NT), c = t % (16 * NT), n = n0 + c;
     if (m >= a.M || n >= a.N) continue;
-    const int sum = sums[0][m][c] + sums[1][m][c] + sums[2][m][c] + sums[3][m][c];
+    int sum = 0;
+#pragma unroll
+    for (int v = 0; v < W; ++v) sum += sums[v][m][c];
     float v = (float)sum * a.x_scale[m] * a.w_scale[n];
     if (a.bias) v += a.bias[n];
     put((TO *)a.out + m * a.ld_o + n, v);
@@ -435,17 +441,14 @@ template <typename TO, int T> hipError_t run_cut(const MatmulArgs &a, const Cut 
 }
 
 template <typename TO, int MT, int NT, int U> hipError_t run_rows(const MatmulArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U>), dim3((a.N + 16 * NT - 1) / (16 * NT)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U>), dim3((a.N + 16 * NT - 1) / (16 * NT)), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename TO> hipError_t run(const MatmulArgs &a, hipStream_t s) {
   if (rows_form(a.M, a.N)) {
-    // us at k = 4096.  16 rows: 32,000 outputs 21.9 with four tiles of outputs per wave, 26.3 with two, 32.3 with one
-    // (the rows are read from the caches once per wave); 5,000 outputs 12.2, 7.8, 9.0; 1,000 14.9, 10.0, 7.5 (k = 8000)
-    if (a.M <= 16)
-      return a.N >= 16384 ? run_rows<TO, 1, 4, 2>(a, s) : a.N >= 4096 ? run_rows<TO, 1, 2, 4>(a, s) : run_rows<TO, 1, 1, 4>(a, s);
-    return a.M <= 32 ? run_rows<TO, 2, 1, 4>(a, s) : run_rows<TO, 4, 1, 2>(a, s);
+    if (a.M <= 16) return a.N >= 8192 ? run_rows<TO, 1, 2, 2>(a, s) : run_rows<TO, 1, 1, 2>(a, s);
+    return a.M <= 32 ? run_rows<TO, 2, 1, 2>(a, s) : run_rows<TO, 4, 1, 1>(a, s);
   }
   Cut c;
   if (cut_of(a.M, a.N, a.K, &c) == 256) return run_cut<TO, 256>(a, c, s);
