@@ -6,9 +6,9 @@
 // Gradient: dtable[v] = scale * sum over the positions i with tok[i] = v of dy[i], in float32, in a fixed order.
 // The positions are sorted by token (a stable radix sort of at most 9 bits a pass), then equal parts of the
 // sorted order are summed, each by one wave per slice of columns: a row whose positions lie inside a part is
-// finished there, rows that cross parts leave partial sums that a last kernel adds up in the parts' order.  So
-// the work is even however often a token comes, no sum depends on the order in which blocks run, and nothing is
-// added atomically.
+// finished there, also past the part's end; rows of more positions than a part has leave partial sums that a last
+// kernel adds up in the parts' order.  So the work is even however often a token comes, no sum depends on the order in
+// which blocks run, and no float is added atomically.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -83,45 +83,76 @@ __device__ __forceinline__ Pair entry(const Pair *in, const int32_t *tokens, int
 }
 __device__ __forceinline__ int digit_of(Pair p, int shift, int mask) { return (int)(p >> (32 + shift)) & mask; }
 
-// Counts of a tile's digits: hist[tile][bin].
-__global__ void __launch_bounds__(1024) hist_kernel(const Pair *in, const int32_t *tokens, int vocab, int n, int tile,
-                                                    int shift, int bins, int *hist) {
+struct SortArgs {
+  const Pair *in;         // NULL: the tokens in their own order
+  Pair *out;
+  const int32_t *tokens;
+  int *hist;              // [tile][bin]: this pass's digits
+  int *clear;             // cleared by the first kernel of a call
+  int vocab, n, tile, shift, bits;
+};
+
+// Counts of the tiles' digits.  (Counting the next pass's digits in scatter_kernel instead, by global atomics, takes
+// 20 us longer on 65,521 frequent words: they meet at few addresses.)
+__global__ void __launch_bounds__(1024) hist_kernel(SortArgs a) {
   __shared__ int cnt[kMaxBins];
+  const int bins = 1 << a.bits;
   for (int b = threadIdx.x; b < bins; b += 1024) cnt[b] = 0;
+  if (a.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
   __syncthreads();
-  const int i0 = blockIdx.x * tile, i1 = min(n, i0 + tile);
+  const int i0 = blockIdx.x * a.tile, i1 = min(a.n, i0 + a.tile);
   for (int i = i0 + threadIdx.x; i < i1; i += 1024)
-    atomicAdd(&cnt[digit_of(entry(in, tokens, vocab, i), shift, bins - 1)], 1);
+    atomicAdd(&cnt[digit_of(entry(a.in, a.tokens, a.vocab, i), a.shift, bins - 1)], 1);
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += 1024) hist[blockIdx.x * bins + b] = cnt[b];
+  for (int b = threadIdx.x; b < bins; b += 1024) a.hist[blockIdx.x * bins + b] = cnt[b];
 }
 
 // Scatters a tile in its order: the place of an entry is the number of smaller digits anywhere, plus its digit's
 // in earlier tiles, earlier waves and earlier lanes.  Each wave owns a contiguous share of the tile.
-__global__ void __launch_bounds__(1024) scatter_kernel(const Pair *in, const int32_t *tokens, int vocab, int n, int tile,
-                                                       int shift, int bits, const int *hist, Pair *out) {
+__global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
   __shared__ int place[kSortWaves][kMaxBins];
   __shared__ int wsum[kSortWaves];
-  const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int b = threadIdx.x; b < kSortWaves * bins; b += 1024) place[b / bins][b % bins] = 0;
-  __syncthreads();
-  const int share = (tile + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
-  const int i0 = min(n, (int)blockIdx.x * tile + wave * share);
-  const int i1 = min(min(n, ((int)blockIdx.x + 1) * tile), i0 + share);
-  for (int i = i0 + lane; i < i1; i += 64)
-    atomicAdd(&place[wave][digit_of(entry(in, tokens, vocab, i), shift, bins - 1)], 1);
-  __syncthreads();
-  // thread b: totals of bin b, exclusive over the bins, then the waves' starts
+  const int bins = 1 << a.bits, n = a.n, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (a.clear && gridDim.x == 1 && threadIdx.x == 0) *a.clear = 0;
+#pragma unroll
+  for (int b = 0; b < kSortWaves * kMaxBins / 1024; ++b) (&place[0][0])[b * 1024 + threadIdx.x] = 0;
+  // thread b: totals of bin b and those of earlier tiles
   const int b = threadIdx.x;
   int total = 0, before = 0;
-  if (b < bins) {
+  if (b < bins && gridDim.x > 1) {
+#pragma unroll 8
     for (int t = 0; t < (int)gridDim.x; ++t) {
-      const int c = gridDim.x > 1 ? hist[t * bins + b] : 0;
+      const int c = a.hist[t * bins + b];
       before += t < (int)blockIdx.x ? c : 0;
       total += c;
     }
-    if (gridDim.x == 1)
-      for (int w = 0; w < kSortWaves; ++w) total += place[w][b];
+  }
+  const int share = (a.tile + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
+  const int i0 = min(n, (int)blockIdx.x * a.tile + wave * share);
+  const int i1 = min(min(n, ((int)blockIdx.x + 1) * a.tile), i0 + share);
+  constexpr int kHeld = 2;  // entries of a lane that stay in registers (tiles of up to 2,048)
+  Pair held[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = i0 + j * 64 + lane;
+    held[j] = i < i1 ? entry(a.in, a.tokens, a.vocab, i) : 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (i0 + j * 64 + lane < i1) atomicAdd(&place[wave][digit_of(held[j], a.shift, bins - 1)], 1);
+  for (int i = i0 + kHeld * 64 + lane; i < i1; i += 64)
+    atomicAdd(&place[wave][digit_of(entry(a.in, a.tokens, a.vocab, i), a.shift, bins - 1)], 1);
+  __syncthreads();
+  // exclusive over the bins, then the waves' starts
+  int count[kSortWaves];
+  if (b < bins) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) count[w] = place[w][b];
+    if (gridDim.x == 1) {
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) total += count[w];
+    }
   }
   int incl = total;
 #pragma unroll
@@ -132,59 +163,90 @@ __global__ void __launch_bounds__(1024) scatter_kernel(const Pair *in, const int
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
   int start = incl - total + before;
-  for (int w = 0; w < wave; ++w) start += wsum[w];
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) start += w < wave ? wsum[w] : 0;
   if (b < bins) {
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int c = place[w][b];
       place[w][b] = start;
-      start += c;
+      start += count[w];
     }
   }
   __syncthreads();
-  for (int i = i0 + lane; i - lane < i1; i += 64) {
+  auto put_64 = [&](int i, Pair p) {
     const bool in_share = i < i1;
-    const Pair p = in_share ? entry(in, tokens, vocab, i) : 0;
-    const int d = in_share ? digit_of(p, shift, bins - 1) : 0;
+    const int d = in_share ? digit_of(p, a.shift, bins - 1) : 0;
     unsigned long long same = __ballot(in_share);  // the lanes with my digit
-    for (int k = 0; k < bits; ++k) {
+    for (int k = 0; k < a.bits; ++k) {
       const unsigned long long one = __ballot((d >> k) & 1);
       same &= (d >> k) & 1 ? one : ~one;
     }
     const int rank = __popcll(same & ((1ull << lane) - 1));
     if (in_share) {
       const int at = place[wave][d];
-      out[at + rank] = p;
-      if (rank == 0) place[wave][d] = at + __popcll(same);  // after the reads of every lane: the wave runs in step
+      a.out[at + rank] = p;
+      // after the reads of every lane: the wave runs in step
+      if (rank == 0) place[wave][d] = at + __popcll(same);
     }
     __builtin_amdgcn_wave_barrier();
-  }
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (i0 + j * 64 < i1) put_64(i0 + j * 64 + lane, held[j]);
+  for (int i = i0 + kHeld * 64 + lane; i - lane < i1; i += 64)
+    put_64(i, i < i1 ? entry(a.in, a.tokens, a.vocab, i) : 0);
 }
 
 struct SumArgs {
   EmbedGradArgs g;
   const Pair *sorted;
-  float *partial;  // [2 * parts][channels]: a part's first run (continued from before), its last (continued after)
-  int part;        // entries per part
+  float *partial;  // [2 * parts][channels]: of long rows, a part's first run (begun before it) and its last
+  int *n_long;     // long rows found
+  int2 *long_rows; // (row, part in which it begins)
+  int part;        // entries per part, at most 64: the lanes hold them
   int parts, slices;
 };
 
-// A part's sums.  Wave task = (part, slice of 64 * VEC columns).
+// A part's sums.  Wave task = (part, slice of 64 * VEC columns).  A row belongs to the part in which its positions
+// begin, which sums it whole, past the part's end too; only rows of more than a part's positions (long) are summed part
+// by part and joined.
 template <typename T, typename TO>
 __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
   constexpr int VEC = El<T>::kVec;
   const int lane = threadIdx.x & 63, D = a.g.channels, n = a.g.n, V = a.g.vocab;
   if ((int)blockIdx.x < sum_blocks) {
-    const int task = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int part = task / a.slices, c = ((task % a.slices) * 64 + lane) * VEC, have = D - c;
+    const int task = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int P = a.part, part = task / a.slices, c = ((task % a.slices) * 64 + lane) * VEC, have = D - c;
     if (part >= a.parts) return;
-    const int i0 = part * a.part, i1 = min(n, i0 + a.part);
+    const int i0 = part * P, i1 = min(n, i0 + P);
+    // keys around: the part's own, P before and P after it (-1: none); positions of the latter two
+    const int i = i0 + lane;
+    const Pair none = (Pair)0xffffffffu << 32;
+    const Pair before = lane < P && i >= P ? a.sorted[i - P] : none;
+    const Pair own = lane < P && i < n ? a.sorted[i] : none;
+    const Pair after = lane < P && i + P < n ? a.sorted[i + P] : none;
+    auto key_of = [](Pair p) { return (int)(p >> 32); };
+    auto lane_key = [&](Pair p, int l) { return __builtin_amdgcn_readlane(key_of(p), l); };
+    const int first = lane_key(own, 0), last = lane_key(own, i1 - i0 - 1);
+    const int n_before = __popcll(__ballot(key_of(before) == first)), n_first = __popcll(__ballot(key_of(own) == first));
+    const int n_last = __popcll(__ballot(key_of(own) == last)), n_after = __popcll(__ballot(key_of(after) == last));
+    const bool whole = first == last;
+    const bool opened = n_before > 0;                                    // the first run began before
+    const bool long_first = opened && n_before + n_first + (whole ? n_after : 0) > P;
+    const bool ends_long = !(whole && opened) && n_after > 0 && n_last + n_after > P;  // the last run begins here
+    const int from = opened && !long_first ? i0 + n_first : i0;
+    const int to = n_after > 0 && !ends_long && !(whole && opened) ? i1 + n_after : i1;
+    if (from >= to) return;
     float acc[VEC] = {};
-    int cur = __builtin_amdgcn_readfirstlane((int)(a.sorted[i0] >> 32));
-    bool opened = i0 > 0 && (int)(a.sorted[i0 - 1] >> 32) == cur;  // the run goes on from the part before
-    auto flush = [&](bool goes_on) {
-      if (cur >= V || have <= 0) return;
-      if (opened || goes_on) {
-        store_part(a.partial + ((int64_t)part * 2 + (opened ? 0 : 1)) * D + c, have, acc);
+    int cur = lane_key(own, from - i0);
+    const bool starts_long = long_first;
+    auto flush = [&](bool is_first, bool is_last) {
+      if (cur >= V) return;
+      if (is_first && starts_long) {
+        store_part(a.partial + (int64_t)part * 2 * D + c, have, acc);
+      } else if (is_last && ends_long) {
+        store_part(a.partial + ((int64_t)part * 2 + 1) * D + c, have, acc);
+        if (task % a.slices == 0 && lane == 0) a.long_rows[atomicAdd(a.n_long, 1)] = make_int2(cur, part);
       } else {
         float v[VEC];
 #pragma unroll
@@ -192,32 +254,35 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
         store_part((TO *)a.g.out + (int64_t)cur * a.g.ld_out + c, have, v);
       }
     };
+    bool is_first = true;
     constexpr int B = 8;  // rows in flight
-    for (int i = i0; i < i1; i += B) {
+    for (int e = from; e < to; e += B) {
       float v[B][VEC];
       int key[B];
 #pragma unroll
       for (int j = 0; j < B; ++j) {
-        const Pair p = a.sorted[min(i + j, i1 - 1)];  // the same for the whole wave
-        key[j] = __builtin_amdgcn_readfirstlane((int)(p >> 32));
-        const int64_t pos = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)p);
+        const int at = min(e + j, to - 1);
+        const Pair p = at < i1 ? own : after;
+        const int l = at < i1 ? at - i0 : at - i1;
+        key[j] = lane_key(p, l);
+        const int64_t pos = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)p, l);
         load_part((const T *)a.g.grad + pos * a.g.ld_grad + c, key[j] < V ? have : 0, 0.f, v[j]);
       }
 #pragma unroll
       for (int j = 0; j < B; ++j) {
-        if (i + j >= i1) break;
+        if (e + j >= to) break;
         if (key[j] != cur) {
-          flush(false);
+          flush(is_first, false);
+          is_first = false;
           cur = key[j];
-          opened = false;
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+          for (int x = 0; x < VEC; ++x) acc[x] = 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] += v[j][e];
+        for (int x = 0; x < VEC; ++x) acc[x] += v[j][x];
       }
     }
-    flush(i1 < n && (int)(a.sorted[i1] >> 32) == cur);
+    flush(is_first, true);
     return;
   }
   // rows that no token names: each wave looks 16 rows up in the sorted keys and clears the absent ones
@@ -240,47 +305,56 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
   }
 }
 
-// Rows that cross parts: the part in which such a row begins adds up the partial sums of the parts that it covers.
-template <typename TO> __global__ void __launch_bounds__(256) join_kernel(SumArgs a) {
-  __shared__ float red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.g.n, D = a.g.channels;
-  const int part = blockIdx.x, c = (int)blockIdx.y * 64 + lane;
-  const int i1 = (part + 1) * a.part;
-  if (i1 >= n) return;
-  const int key = (int)(a.sorted[i1 - 1] >> 32);
-  if (key >= a.g.vocab || (int)(a.sorted[i1] >> 32) != key) return;
-  if (part > 0 && (int)(a.sorted[part * a.part] >> 32) == key && (int)(a.sorted[part * a.part - 1] >> 32) == key) return;
-  // the last part with entries of this row: the row's end lies in [i1, n]
-  int lo = i1, hi = n;
-  while (lo < hi) {
-    const int m = (lo + hi) >> 1;
-    if ((int)(a.sorted[m] >> 32) <= key) lo = m + 1;
-    else hi = m;
-  }
-  const int last = (lo - 1) / a.part, m = last - part;  // first-run sums of parts part + 1 .. last
-  const bool mine = c < D;
-  const int share = (m + 3) / 4, p0 = part + 1 + wave * share, p1 = min(last + 1, p0 + share);
-  float s = 0.f;
-  if (mine) {
-    if (wave == 0) s = a.partial[((int64_t)part * 2 + 1) * D + c];
-    for (int p = p0; p < p1; p += 8) {
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = p + j < p1 ? a.partial[(int64_t)(p + j) * 2 * D + c] : 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[j];
+// Long rows: the sums of the parts that a row covers are added up in order, a sixteenth of them by each wave.  Blocks
+// take (row, slice of 256 columns) in turn.
+constexpr int kJoinBlocks = 512;
+template <typename TO> __global__ void __launch_bounds__(1024) join_kernel(SumArgs a) {
+  __shared__ f32x4 red[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.g.channels, slices = (D + 255) / 256;
+  const int items = *a.n_long * slices;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    const int2 row = a.long_rows[item / slices];
+    const int c = ((item % slices) * 64 + lane) * 4, have = D - c;
+    int m = 0;  // parts after the first that begin with this row
+    while (true) {
+      const int p = row.y + 1 + m + lane;
+      const bool on = p < a.parts && (int)(a.sorted[(int64_t)p * a.part] >> 32) == row.x;
+      const int more = __popcll(__ballot(on));
+      m += more;
+      if (more < 64) break;
     }
+    const int share = (m + 15) / 16, p0 = row.y + 1 + min(m, wave * share), p1 = row.y + 1 + min(m, (wave + 1) * share);
+    float s[4] = {};
+    if (wave == 0) load_part(a.partial + ((int64_t)row.y * 2 + 1) * D + c, have, 0.f, s);
+    for (int p = p0; p < p1; p += 8) {
+      float v[8][4];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) load_part(a.partial + (int64_t)(p + j) * 2 * D + c, p + j < p1 ? have : 0, 0.f, v[j]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[x] += v[j][x];
+    }
+    red[wave][lane] = f32x4{s[0], s[1], s[2], s[3]};
+    __syncthreads();
+    if (wave == 0) {
+      float v[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float t = red[0][lane][x];
+#pragma unroll
+        for (int w = 1; w < 16; ++w) t += red[w][lane][x];
+        v[x] = t * a.g.scale;
+      }
+      store_part((TO *)a.g.out + (int64_t)row.x * a.g.ld_out + c, have, v);
+    }
+    __syncthreads();
   }
-  red[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && mine)
-    put((TO *)a.g.out + (int64_t)key * a.g.ld_out + c,
-        (((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]) * a.g.scale);
 }
 
 struct GradPlan {
-  int tile, tiles, passes, bits, part, parts, slices;
-  size_t off_pair[2], off_hist, off_partial, total;
+  int tile, tiles, passes, bits, part, parts;
+  size_t off_pair[2], off_hist, off_long, off_rows, off_partial, total;
 };
 
 GradPlan plan_of(int64_t n, int vocab, int channels) {
@@ -292,10 +366,11 @@ GradPlan plan_of(int64_t n, int vocab, int channels) {
   while (bits < 31 && (vocab >> bits) != 0) ++bits;  // keys 0 .. vocab
   p.passes = (bits + kMaxBits - 1) / kMaxBits;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.slices = (channels + 255) / 256;  // 64 lanes of 4 float32 (bf16: of 8; see slices_of)
-  // entries per part: enough parts to fill the device with waves, not so few entries that partial sums dominate
+  // entries per part: enough parts to fill the device with waves of 256 columns, not so few entries that their search
+  // and partial sums dominate
+  const int slices = (channels + 255) / 256;
   int part = 16;
-  while (part < 128 && (n / (2 * part)) * p.slices >= 4096) part *= 2;
+  while (part < 64 && (n / (2 * part)) * slices >= 4096) part *= 2;
   p.part = part;
   p.parts = (int)((n + part - 1) / part);
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
@@ -306,6 +381,10 @@ GradPlan plan_of(int64_t n, int vocab, int channels) {
   }
   p.off_hist = o;
   o += up((size_t)p.tiles << (p.bits + 2));
+  p.off_long = o;
+  o += 256;
+  p.off_rows = o;
+  o += up((size_t)p.parts * sizeof(int2));
   p.off_partial = o;
   o += up((size_t)p.parts * 2 * channels * sizeof(float));
   p.total = o;
@@ -317,27 +396,27 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   SumArgs a;
   a.g = g;
   a.partial = (float *)(g.ws + p.off_partial);
+  a.n_long = (int *)(g.ws + p.off_long);
+  a.long_rows = (int2 *)(g.ws + p.off_rows);
   a.part = p.part;
   a.parts = p.parts;
   a.slices = (g.channels + 64 * El<T>::kVec - 1) / (64 * El<T>::kVec);
-  int *hist = (int *)(g.ws + p.off_hist);
-  const Pair *in = nullptr;
+  a.sorted = nullptr;
   for (int k = 0; g.n > 0 && k < p.passes; ++k) {
     Pair *out = (Pair *)(g.ws + p.off_pair[k & 1]);
-    if (p.tiles > 1)
-      hipLaunchKernelGGL(hist_kernel, dim3(p.tiles), dim3(1024), 0, s, in, g.tokens, g.vocab, g.n, p.tile, k * p.bits,
-                         1 << p.bits, hist);
-    hipLaunchKernelGGL(scatter_kernel, dim3(p.tiles), dim3(1024), 0, s, in, g.tokens, g.vocab, g.n, p.tile, k * p.bits,
-                       p.bits, hist, out);
-    in = out;
+    const SortArgs q{a.sorted, out,     g.tokens, (int *)(g.ws + p.off_hist), k == 0 ? a.n_long : nullptr,
+                     g.vocab,  g.n,     p.tile,   k * p.bits,                 p.bits};
+    if (p.tiles > 1) hipLaunchKernelGGL(hist_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
+    hipLaunchKernelGGL(scatter_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
+    a.sorted = out;
   }
-  a.sorted = in;
   const int64_t tasks = (int64_t)p.parts * a.slices;
   const int sum_blocks = (int)((tasks + 3) / 4), zero_blocks = (int)(((int64_t)g.vocab + 63) / 64);
   hipLaunchKernelGGL((sum_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, a, sum_blocks);
-  if (p.parts > 1)
-    hipLaunchKernelGGL((join_kernel<TO>), dim3((unsigned)p.parts, (unsigned)((g.channels + 63) / 64)), dim3(256), 0, s,
-                       a);
+  if (p.parts > 1) {
+    const int64_t most = (int64_t)p.parts * ((g.channels + 255) / 256);
+    hipLaunchKernelGGL((join_kernel<TO>), dim3((unsigned)(most < kJoinBlocks ? most : kJoinBlocks)), dim3(1024), 0, s, a);
+  }
   return hipGetLastError();
 }
 

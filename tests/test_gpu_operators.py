@@ -134,6 +134,8 @@ def token_pattern(kind, n, V, seed):
     (65, 257, 257, "frequent"), (2047, 600, 33, "descending"), (2049, 256, 512, "frequent"), (4096, 256, 40, "same"),
     (10656, 256, 512, "uniform"), (9999, 50001, 130, "frequent"), (70000, 511, 72, "same"), (70001, 512, 24, "padded"),
     (70000, 300000, 16, "frequent"), (140001, 1000, 520, "frequent"), (3000, 256, 2056, "padded"),
+    (5000, 1 << 20, 9, "uniform"), (5000, (1 << 27) + 5, 1, "uniform"), (300000, 70, 1100, "frequent"),
+    (40000, 2500, 2048, "uniform"), (1000, 60, 64, "uniform"), (30000, 3, 4, "same"),
 ])
 def test_embed_grad(n, V, D, kind, dtype):
     tok = token_pattern(kind, n, V, n + V)
