@@ -12,6 +12,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fwg.h"
 #include "fwg_ops.h"
 #include "fwg_ops_dev.h"
@@ -207,6 +209,19 @@ struct SumArgs {
   int parts, slices;
 };
 
+// 16 bytes as loaded, as floats.
+__device__ __forceinline__ void expand(const u32x4 &r, float (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(r[j]);
+}
+__device__ __forceinline__ void expand(const u32x4 &r, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = mfd::bf_lo(r[j]);
+    v[2 * j + 1] = mfd::bf_hi(r[j]);
+  }
+}
+
 // A part's sums.  Wave task = (part, slice of 64 * VEC columns).  A row belongs to the part in which its positions
 // begin, which sums it whole, past the part's end too; only rows of more than a part's positions (long) are summed part
 // by part and joined.
@@ -255,33 +270,43 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
       }
     };
     bool is_first = true;
-    constexpr int B = 8;  // rows in flight
-    for (int e = from; e < to; e += B) {
-      float v[B][VEC];
-      int key[B];
+    // rows in flight; where the whole wave's columns exist they stay as loaded until they are added
+    auto add_rows = [&](auto full) {
+      constexpr bool FULL = decltype(full)::value;
+      constexpr int B = FULL ? 16 : 8;
+      for (int e = from; e < to; e += B) {
+        u32x4 raw[FULL ? B : 1];
+        float v[B][VEC];
+        int key[B];
 #pragma unroll
-      for (int j = 0; j < B; ++j) {
-        const int at = min(e + j, to - 1);
-        const Pair p = at < i1 ? own : after;
-        const int l = at < i1 ? at - i0 : at - i1;
-        key[j] = lane_key(p, l);
-        const int64_t pos = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)p, l);
-        load_part((const T *)a.g.grad + pos * a.g.ld_grad + c, key[j] < V ? have : 0, 0.f, v[j]);
-      }
-#pragma unroll
-      for (int j = 0; j < B; ++j) {
-        if (e + j >= to) break;
-        if (key[j] != cur) {
-          flush(is_first, false);
-          is_first = false;
-          cur = key[j];
-#pragma unroll
-          for (int x = 0; x < VEC; ++x) acc[x] = 0.f;
+        for (int j = 0; j < B; ++j) {
+          const int at = min(e + j, to - 1);
+          const Pair p = at < i1 ? own : after;
+          const int l = at < i1 ? at - i0 : at - i1;
+          key[j] = lane_key(p, l);
+          const int64_t pos = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)p, l);
+          const T *row = (const T *)a.g.grad + pos * a.g.ld_grad + c;
+          if constexpr (FULL) raw[j] = *(const u32x4_el *)row;
+          else load_part(row, key[j] < V ? have : 0, 0.f, v[j]);
         }
 #pragma unroll
-        for (int x = 0; x < VEC; ++x) acc[x] += v[j][x];
+        for (int j = 0; j < B; ++j) {
+          if (e + j >= to) break;
+          if (key[j] != cur) {
+            flush(is_first, false);
+            is_first = false;
+            cur = key[j];
+#pragma unroll
+            for (int x = 0; x < VEC; ++x) acc[x] = 0.f;
+          }
+          if constexpr (FULL) expand(raw[j], v[j]);
+#pragma unroll
+          for (int x = 0; x < VEC; ++x) acc[x] += v[j][x];
+        }
       }
-    }
+    };
+    if (((task % a.slices) + 1) * 64 * VEC <= D) add_rows(std::true_type());
+    else add_rows(std::false_type());
     flush(is_first, true);
     return;
   }
@@ -305,11 +330,11 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
   }
 }
 
-// Long rows: the sums of the parts that a row covers are added up in order, a sixteenth of them by each wave.  Blocks
+// Long rows: the sums of the parts that a row covers are added up in order, an eighth of them by each wave.  Blocks
 // take (row, slice of 256 columns) in turn.
-constexpr int kJoinBlocks = 512;
-template <typename TO> __global__ void __launch_bounds__(1024) join_kernel(SumArgs a) {
-  __shared__ f32x4 red[16][64];
+constexpr int kJoinBlocks = 1024, kJoinWaves = 8;
+template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(SumArgs a) {
+  __shared__ f32x4 red[kJoinWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.g.channels, slices = (D + 255) / 256;
   const int items = *a.n_long * slices;
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
@@ -323,7 +348,7 @@ template <typename TO> __global__ void __launch_bounds__(1024) join_kernel(SumAr
       m += more;
       if (more < 64) break;
     }
-    const int share = (m + 15) / 16, p0 = row.y + 1 + min(m, wave * share), p1 = row.y + 1 + min(m, (wave + 1) * share);
+    const int share = (m + kJoinWaves - 1) / kJoinWaves, p0 = row.y + 1 + min(m, wave * share), p1 = row.y + 1 + min(m, (wave + 1) * share);
     float s[4] = {};
     if (wave == 0) load_part(a.partial + ((int64_t)row.y * 2 + 1) * D + c, have, 0.f, s);
     for (int p = p0; p < p1; p += 8) {
@@ -343,7 +368,7 @@ template <typename TO> __global__ void __launch_bounds__(1024) join_kernel(SumAr
       for (int x = 0; x < 4; ++x) {
         float t = red[0][lane][x];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) t += red[w][lane][x];
+        for (int w = 1; w < kJoinWaves; ++w) t += red[w][lane][x];
         v[x] = t * a.g.scale;
       }
       store_part((TO *)a.g.out + (int64_t)row.x * a.g.ld_out + c, have, v);
@@ -415,7 +440,8 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   hipLaunchKernelGGL((sum_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, a, sum_blocks);
   if (p.parts > 1) {
     const int64_t most = (int64_t)p.parts * ((g.channels + 255) / 256);
-    hipLaunchKernelGGL((join_kernel<TO>), dim3((unsigned)(most < kJoinBlocks ? most : kJoinBlocks)), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((join_kernel<TO>), dim3((unsigned)(most < kJoinBlocks ? most : kJoinBlocks)),
+                       dim3(64 * kJoinWaves), 0, s, a);
   }
   return hipGetLastError();
 }
