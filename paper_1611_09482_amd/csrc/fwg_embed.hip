@@ -23,7 +23,7 @@ namespace emb {
 
 using namespace opd;
 
-template <typename TI, typename TO, int R>
+template <typename TI, typename TO, int R, bool STREAM>
 __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, int log_tpr) {
   constexpr int VEC = El<TI>::kVec;
   const int tpr = 1 << log_tpr, per = 256 >> log_tpr;
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, int log_tpr) {
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     const int64_t r = r0 + (int64_t)j * per;
-    if (r < a.n) store_part((TO *)a.out + r * a.ld_out + c, have, v[j]);
+    if (r < a.n) store_part<STREAM>((TO *)a.out + r * a.ld_out + c, have, v[j]);
   }
 }
 
@@ -59,12 +59,12 @@ template <typename TI, typename TO> hipError_t run(const EmbedArgs &a, hipStream
   const unsigned gy = (unsigned)((pieces + (1 << log_tpr) - 1) >> log_tpr);
   const int64_t per = 256 >> log_tpr;
   // four rows per thread where that still leaves every compute unit several blocks
-  if ((a.n + 4 * per - 1) / (4 * per) * gy >= 2048)
-    hipLaunchKernelGGL((embed_kernel<TI, TO, 4>), dim3((unsigned)((a.n + 4 * per - 1) / (4 * per)), gy), dim3(256), 0,
-                       s, a, log_tpr);
-  else
-    hipLaunchKernelGGL((embed_kernel<TI, TO, 1>), dim3((unsigned)((a.n + per - 1) / per), gy), dim3(256), 0, s, a,
-                       log_tpr);
+  const bool many = (a.n + 4 * per - 1) / (4 * per) * gy >= 2048;
+  const dim3 grid((unsigned)((a.n + (many ? 4 : 1) * per - 1) / ((many ? 4 : 1) * per)), gy);
+  if (!many) hipLaunchKernelGGL((embed_kernel<TI, TO, 1, false>), grid, dim3(256), 0, s, a, log_tpr);
+  else if (a.n * a.channels * (int64_t)sizeof(TO) < kStreamBytes)
+    hipLaunchKernelGGL((embed_kernel<TI, TO, 4, false>), grid, dim3(256), 0, s, a, log_tpr);
+  else hipLaunchKernelGGL((embed_kernel<TI, TO, 4, true>), grid, dim3(256), 0, s, a, log_tpr);
   return hipGetLastError();
 }
 

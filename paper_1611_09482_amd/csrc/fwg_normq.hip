@@ -24,7 +24,7 @@ constexpr float kTinyIn = 7.52316384526264e-37f;  // 2^-120: 127 / max stays fin
 __device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
 
 // TPR threads per row (64: a wave per row), NP pieces per thread.
-template <typename T, int TPR, int NP>
+template <typename T, int TPR, int NP, bool STREAM>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_quant_kernel(NormArgs a) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kW = TPR / 64;
   __shared__ float red[2 * kW];
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_quant_kernel(NormA
       if (a.norm) ss += h[p][i] * h[p][i];
       top = max_nan(fabsf(hg[p][i]), top);
     }
-    if (a.summed) store_part((T *)a.summed + r * a.ld_s + c, a.channels - c, h[p]);
+    if (a.summed) store_part<STREAM>((T *)a.summed + r * a.ld_s + c, a.channels - c, h[p]);
   }
   // a NaN or an infinity anywhere goes on in the sum
   const float poison = top < kInf ? 0.f : __builtin_nanf("");
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_quant_kernel(NormA
 #pragma unroll
       for (int i = 0; i < kE; ++i) w[i / 4] |= ((uint32_t)(int)v[i] & 0xffu) << (8 * (i % 4));
       typedef unsigned int u32x2_b __attribute__((ext_vector_type(2), aligned(1)));
-      *(u32x2_b *)q = u32x2_b{w[0], w[1]};
+      put_vector<STREAM>((u32x2_b *)q, u32x2_b{w[0], w[1]});
     } else {
       for (int i = 0; i < kE; ++i)
         if (i < have) q[i] = (int8_t)(int)v[i];
@@ -106,15 +106,17 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_quant_kernel(NormA
     if (a.values) {
 #pragma unroll
       for (int i = 0; i < kE; ++i) v[i] *= scale;
-      store_part(a.values + r * a.ld_v + c, have, v);
+      store_part<STREAM>(a.values + r * a.ld_v + c, have, v);
     }
   }
 }
 
 template <typename T, int TPR, int NP> hipError_t go(const NormArgs &a, hipStream_t s) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
-  hipLaunchKernelGGL((norm_quant_kernel<T, TPR, NP>), dim3((unsigned)((a.rows + kRows - 1) / kRows)),
-                     dim3(TPR < 256 ? 256 : TPR), 0, s, a);
+  const dim3 grid((unsigned)((a.rows + kRows - 1) / kRows)), block(TPR < 256 ? 256 : TPR);
+  const int64_t bytes = a.rows * a.channels * (1 + (a.summed ? (int64_t)sizeof(T) : 0) + (a.values ? 2 : 0));
+  if (bytes < kStreamBytes) hipLaunchKernelGGL((norm_quant_kernel<T, TPR, NP, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_quant_kernel<T, TPR, NP, true>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

@@ -62,17 +62,24 @@ template <int N> __device__ __forceinline__ void load(const uint16_t *p, float (
     }
   }
 }
-template <int N> __device__ __forceinline__ void store(float *p, const float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) *(f32x4_el *)(p + 4 * i) = f32x4_el{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+// STREAM: past the caches (outputs too large to be found there by whoever reads them next).
+template <bool STREAM, typename V> __device__ __forceinline__ void put_vector(V *p, V v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
 }
-template <int N> __device__ __forceinline__ void store(uint16_t *p, const float (&v)[N]) {
+template <bool STREAM = false, int N> __device__ __forceinline__ void store(float *p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i)
+    put_vector<STREAM>((f32x4_el *)(p + 4 * i), f32x4_el{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]});
+}
+template <bool STREAM = false, int N> __device__ __forceinline__ void store(uint16_t *p, const float (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N / 8; ++i)
-    *(u32x4_el *)(p + 8 * i) = u32x4_el{pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
-                                        pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7])};
+    put_vector<STREAM>((u32x4_el *)(p + 8 * i),
+                       u32x4_el{pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
+                                pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7])});
   if constexpr (N % 8 == 4)
-    *(u32x2_el *)(p + N - 4) = u32x2_el{pack2(v[N - 4], v[N - 3]), pack2(v[N - 2], v[N - 1])};
+    put_vector<STREAM>((u32x2_el *)(p + N - 4), u32x2_el{pack2(v[N - 4], v[N - 3]), pack2(v[N - 2], v[N - 1])});
 }
 
 // The same where only the first `have` elements exist (have may be <= 0 or >= N); absent ones read as `fill`.
@@ -85,10 +92,10 @@ __device__ __forceinline__ void load_part(const T *p, int have, float fill, floa
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = i < have ? to_f(p[i]) : fill;
 }
-template <typename T, int N>
+template <bool STREAM = false, typename T, int N>
 __device__ __forceinline__ void store_part(T *p, int have, const float (&v)[N]) {
   if (have >= N) {
-    store(p, v);
+    store<STREAM>(p, v);
     return;
   }
 #pragma unroll
