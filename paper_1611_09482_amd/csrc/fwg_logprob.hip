@@ -195,7 +195,7 @@ __device__ __forceinline__ void take(double &list, int k, const float (&batch)[U
 #pragma unroll 1
   for (int u = 0; u < U; ++u) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) append(z[i], c + i, z[i] >= least, n, s);
+    for (int i = 0; i < VEC; ++i) append(z[i], min(c, end - VEC) + i, z[i] >= least, n, s);
 #pragma unroll
     for (int i = 0; i < N - VEC; ++i) z[i] = z[i + VEC];  // a loop over registers: move, not index
     c += 64 * VEC;
@@ -234,7 +234,8 @@ template <typename T> __device__ __forceinline__ void fill(double &list, int k, 
   list = s.place[lane];
 }
 
-// One wave's share of a row: batches of 64 * U vectors, `step` batches apart, from element `at` up to `end`.
+// One wave's share of a row: batches of 64 * U vectors, `step` elements apart, from element `at` up to `end` (at least a
+// vector from the row's start).
 template <typename T, bool TOP, int U>
 __device__ __forceinline__ void scan(const T *row, int at, int end, int step, int k, Acc &acc, double &list, Select *sel) {
   constexpr int VEC = El<T>::kVec, N = U * VEC;
@@ -244,11 +245,19 @@ __device__ __forceinline__ void scan(const T *row, int at, int end, int step, in
     float z[N];
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const int c = at + (j * 64 + lane) * VEC;
+      // a vector that would pass the end is taken from the last VEC elements instead
       float v[VEC];
-      load_part(row + c, end - c, -kInf, v);
+      load(row + min(at + (j * 64 + lane) * VEC, end - VEC), v);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) z[j * VEC + i] = v[i];
+    }
+    if (at + 64 * N > end) {  // and what it has from vectors before does not count again
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int over = at + (j * 64 + lane) * VEC - (end - VEC);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) z[j * VEC + i] = i < over ? -kInf : z[j * VEC + i];
+      }
     }
     float best[U], bm = -kInf;
 #pragma unroll

@@ -97,6 +97,19 @@ def _vector(name: str, t, n: int, dtype, device: int) -> int:
     return t.data_ptr()
 
 
+def _like(name: str, t, dtype, shape, device: int, out: bool = False):
+    """(address, stride) of a tensor of this type and shape seen as rows."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _refuse(name, t, device)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}: {dtype} is wanted")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is wanted")
+    if t.is_contiguous() and shape:
+        return t.data_ptr(), shape[-1]
+    return t.data_ptr(), _rows(name, t, out)[2]
+
+
 def _shaped(name: str, t, shape) -> None:
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}: {tuple(shape)} is wanted")
@@ -183,11 +196,9 @@ def quant_rows(x, out=None) -> QuantRows:
         out = QuantRows(torch.empty(x.shape, dtype=torch.int8, device=x.device),
                         torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device))
     q, scale = out
-    _typed("out.q", q, torch.int8, dev)
-    _shaped("out.q", q, x.shape)
-    _check(_library().fwg_quant_rows(kind, rows, width, x.data_ptr(), stride, q.data_ptr(),
-                                     _rows("out.q", q, True)[2], _vector("out.scale", scale, rows, torch.float32, dev),
-                                     _stream(dev)))
+    qp, qstride = _like("out.q", q, torch.int8, x.shape, dev, True)
+    _check(_library().fwg_quant_rows(kind, rows, width, x.data_ptr(), stride, qp, qstride,
+                                     _vector("out.scale", scale, rows, torch.float32, dev), _stream(dev)))
     return out if isinstance(out, QuantRows) else QuantRows(*out)
 
 
@@ -198,31 +209,19 @@ def norm_quant(x, gain=None, residual=None, eps: float = 1e-6, values: bool = Fa
     the four tensors (None: not wanted); out's `summed` may be x or residual itself."""
     dev = _device()
     kind, rows, width, stride = _matrix("x", x, dev)
-    rp, rstride = None, 0
-    if residual is not None:
-        _typed("residual", residual, x.dtype, dev)
-        _shaped("residual", residual, x.shape)
-        rp, rstride = residual.data_ptr(), _rows("residual", residual)[2]
+    shape, dtype = x.shape, x.dtype
+    rp, rstride = (None, 0) if residual is None else _like("residual", residual, dtype, shape, dev)
     if out is None:
-        out = NormQuant(torch.empty(x.shape, dtype=torch.int8, device=x.device),
-                        torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device),
-                        None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device),
-                        torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
+        out = NormQuant(torch.empty(shape, dtype=torch.int8, device=x.device),
+                        torch.empty(shape[:-1], dtype=torch.float32, device=x.device),
+                        None if residual is None else torch.empty(shape, dtype=dtype, device=x.device),
+                        torch.empty(shape, dtype=torch.bfloat16, device=x.device) if values else None)
     q, scale, summed, vals = out
-    _typed("out.q", q, torch.int8, dev)
-    _shaped("out.q", q, x.shape)
-    sp, sstride, vp, vstride = None, 0, None, 0
-    if summed is not None:
-        _typed("out.summed", summed, x.dtype, dev)
-        _shaped("out.summed", summed, x.shape)
-        sp, sstride = summed.data_ptr(), _rows("out.summed", summed, True)[2]
-    if vals is not None:
-        _typed("out.values", vals, torch.bfloat16, dev)
-        _shaped("out.values", vals, x.shape)
-        vp, vstride = vals.data_ptr(), _rows("out.values", vals, True)[2]
-    _check(_library().fwg_norm_quant(kind, rows, width, x.data_ptr(), stride, rp, rstride,
-                                     None if gain is None else _vector("gain", gain, width, torch.float32, dev), eps, sp,
-                                     sstride, q.data_ptr(), _rows("out.q", q, True)[2],
+    qp, qstride = _like("out.q", q, torch.int8, shape, dev, True)
+    sp, sstride = (None, 0) if summed is None else _like("out.summed", summed, dtype, shape, dev, True)
+    vp, vstride = (None, 0) if vals is None else _like("out.values", vals, torch.bfloat16, shape, dev, True)
+    gp = None if gain is None else _vector("gain", gain, width, torch.float32, dev)
+    _check(_library().fwg_norm_quant(kind, rows, width, x.data_ptr(), stride, rp, rstride, gp, eps, sp, sstride, qp, qstride,
                                      _vector("out.scale", scale, rows, torch.float32, dev), vp, vstride, _stream(dev)))
     return out if isinstance(out, NormQuant) else NormQuant(*out)
 
@@ -300,8 +299,7 @@ def log_probs_grad(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, o
     ids = _vector("tokens", tokens, rows, torch.int32, dev)
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _typed("out", out, logits.dtype, dev)
-    _shaped("out", out, logits.shape)
+    op, ostride = _like("out", out, logits.dtype, logits.shape, dev, True)
     if grad_entropy is not None and entropy is None:
         raise ValueError("grad_entropy is given without entropy")
     _check(_library().fwg_log_probs_grad(
@@ -309,5 +307,5 @@ def log_probs_grad(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, o
         None if entropy is None else _vector("entropy", entropy, rows, torch.float32, dev),
         _vector("grad_logp", grad_logp, rows, torch.float32, dev),
         None if grad_entropy is None else _vector("grad_entropy", grad_entropy, rows, torch.float32, dev),
-        out.data_ptr(), _rows("out", out, True)[2], _stream(dev)))
+        op, ostride, _stream(dev)))
     return out
