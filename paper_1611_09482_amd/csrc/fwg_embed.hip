@@ -73,7 +73,7 @@ template <typename TI, typename TO> hipError_t run(const EmbedArgs &a, hipStream
 // Sorted entries: key in the high word (vocab for tokens outside the table), position in the low one.
 typedef unsigned long long Pair;
 constexpr int kSortWaves = 16, kMaxBits = 9, kMaxBins = 1 << kMaxBits;
-constexpr int kMinTile = 2048, kMaxTiles = 64;
+constexpr int kMinTile = 2048, kMaxTiles = 128;
 
 __device__ __forceinline__ Pair pair_of(const int32_t *tokens, int vocab, int i) {
   const int t = tokens[i];
@@ -89,7 +89,7 @@ struct SortArgs {
   const Pair *in;         // NULL: the tokens in their own order
   Pair *out;
   const int32_t *tokens;
-  int *hist;              // [tile][bin]: this pass's digits
+  int *hist;              // [tile][bin]: this pass's digits (NULL: each block counts all tokens itself)
   int *clear;             // cleared by the first kernel of a call
   int vocab, n, tile, shift, bits;
 };
@@ -114,14 +114,16 @@ __global__ void __launch_bounds__(1024) hist_kernel(SortArgs a) {
 __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
   __shared__ int place[kSortWaves][kMaxBins];
   __shared__ int wsum[kSortWaves];
+  __shared__ int ahead[kMaxBins], behind[kMaxBins];  // digits of other tiles, before this one and after it
   const int bins = 1 << a.bits, n = a.n, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (a.clear && gridDim.x == 1 && threadIdx.x == 0) *a.clear = 0;
+  if (a.clear && !a.hist && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
 #pragma unroll
   for (int b = 0; b < kSortWaves * kMaxBins / 1024; ++b) (&place[0][0])[b * 1024 + threadIdx.x] = 0;
+  if (threadIdx.x < kMaxBins) ahead[threadIdx.x] = behind[threadIdx.x] = 0;
   // thread b: totals of bin b and those of earlier tiles
   const int b = threadIdx.x;
   int total = 0, before = 0;
-  if (b < bins && gridDim.x > 1) {
+  if (b < bins && a.hist) {
 #pragma unroll 8
     for (int t = 0; t < (int)gridDim.x; ++t) {
       const int c = a.hist[t * bins + b];
@@ -140,6 +142,12 @@ __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
     held[j] = i < i1 ? entry(a.in, a.tokens, a.vocab, i) : 0;
   }
   __syncthreads();
+  if (!a.hist) {
+    const int t0 = (int)blockIdx.x * a.tile, t1 = t0 + a.tile;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 1024)
+      if (i < t0 || i >= t1) atomicAdd(&(i < t0 ? ahead : behind)[digit_of(entry(a.in, a.tokens, a.vocab, i), a.shift, bins - 1)], 1);
+  }
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
     if (i0 + j * 64 + lane < i1) atomicAdd(&place[wave][digit_of(held[j], a.shift, bins - 1)], 1);
@@ -151,7 +159,9 @@ __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
   if (b < bins) {
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) count[w] = place[w][b];
-    if (gridDim.x == 1) {
+    if (!a.hist) {
+      before = ahead[b];
+      total = before + behind[b];
 #pragma unroll
       for (int w = 0; w < kSortWaves; ++w) total += count[w];
     }
@@ -202,7 +212,8 @@ __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
 struct SumArgs {
   EmbedGradArgs g;
   const Pair *sorted;
-  float *partial;  // [2 * parts][channels]: of long rows, a part's first run (begun before it) and its last
+  float *partial;  // [2 * parts][ld_p]: of long rows, a part's first run (begun before it) and its last
+  int ld_p;        // channels, rounded up to whole vectors
   int *n_long;     // long rows found
   int2 *long_rows; // (row, part in which it begins)
   int part;        // entries per part, at most 64: the lanes hold them
@@ -258,9 +269,9 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
     auto flush = [&](bool is_first, bool is_last) {
       if (cur >= V) return;
       if (is_first && starts_long) {
-        store_part(a.partial + (int64_t)part * 2 * D + c, have, acc);
+        store_part(a.partial + (int64_t)part * 2 * a.ld_p + c, have, acc);
       } else if (is_last && ends_long) {
-        store_part(a.partial + ((int64_t)part * 2 + 1) * D + c, have, acc);
+        store_part(a.partial + ((int64_t)part * 2 + 1) * a.ld_p + c, have, acc);
         if (task % a.slices == 0 && lane == 0) a.long_rows[atomicAdd(a.n_long, 1)] = make_int2(cur, part);
       } else {
         float v[VEC];
@@ -291,7 +302,6 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
         }
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-          if (e + j >= to) break;
           if (key[j] != cur) {
             flush(is_first, false);
             is_first = false;
@@ -299,9 +309,10 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
 #pragma unroll
             for (int x = 0; x < VEC; ++x) acc[x] = 0.f;
           }
+          // (no early end of the loop: the loads would move behind it, one after the other)
           if constexpr (FULL) expand(raw[j], v[j]);
 #pragma unroll
-          for (int x = 0; x < VEC; ++x) acc[x] += v[j][x];
+          for (int x = 0; x < VEC; ++x) acc[x] += e + j < to ? v[j][x] : 0.f;
         }
       }
     };
@@ -330,16 +341,19 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
   }
 }
 
-// Long rows: the sums of the parts that a row covers are added up in order, an eighth of them by each wave.  Blocks
-// take (row, slice of 256 columns) in turn.
+// Long rows: the sums of the parts that a row covers are added up in order.  Blocks take (row, slice of up to 256
+// columns) in turn; 4 columns per lane, and where a row has fewer columns than a wave's, groups of lanes (and always the
+// block's waves) take a share of the parts each.
 constexpr int kJoinBlocks = 1024, kJoinWaves = 8;
-template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(SumArgs a) {
+template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(SumArgs a, int log_lanes) {
   __shared__ f32x4 red[kJoinWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.g.channels, slices = (D + 255) / 256;
+  const int L = 1 << log_lanes, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.g.channels;
+  const int slices = (D + 4 * L - 1) / (4 * L), units = kJoinWaves * (64 >> log_lanes);
+  const int unit = wave * (64 >> log_lanes) + (lane >> log_lanes);
   const int items = *a.n_long * slices;
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
     const int2 row = a.long_rows[item / slices];
-    const int c = ((item % slices) * 64 + lane) * 4, have = D - c;
+    const int c = ((item % slices) * L + (lane & (L - 1))) * 4, have = D - c;
     int m = 0;  // parts after the first that begin with this row
     while (true) {
       const int p = row.y + 1 + m + lane;
@@ -348,29 +362,32 @@ template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_k
       m += more;
       if (more < 64) break;
     }
-    const int share = (m + kJoinWaves - 1) / kJoinWaves, p0 = row.y + 1 + min(m, wave * share), p1 = row.y + 1 + min(m, (wave + 1) * share);
-    float s[4] = {};
-    if (wave == 0) load_part(a.partial + ((int64_t)row.y * 2 + 1) * D + c, have, 0.f, s);
-    for (int p = p0; p < p1; p += 8) {
-      float v[8][4];
+    const int share = (m + units - 1) / units, p0 = row.y + 1 + min(m, unit * share), p1 = row.y + 1 + min(m, (unit + 1) * share);
+    // whole vectors: what lies between a row's channels and ld_p is read, and not stored
+    const f32x4 *from = (const f32x4 *)(a.partial + (have > 0 ? c : 0));
+    const int64_t ld = a.ld_p / 4;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (unit == 0) s = from[((int64_t)row.y * 2 + 1) * ld];
+    for (int p = p0; p < p1; p += 16) {
+      f32x4 v[16];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) load_part(a.partial + (int64_t)(p + j) * 2 * D + c, p + j < p1 ? have : 0, 0.f, v[j]);
+      for (int j = 0; j < 16; ++j) v[j] = from[(int64_t)min(p + j, p1 - 1) * 2 * ld];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 16; ++j)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) s[x] += v[j][x];
+        for (int x = 0; x < 4; ++x) s[x] += p + j < p1 ? v[j][x] : 0.f;
     }
-    red[wave][lane] = f32x4{s[0], s[1], s[2], s[3]};
+    red[wave][lane] = s;
     __syncthreads();
-    if (wave == 0) {
-      float v[4];
+    if (wave == 0 && lane < L) {
+      float v[4] = {};
+      for (int u = 0; u < units; ++u) {
+        const f32x4 t = red[u >> (6 - log_lanes)][((u & ((64 >> log_lanes) - 1)) << log_lanes) + lane];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        float t = red[0][lane][x];
-#pragma unroll
-        for (int w = 1; w < kJoinWaves; ++w) t += red[w][lane][x];
-        v[x] = t * a.g.scale;
+        for (int x = 0; x < 4; ++x) v[x] += t[x];
       }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[x] *= a.g.scale;
       store_part((TO *)a.g.out + (int64_t)row.x * a.g.ld_out + c, have, v);
     }
     __syncthreads();
@@ -411,7 +428,7 @@ GradPlan plan_of(int64_t n, int vocab, int channels) {
   p.off_rows = o;
   o += up((size_t)p.parts * sizeof(int2));
   p.off_partial = o;
-  o += up((size_t)p.parts * 2 * channels * sizeof(float));
+  o += up((size_t)p.parts * 2 * ((channels + 3) / 4 * 4) * sizeof(float));
   p.total = o;
   return p;
 }
@@ -421,17 +438,21 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   SumArgs a;
   a.g = g;
   a.partial = (float *)(g.ws + p.off_partial);
+  a.ld_p = (g.channels + 3) / 4 * 4;
   a.n_long = (int *)(g.ws + p.off_long);
   a.long_rows = (int2 *)(g.ws + p.off_rows);
   a.part = p.part;
   a.parts = p.parts;
   a.slices = (g.channels + 64 * El<T>::kVec - 1) / (64 * El<T>::kVec);
   a.sorted = nullptr;
+  int *hist = (int *)(g.ws + p.off_hist);
+  // up to 16,384 tokens every block counts all of them itself, which takes less than a launch
+  const bool counted = p.tiles > 1 && g.n > 16384;
   for (int k = 0; g.n > 0 && k < p.passes; ++k) {
     Pair *out = (Pair *)(g.ws + p.off_pair[k & 1]);
-    const SortArgs q{a.sorted, out,     g.tokens, (int *)(g.ws + p.off_hist), k == 0 ? a.n_long : nullptr,
-                     g.vocab,  g.n,     p.tile,   k * p.bits,                 p.bits};
-    if (p.tiles > 1) hipLaunchKernelGGL(hist_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
+    const SortArgs q{a.sorted, out, g.tokens, counted ? hist : nullptr, k == 0 ? a.n_long : nullptr,
+                     g.vocab, g.n, p.tile, k * p.bits, p.bits};
+    if (counted) hipLaunchKernelGGL(hist_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
     hipLaunchKernelGGL(scatter_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
     a.sorted = out;
   }
@@ -440,8 +461,10 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   hipLaunchKernelGGL((sum_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, a, sum_blocks);
   if (p.parts > 1) {
     const int64_t most = (int64_t)p.parts * ((g.channels + 255) / 256);
+    int log_lanes = 0;
+    while (log_lanes < 6 && (4 << log_lanes) < g.channels) ++log_lanes;
     hipLaunchKernelGGL((join_kernel<TO>), dim3((unsigned)(most < kJoinBlocks ? most : kJoinBlocks)),
-                       dim3(64 * kJoinWaves), 0, s, a);
+                       dim3(64 * kJoinWaves), 0, s, a, log_lanes);
   }
   return hipGetLastError();
 }
