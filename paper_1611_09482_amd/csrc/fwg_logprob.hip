@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kThreadsLp) short_kernel(LogProbArgs a) {
 #pragma unroll
       for (int i = 0; i < TOP; ++i) {
         const int j = g * TOP + i, c = ((j / VEC) * L + l) * VEC + j % VEC;
-        k[i] = c < a.vocab ? key_of(z[j], c) : below(-kInf);
+        k[i] = key_of(z[j], c);  // places past the vocabulary: -inf, after every token
       }
       sort_keys(k);
       if (g == 0) {

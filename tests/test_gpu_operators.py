@@ -680,3 +680,14 @@ def test_refusals():
     ]:
         with pytest.raises(error):
             call()
+
+
+# ---- the example: all of them together ----
+
+def test_example_trains_and_serves():
+    import examples.score_tokens as example
+    first, full, eight = example.main(streams=8, length=600, steps=60)
+    assert full < first - 0.5, (first, full)
+    # 8 bits: rows and weights are within half a 127th of their largest element, which moves a logit by a few
+    # hundredths and a mean log probability by less
+    assert abs(eight - full) < 0.03, (full, eight)
