@@ -394,6 +394,79 @@ template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_k
   }
 }
 
+// Few tokens: one launch without sorting.  A wave takes a position and a slice of 64 * VEC columns; the wave of a
+// token's first position adds up all of its positions, in order.  The remaining waves clear the rows that no token names,
+// 16 each.  Every block holds the tokens in LDS.  512 tokens of 256 classes x 512 float32: 6.7 us (the host's time for a
+// call), sorted 14.5; all of one class: 36 us, sorted 16, since one wave per slice then adds them all.
+constexpr int kFew = 512;
+template <typename T, typename TO>
+__global__ void __launch_bounds__(256) few_kernel(EmbedGradArgs a, int slices, int sum_blocks) {
+  constexpr int VEC = El<T>::kVec, B = 8;
+  __shared__ int tok[kFew];
+  __shared__ unsigned named[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n, V = a.vocab, D = a.channels;
+  for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 256) {
+    const int t = i < n ? a.tokens[i] : -1;
+    tok[i] = t < V ? t : -1;
+  }
+  if (threadIdx.x < 4) named[threadIdx.x] = 0u;
+  __syncthreads();
+  if ((int)blockIdx.x < sum_blocks) {
+    const int task = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
+    const int i = task / slices, c = ((task % slices) * 64 + lane) * VEC, have = D - c;
+    if (i >= n) return;
+    const int t = __builtin_amdgcn_readfirstlane(tok[i]);
+    if (t < 0) return;
+    for (int j = 0; j < i; j += 64)
+      if (__ballot(tok[j + lane] == t && j + lane < i)) return;
+    const bool full = ((task % slices) + 1) * 64 * VEC <= D;
+    float acc[VEC] = {};
+    for (int j = i / 64 * 64; j < n; j += 64)
+      for (unsigned long long m = __ballot(tok[j + lane] == t); m;) {
+        int pos[B];
+        int k = 0;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          pos[b] = j + (m ? __ffsll((long long)m) - 1 : 0);
+          k += m ? 1 : 0;
+          m &= m - 1;
+        }
+        float v[B][VEC];
+        if (full) {
+          u32x4 raw[B];
+#pragma unroll
+          for (int b = 0; b < B; ++b) raw[b] = *(const u32x4_el *)((const T *)a.grad + (int64_t)pos[b] * a.ld_grad + c);
+#pragma unroll
+          for (int b = 0; b < B; ++b) expand(raw[b], v[b]);
+        } else {
+#pragma unroll
+          for (int b = 0; b < B; ++b)
+            load_part((const T *)a.grad + (int64_t)pos[b] * a.ld_grad + c, b < k ? have : 0, 0.f, v[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int x = 0; x < VEC; ++x) acc[x] += b < k ? v[b][x] : 0.f;
+      }
+#pragma unroll
+    for (int x = 0; x < VEC; ++x) acc[x] *= a.scale;
+    store_part((TO *)a.out + (int64_t)t * a.ld_out + c, have, acc);
+    return;
+  }
+  const int r0 = (((int)blockIdx.x - sum_blocks) * 4 + wave) * 16;
+  for (int j = 0; j < n; j += 64) {
+    const int d = tok[j + lane] - r0;
+    if (d >= 0 && d < 16) atomicOr(&named[wave], 1u << d);
+  }
+  __syncthreads();
+  const float zero[VEC] = {};
+  for (int d = 0; d < 16 && r0 + d < V; ++d) {
+    if (named[wave] >> d & 1) continue;
+    TO *out = (TO *)a.out + (int64_t)(r0 + d) * a.ld_out;
+    for (int c = lane * VEC; c < D; c += 64 * VEC) store_part(out + c, D - c, zero);
+  }
+}
+
 struct GradPlan {
   int tile, tiles, passes, bits, part, parts;
   size_t off_pair[2], off_hist, off_long, off_rows, off_partial, total;
@@ -434,6 +507,13 @@ GradPlan plan_of(int64_t n, int vocab, int channels) {
 }
 
 template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, hipStream_t s) {
+  if (g.n <= kFew) {
+    const int slices = (g.channels + 64 * El<T>::kVec - 1) / (64 * El<T>::kVec);
+    const int sum_blocks = (int)(((int64_t)g.n * slices + 3) / 4), zero_blocks = (int)(((int64_t)g.vocab + 63) / 64);
+    hipLaunchKernelGGL((few_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, g, slices,
+                       sum_blocks);
+    return hipGetLastError();
+  }
   const GradPlan p = plan_of(g.n, g.vocab, g.channels);
   SumArgs a;
   a.g = g;
@@ -448,7 +528,7 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   int *hist = (int *)(g.ws + p.off_hist);
   // up to 16,384 tokens every block counts all of them itself, which takes less than a launch
   const bool counted = p.tiles > 1 && g.n > 16384;
-  for (int k = 0; g.n > 0 && k < p.passes; ++k) {
+  for (int k = 0; k < p.passes; ++k) {
     Pair *out = (Pair *)(g.ws + p.off_pair[k & 1]);
     const SortArgs q{a.sorted, out, g.tokens, counted ? hist : nullptr, k == 0 ? a.n_long : nullptr,
                      g.vocab, g.n, p.tile, k * p.bits, p.bits};
@@ -477,7 +557,9 @@ hipError_t launch_embed(const EmbedArgs &a, int dtype, int out_dtype, hipStream_
   return out_dtype == FWG_BF16 ? emb::run<float, uint16_t>(a, s) : emb::run<float, float>(a, s);
 }
 
-size_t embed_grad_bytes(int64_t n, int vocab, int channels) { return n <= 0 ? 0 : emb::plan_of(n, vocab, channels).total; }
+size_t embed_grad_bytes(int64_t n, int vocab, int channels) {
+  return n <= emb::kFew ? 0 : emb::plan_of(n, vocab, channels).total;
+}
 
 hipError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, int out_dtype, hipStream_t s) {
   if (dtype == FWG_BF16)

@@ -54,7 +54,12 @@ def _matrix(name: str, t, device: int, out: bool = False):
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise TypeError(f"{name} is {t.dtype}: float32 or bfloat16 is wanted")
-    return (kind,) + _rows(name, t, out)
+    shape = t.shape
+    if len(shape) == 2 and t.is_contiguous():
+        rows, width = shape
+        return kind, rows, width, width
+    rows, width, stride = _rows(name, t, out)
+    return kind, rows, width, stride
 
 
 def _rows(name: str, t, out: bool = False):

@@ -136,6 +136,8 @@ def token_pattern(kind, n, V, seed):
     (70000, 300000, 16, "frequent"), (140001, 1000, 520, "frequent"), (3000, 256, 2056, "padded"),
     (5000, 1 << 20, 9, "uniform"), (5000, (1 << 27) + 5, 1, "uniform"), (300000, 70, 1100, "frequent"),
     (40000, 2500, 2048, "uniform"), (1000, 60, 64, "uniform"), (30000, 3, 4, "same"),
+    (511, 300, 520, "frequent"), (512, 70000, 100, "padded"), (513, 40, 1024, "frequent"), (512, 9, 300, "same"),
+    (500, 17, 1031, "descending"),
 ])
 def test_embed_grad(n, V, D, kind, dtype):
     tok = token_pattern(kind, n, V, n + V)

@@ -20,7 +20,7 @@ def lib():
 GOOD = {
     "fwg_embed": dict(dtype=1, out_dtype=0, n=5, vocab=9, channels=4, table=FAKE, table_stride=4, tokens=FAKE, scale=1.0,
                       out=FAKE, out_stride=4, stream=None),
-    "fwg_embed_grad": dict(dtype=1, out_dtype=0, n=5, vocab=9, channels=4, grad=FAKE, grad_stride=4, tokens=FAKE,
+    "fwg_embed_grad": dict(dtype=1, out_dtype=0, n=5000, vocab=9, channels=4, grad=FAKE, grad_stride=4, tokens=FAKE,
                            scale=1.0, out=FAKE, out_stride=4, ws=FAKE, ws_bytes=1 << 20, stream=None),
     "fwg_quant_rows": dict(dtype=0, rows=5, channels=4, x=FAKE, x_stride=4, q=FAKE, q_stride=4, scale=FAKE, stream=None),
     "fwg_norm_quant": dict(dtype=0, rows=5, channels=4, x=FAKE, x_stride=4, residual=FAKE, residual_stride=4, gain=FAKE,
@@ -112,8 +112,8 @@ def size(fn, *args):
 
 def test_workspace_sizes(lib):
     assert size(lib.fwg_embed_grad_workspace, 0, 10, 10) == (B.FWG_OK, 0)
-    rc, small = size(lib.fwg_embed_grad_workspace, 100, 256, 64)
-    assert rc == B.FWG_OK and small >= 2 * 8 * 100
+    rc, small = size(lib.fwg_embed_grad_workspace, 1000, 256, 64)
+    assert rc == B.FWG_OK and small >= 2 * 8 * 1000
     rc, large = size(lib.fwg_embed_grad_workspace, 100000, 256, 64)
     assert rc == B.FWG_OK and large > small
     assert size(lib.fwg_embed_grad_workspace, -1, 10, 10)[0] == EINVAL
