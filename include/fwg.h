@@ -291,7 +291,8 @@ int fwg_device_status(fwg_handle *h);
  * Outputs must not overlap inputs except where a call says so.  Zero rows are a no-op.  Sums, softmax statistics
  * and norms are float32 (8-bit products: exact 32-bit integers), rounded once, to nearest even, where an output is
  * bf16, and are added up in an order that depends on the sizes only: the same call gives the same bits.
- * A token outside [0, vocab) is padding: it names no row and has log probability 0.
+ * A token outside [0, vocab) is padding: it names no row and has log probability 0.  vocab and outputs go up to 2^29,
+ * channels (where nothing else is said) to 2^20, rows to 2^40.
  * ------------------------------------------------------------------------- */
 
 /* out[i] = scale * table[tokens[i]], i in [0, n); a padding token's row is zero.  table: [vocab][channels] of

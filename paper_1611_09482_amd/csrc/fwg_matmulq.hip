@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "fwg.h"
@@ -422,10 +423,22 @@ int cut_of(int64_t M, int N, int K, Cut *c) {
   return side;
 }
 
+// Lets a kernel have its LDS, once per device (`done`: one bit each; a device past the 64th is told every time).
+hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 template <typename TO, bool ALIGNED, int T> hipError_t run_tiles(const MatmulArgs &a, const Cut &c, hipStream_t s) {
-  static const hipError_t set = hipFuncSetAttribute((const void *)tile_kernel<TO, ALIGNED, T>,
-                                                    hipFuncAttributeMaxDynamicSharedMemorySize, Tile<T>::kLds);
-  if (set != hipSuccess) return set;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, T>, Tile<T>::kLds, done);
+  if (e != hipSuccess) return e;
   // a block goes through several tiles where there are more than the device holds (one of 256, or two of 128 per
   // compute unit)
   const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = T == 256 ? 256 : 512;

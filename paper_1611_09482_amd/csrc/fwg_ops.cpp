@@ -13,7 +13,7 @@ using namespace fwg;
 
 namespace {
 
-constexpr int kMaxVocab = 1 << 30, kMaxChannels = 1 << 20;
+constexpr int kMaxVocab = 1 << 29, kMaxChannels = 1 << 20;
 constexpr int64_t kMaxRows = (int64_t)1 << 40, kMaxTokens = (int64_t)1 << 30;
 
 int size_of(int dtype) { return dtype == FWG_BF16 ? 2 : 4; }
