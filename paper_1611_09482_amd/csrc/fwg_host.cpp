@@ -19,6 +19,7 @@
 #include "fwg_wave.h"
 #include "fwg_chain.h"
 #include "fwg_wide.h"
+#include "fwg_ops.h"
 
 using namespace fwg;
 

@@ -9,9 +9,6 @@
 
 namespace fwg {
 
-// Sets the calling thread's fwg_last_error() message and returns `code` (fwg_host.cpp).
-int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-
 constexpr int kThreads = 256;     // every step kernel runs 4 waves of 64 lanes
 constexpr int kMaxLayers = 1024;  // per-layer slot counters live in LDS
 

@@ -6,7 +6,6 @@
 #include <cmath>
 
 #include "fwg.h"
-#include "fwg_internal.h"
 #include "fwg_ops.h"
 
 using namespace fwg;

@@ -9,6 +9,9 @@
 
 namespace fwg {
 
+// Sets the calling thread's fwg_last_error() message and returns `code` (fwg_host.cpp).
+int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+
 // Outputs from this size on are stored past the caches.  Half of the 256 MB last-level cache and less is better left
 // there for whoever reads it next: embed and a sum over its output take 73 us (84 past the caches) at 128 MB, but 126
 // (121) at 192 MB and 174 (160) at 256 MB.  norm_quant alone: 89 us (66) at 240 MB, 114 (86) at 320 MB.
