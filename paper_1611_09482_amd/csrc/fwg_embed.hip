@@ -242,7 +242,11 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
   const int lane = threadIdx.x & 63, D = a.g.channels, n = a.g.n, V = a.g.vocab;
   if ((int)blockIdx.x < sum_blocks) {
     const int task = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
-    const int P = a.part, part = task / a.slices, c = ((task % a.slices) * 64 + lane) * VEC, have = D - c;
+    // the lane's columns; a vector that would pass the last one is the last whole vector instead, and two lanes then sum
+    // and store the same columns, alike
+    const int P = a.part, part = task / a.slices, c0 = ((task % a.slices) * 64 + lane) * VEC;
+    const bool whole_vectors = D >= VEC;
+    const int c = whole_vectors ? min(c0, D - VEC) : c0, have = c0 < D ? (whole_vectors ? VEC : D - c0) : 0;
     if (part >= a.parts) return;
     const int i0 = part * P, i1 = min(n, i0 + P);
     // keys around: the part's own, P before and P after it (-1: none); positions of the latter two
@@ -281,7 +285,7 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
       }
     };
     bool is_first = true;
-    // rows in flight; where the whole wave's columns exist they stay as loaded until they are added
+    // rows in flight; they stay as loaded until they are added
     auto add_rows = [&](auto full) {
       constexpr bool FULL = decltype(full)::value;
       constexpr int B = FULL ? 16 : 8;
@@ -316,7 +320,7 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
         }
       }
     };
-    if (((task % a.slices) + 1) * 64 * VEC <= D) add_rows(std::true_type());
+    if (whole_vectors) add_rows(std::true_type());
     else add_rows(std::false_type());
     flush(is_first, true);
     return;
@@ -413,13 +417,14 @@ __global__ void __launch_bounds__(256) few_kernel(EmbedGradArgs a, int slices, i
   __syncthreads();
   if ((int)blockIdx.x < sum_blocks) {
     const int task = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
-    const int i = task / slices, c = ((task % slices) * 64 + lane) * VEC, have = D - c;
+    const int i = task / slices, c0 = ((task % slices) * 64 + lane) * VEC;
+    const bool full = D >= VEC;  // columns as in sum_kernel
+    const int c = full ? min(c0, D - VEC) : c0, have = c0 < D ? (full ? VEC : D - c0) : 0;
     if (i >= n) return;
     const int t = __builtin_amdgcn_readfirstlane(tok[i]);
     if (t < 0) return;
     for (int j = 0; j < i; j += 64)
       if (__ballot(tok[j + lane] == t && j + lane < i)) return;
-    const bool full = ((task % slices) + 1) * 64 * VEC <= D;
     float acc[VEC] = {};
     for (int j = i / 64 * 64; j < n; j += 64)
       for (unsigned long long m = __ballot(tok[j + lane] == t); m;) {

@@ -30,6 +30,20 @@ __device__ __forceinline__ i32x4 mma(const i32x4 &a, const i32x4 &b, const i32x4
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
+// 16 bytes at any address.  Where they are no aligned words the hardware takes 2.3 times as long (16 x 7,637 x 4,343: 22.7
+// us, x 4,352: 9.8), so with SHIFT the five words that hold the bytes are loaded and shifted: 14.2 us.  (For the tiles
+// below it costs more than it saves: 4,000 x 8,000 x 1,001 takes 71 us with it, 60 without.)
+template <bool SHIFT> __device__ __forceinline__ i32x4 load_any(const int8_t *p) {
+  if constexpr (!SHIFT) return *(const i32x4_b *)p;
+  typedef unsigned int u32x4_w __attribute__((ext_vector_type(4), aligned(4)));
+  const unsigned s = (unsigned)(uintptr_t)p & 3u;
+  const int8_t *q = p - s;
+  const u32x4_w a = *(const u32x4_w *)q;
+  const unsigned e = *(const unsigned *)(q + (s ? 16 : 12));  // not past the words that hold the bytes
+  return i32x4{(int)__builtin_amdgcn_alignbyte(a[1], a[0], s), (int)__builtin_amdgcn_alignbyte(a[2], a[1], s),
+               (int)__builtin_amdgcn_alignbyte(a[3], a[2], s), (int)__builtin_amdgcn_alignbyte(e, a[3], s)};
+}
+
 // 16 bytes of a row from byte k on; bytes from K on are 0.
 __device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K) {
   i32x4 v = {0, 0, 0, 0};
@@ -306,7 +320,7 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulArgs a
 // cache), one row in 25 us (5.2 TB/s).  W: with 4 waves 16 x 1,000 x 8,000 takes 17 us instead of 10, 16 x 4,096 x
 // 8,192 15.9 instead of 10.8.  NT: two tiles of outputs share the rows' reads (16 x 32,000 x 4,096 31 us, 38 with one) but
 // leave compute units idle below 8,192 outputs (16 x 4,096 x 8,192 15.1 us, 10.8 with one).
-template <typename TO, int MT, int NT, int kUnits>
+template <typename TO, int MT, int NT, int kUnits, bool SHIFT>
 __global__ void __launch_bounds__(1024) rows_kernel(MatmulArgs a) {
   constexpr int W = 16;
   __shared__ int sums[W][MT * 16][NT * 16];
@@ -326,9 +340,9 @@ __global__ void __launch_bounds__(1024) rows_kernel(MatmulArgs a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) vw[u][h][i] = *(const i32x4_b *)(w[i] + k + u * (128 * W) + h * 64 + p);
+        for (int i = 0; i < NT; ++i) vw[u][h][i] = load_any<SHIFT>(w[i] + k + u * (128 * W) + h * 64 + p);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) vx[u][h][j] = *(const i32x4_b *)(x[j] + k + u * (128 * W) + h * 64 + p);
+        for (int j = 0; j < MT; ++j) vx[u][h][j] = load_any<SHIFT>(x[j] + k + u * (128 * W) + h * 64 + p);
       }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
@@ -423,6 +437,11 @@ int cut_of(int64_t M, int N, int K, Cut *c) {
   return side;
 }
 
+// Whether all rows of both operands start at multiples of so many bytes.
+bool aligned_to(const MatmulArgs &a, int bytes) {
+  return (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & (bytes - 1)) == 0;
+}
+
 // Lets a kernel have its LDS, once per device (`done`: one bit each; a device past the 64th is told every time).
 hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
   int dev = 0;
@@ -448,13 +467,14 @@ template <typename TO, bool ALIGNED, int T> hipError_t run_tiles(const MatmulArg
 }
 
 template <typename TO, int T> hipError_t run_cut(const MatmulArgs &a, const Cut &c, hipStream_t s) {
-  const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
   const bool near = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
-  return aligned && near ? run_tiles<TO, true, T>(a, c, s) : run_tiles<TO, false, T>(a, c, s);
+  return aligned_to(a, 16) && near ? run_tiles<TO, true, T>(a, c, s) : run_tiles<TO, false, T>(a, c, s);
 }
 
 template <typename TO, int MT, int NT, int U> hipError_t run_rows(const MatmulArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U>), dim3((a.N + 16 * NT - 1) / (16 * NT)), dim3(1024), 0, s, a);
+  const dim3 grid((a.N + 16 * NT - 1) / (16 * NT));
+  if (aligned_to(a, 4)) hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U, false>), grid, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U, true>), grid, dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
