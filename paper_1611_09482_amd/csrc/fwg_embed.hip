@@ -407,10 +407,10 @@ template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_k
   }
 }
 
-// Few tokens: one launch without sorting.  A wave takes a position and a slice of 64 * VEC columns; the wave of a
-// token's first position adds up all of its positions, in order.  The remaining waves clear the rows that no token names,
-// 16 each.  Every block holds the tokens in LDS.  512 tokens of 256 classes x 512 float32: 6.7 us (the host's time for a
-// call), sorted 14.5; all of one class: 36 us, sorted 16, since one wave per slice then adds them all.
+// Few tokens and a table too large for scan_kernel: one launch without sorting.  A wave takes a position and a slice of
+// 64 * VEC columns; the wave of a token's first position adds up all of its positions, in order.  The remaining waves
+// clear the rows that no token names, 16 each.  Every block holds the tokens in LDS.  512 tokens of 4,000 words x 256 bf16:
+// 6.4 us (the host's time for a call), sorted 20; 460 of them alike: 46 us, since one wave per slice then adds them all.
 constexpr int kFew = 512;
 template <typename T, typename TO>
 __global__ void __launch_bounds__(256) few_kernel(EmbedGradArgs a, int slices, int sum_blocks) {
@@ -481,6 +481,66 @@ __global__ void __launch_bounds__(256) few_kernel(EmbedGradArgs a, int slices, i
   }
 }
 
+// Up to 1,024 tokens and a small table: a block takes a row of the table and a slice of 64 * VEC columns; each of its 16
+// waves looks through 64 of the tokens and adds up the row's positions among them, in order, and the waves' sums meet in
+// LDS.  Bound by latency: 1,024 tokens of 256 classes x 512 float32 in 7.5 us (the host's time for a call), sorted 15; if
+// 9 in 10 are of one class 20 us, sorted 16, and of 512 tokens 12 us, by few_kernel 36.
+constexpr int kScanWaves = 16, kScan = 64 * kScanWaves;
+template <typename T, typename TO>
+__global__ void __launch_bounds__(64 * kScanWaves) scan_kernel(EmbedGradArgs a) {
+  constexpr int VEC = El<T>::kVec, B = 8;
+  __shared__ float red[kScanWaves][64 * VEC];
+  __shared__ int some[kScanWaves];  // waves that found positions
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = a.channels;
+  const int row = blockIdx.x, c0 = ((int)blockIdx.y * 64 + lane) * VEC, i0 = wave * 64;
+  const bool full = D >= VEC;  // columns as in sum_kernel
+  const int c = full ? min(c0, D - VEC) : c0, have = c0 < D ? (full ? VEC : D - c0) : 0;
+  float acc[VEC] = {};
+  unsigned long long m = __ballot(i0 + lane < a.n && a.tokens[min(i0 + lane, a.n - 1)] == row);
+  const bool mine = m != 0;
+  if (lane == 0) some[wave] = mine;
+  while (m) {
+    int pos[B];
+    int k = 0;
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      pos[b] = i0 + (m ? __ffsll((long long)m) - 1 : 0);
+      k += m ? 1 : 0;
+      m &= m - 1;
+    }
+    float v[B][VEC];
+    if (full) {
+      u32x4 raw[B];
+#pragma unroll
+      for (int b = 0; b < B; ++b) raw[b] = *(const u32x4_el *)((const T *)a.grad + (int64_t)pos[b] * a.ld_grad + c);
+#pragma unroll
+      for (int b = 0; b < B; ++b) expand(raw[b], v[b]);
+    } else {
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        load_part((const T *)a.grad + (int64_t)pos[b] * a.ld_grad + c, b < k ? have : 0, 0.f, v[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int x = 0; x < VEC; ++x) acc[x] += b < k ? v[b][x] : 0.f;
+  }
+  if (mine) store(&red[wave][lane * VEC], acc);
+  __syncthreads();
+  if (wave != 0) return;
+  for (unsigned long long w = __ballot(lane > 0 && lane < kScanWaves && some[lane & (kScanWaves - 1)]); w; w &= w - 1)
+#pragma unroll
+    for (int x = 0; x < VEC; ++x) acc[x] += red[__ffsll((long long)w) - 1][lane * VEC + x];
+#pragma unroll
+  for (int x = 0; x < VEC; ++x) acc[x] *= a.scale;
+  store_part((TO *)a.out + (int64_t)row * a.ld_out + c, have, acc);
+}
+// Blocks look for tokens in vain where a table has many rows: 4,096 rows take 512 tokens 8.6 to 11 us and few_kernel 6.4,
+// 1,024 tokens 10 to 13 us and the sort 20.
+bool scan_form(int n, int vocab, int slices) {
+  return n > 0 && n <= kScan && (int64_t)vocab * slices <= (n <= kFew ? 2048 : 4096);
+}
+
 struct GradPlan {
   int tile, tiles, passes, bits, part, parts;
   size_t off_pair[2], off_hist, off_long, off_rows, off_partial, total;
@@ -521,8 +581,12 @@ GradPlan plan_of(int64_t n, int vocab, int channels) {
 }
 
 template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, hipStream_t s) {
+  const int slices = (g.channels + 64 * El<T>::kVec - 1) / (64 * El<T>::kVec);
+  if (scan_form(g.n, g.vocab, slices)) {
+    hipLaunchKernelGGL((scan_kernel<T, TO>), dim3(g.vocab, slices), dim3(64 * kScanWaves), 0, s, g);
+    return hipGetLastError();
+  }
   if (g.n <= kFew) {
-    const int slices = (g.channels + 64 * El<T>::kVec - 1) / (64 * El<T>::kVec);
     const int sum_blocks = (int)(((int64_t)g.n * slices + 3) / 4), zero_blocks = (int)(((int64_t)g.vocab + 63) / 64);
     hipLaunchKernelGGL((few_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, g, slices,
                        sum_blocks);
@@ -537,7 +601,7 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   a.long_rows = (int2 *)(g.ws + p.off_rows);
   a.part = p.part;
   a.parts = p.parts;
-  a.slices = (g.channels + 64 * El<T>::kVec - 1) / (64 * El<T>::kVec);
+  a.slices = slices;
   a.sorted = nullptr;
   int *hist = (int *)(g.ws + p.off_hist);
   // up to 16,384 tokens every block counts all of them itself, which takes less than a launch

@@ -137,7 +137,9 @@ def token_pattern(kind, n, V, seed):
     (5000, 1 << 20, 9, "uniform"), (5000, (1 << 27) + 5, 1, "uniform"), (300000, 70, 1100, "frequent"),
     (40000, 2500, 2048, "uniform"), (1000, 60, 64, "uniform"), (30000, 3, 4, "same"),
     (511, 300, 520, "frequent"), (512, 70000, 100, "padded"), (513, 40, 1024, "frequent"), (512, 9, 300, "same"),
-    (500, 17, 1031, "descending"),
+    (500, 17, 1031, "descending"), (1024, 256, 512, "frequent"), (1024, 4096, 250, "same"), (1024, 1, 1030, "same"),
+    (1025, 31, 20, "padded"), (1024, 4097, 64, "frequent"), (700, 900, 3, "padded"), (512, 2049, 256, "same"),
+    (511, 2048, 256, "descending"), (66, 5000, 2, "frequent"), (1, 1, 2056, "uniform"),
 ])
 def test_embed_grad(n, V, D, kind, dtype):
     tok = token_pattern(kind, n, V, n + V)
