@@ -86,13 +86,40 @@ __device__ __forceinline__ Pair entry(const Pair *in, const int32_t *tokens, int
 }
 __device__ __forceinline__ int digit_of(Pair p, int shift, int mask) { return (int)(p >> (32 + shift)) & mask; }
 
+// Rows that no token names, cleared by blocks beside the sort's, which leave the memory idle: 65,521 tokens of 50,001
+// words x 2,048, bf16 into a float32 table, 181 us for 198 with sum_kernel clearing them as it does after one-launch sorts.
+struct ZeroArgs {
+  char *out;
+  int64_t ld, bytes;  // of a row, in bytes
+  int row0, row1;     // this launch's share
+};
+constexpr int kZeroRows = 4;  // per wave
+// (a token's entry of `some` names a position of that token if and only if it occurs, whatever the memory held before)
+__device__ __forceinline__ void zero_rows(const ZeroArgs &z, const int *some, const int32_t *tokens, int n, int block) {
+  typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
+  const int lane = threadIdx.x & 63, r0 = z.row0 + (block * kSortWaves + (threadIdx.x >> 6)) * kZeroRows;
+  bool absent = false;
+  if (lane < kZeroRows && r0 + lane < z.row1) {
+    const unsigned at = some[r0 + lane];
+    absent = at >= (unsigned)n || tokens[at] != r0 + lane;
+  }
+  for (unsigned long long m = __ballot(absent); m; m &= m - 1) {
+    char *row = z.out + (int64_t)(r0 + __ffsll((long long)m) - 1) * z.ld;
+    const int64_t whole = z.bytes & ~(int64_t)15;
+    for (int64_t o = lane * 16; o < whole; o += 64 * 16) *(u32x4_2 *)(row + o) = u32x4_2{0u, 0u, 0u, 0u};
+    if (whole + lane * 2 < z.bytes) *(uint16_t *)(row + whole + lane * 2) = 0;
+  }
+}
+
 struct SortArgs {
   const Pair *in;         // NULL: the tokens in their own order
   Pair *out;
   const int32_t *tokens;
   int *hist;              // [tile][bin]: this pass's digits (NULL: each block counts all tokens itself)
   int *clear;             // cleared by the first kernel of a call
-  int vocab, n, tile, shift, bits;
+  int vocab, n, tile, tiles, shift, bits;
+  int *some;              // [vocab] for each token that occurs one of its positions, else anything; NULL: not kept
+  ZeroArgs zero;
 };
 
 // Counts of the tiles' digits.  (Counting the next pass's digits in scatter_kernel instead, by global atomics, takes
@@ -100,18 +127,23 @@ struct SortArgs {
 __global__ void __launch_bounds__(1024) hist_kernel(SortArgs a) {
   __shared__ int cnt[kMaxBins];
   const int bins = 1 << a.bits;
+  if ((int)blockIdx.x >= a.tiles) return zero_rows(a.zero, a.some, a.tokens, a.n, blockIdx.x - a.tiles);
   for (int b = threadIdx.x; b < bins; b += 1024) cnt[b] = 0;
   if (a.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
   __syncthreads();
   const int i0 = blockIdx.x * a.tile, i1 = min(a.n, i0 + a.tile);
-  for (int i = i0 + threadIdx.x; i < i1; i += 1024)
-    atomicAdd(&cnt[digit_of(entry(a.in, a.tokens, a.vocab, i), a.shift, bins - 1)], 1);
+  for (int i = i0 + threadIdx.x; i < i1; i += 1024) {
+    const Pair p = entry(a.in, a.tokens, a.vocab, i);
+    atomicAdd(&cnt[digit_of(p, a.shift, bins - 1)], 1);
+    if (!a.in && a.some && (int)(p >> 32) < a.vocab) a.some[p >> 32] = i;
+  }
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += 1024) a.hist[blockIdx.x * bins + b] = cnt[b];
 }
 
-// Bound by latency, not bytes: 65,521 tokens (32 blocks) in 6.6 us a pass, and 4.6 us for hist_kernel.  Up to 16,384 tokens
-// each block counts all tokens itself instead of reading hist: 10,656 tokens in 8.7 us (2.7 + 6.9 us and a launch before).
+// Bound by latency, not bytes: 65,521 tokens (32 blocks) in 6.6 us a pass, and 4.6 us for hist_kernel (15 to 17 us
+// each with 276 MB of zeros beside them).  Up to 16,384 tokens each block counts all tokens itself instead of reading hist:
+// 10,656 tokens in 8.7 us (2.7 + 6.9 us and a launch before).
 //
 // Scatters a tile in its order: the place of an entry is the number of smaller digits anywhere, plus its digit's
 // in earlier tiles, earlier waves and earlier lanes.  Each wave owns a contiguous share of the tile.
@@ -120,6 +152,7 @@ __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
   __shared__ int wsum[kSortWaves];
   __shared__ int ahead[kMaxBins], behind[kMaxBins];  // digits of other tiles, before this one and after it
   const int bins = 1 << a.bits, n = a.n, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if ((int)blockIdx.x >= a.tiles) return zero_rows(a.zero, a.some, a.tokens, n, blockIdx.x - a.tiles);
   if (a.clear && !a.hist && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
 #pragma unroll
   for (int b = 0; b < kSortWaves * kMaxBins / 1024; ++b) (&place[0][0])[b * 1024 + threadIdx.x] = 0;
@@ -129,7 +162,7 @@ __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
   int total = 0, before = 0;
   if (b < bins && a.hist) {
 #pragma unroll 8
-    for (int t = 0; t < (int)gridDim.x; ++t) {
+    for (int t = 0; t < a.tiles; ++t) {
       const int c = a.hist[t * bins + b];
       before += t < (int)blockIdx.x ? c : 0;
       total += c;
@@ -237,8 +270,9 @@ __device__ __forceinline__ void expand(const u32x4 &r, float (&v)[8]) {
   }
 }
 
-// Bound by memory.  65,521 tokens of 50,001 words x 2,048 bf16, the table's zeros included, in 130 to 155 us (4.4 to 5.2
-// TB/s), of 192 for the call; 10,656 tokens of 256 classes x 512 float32 in 6.5 us of 21.
+// Bound by memory.  65,521 tokens of 50,001 words x 2,048, bf16 into float32, in 121 us (402 MB, while zeros that the
+// launches before wrote are still on their way from the caches to the memory), of 181 for the call; 10,656 tokens of 256
+// classes x 512 float32 in 6.5 us of 21.
 //
 // A part's sums.  Wave task = (part, slice of 64 * VEC columns).  A row belongs to the part in which its positions
 // begin, which sums it whole, past the part's end too; only rows of more than a part's positions (long) are summed part
@@ -543,7 +577,8 @@ bool scan_form(int n, int vocab, int slices) {
 
 struct GradPlan {
   int tile, tiles, passes, bits, part, parts;
-  size_t off_pair[2], off_hist, off_long, off_rows, off_partial, total;
+  bool counted, zero_early;
+  size_t off_pair[2], off_hist, off_some, off_long, off_rows, off_partial, total;
 };
 
 GradPlan plan_of(int64_t n, int vocab, int channels) {
@@ -570,6 +605,13 @@ GradPlan plan_of(int64_t n, int vocab, int channels) {
   }
   p.off_hist = o;
   o += up((size_t)p.tiles << (p.bits + 2));
+  // up to 16,384 tokens every block counts all of them itself, which takes less than a launch
+  p.counted = p.tiles > 1 && n > 16384;
+  // (narrower tables are cleared in no time, and `some` would be more than a few hundredths of them: 300,000 words x 64
+  // bf16 take 20,000 tokens 48 us with it and 65 without)
+  p.zero_early = p.counted && channels >= 64;
+  p.off_some = o;
+  o += p.zero_early ? up((size_t)vocab * sizeof(int)) : 0;
   p.off_long = o;
   o += 256;
   p.off_rows = o;
@@ -604,18 +646,41 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   a.slices = slices;
   a.sorted = nullptr;
   int *hist = (int *)(g.ws + p.off_hist);
-  // up to 16,384 tokens every block counts all of them itself, which takes less than a launch
-  const bool counted = p.tiles > 1 && g.n > 16384;
+  const int shares = p.zero_early ? 2 * p.passes - 1 : 0;  // the launches after the first
+  const int per_share = shares ? (g.vocab + shares - 1) / shares : 0;
+  int share = 0;
+  SortArgs q;
+  q.tokens = g.tokens;
+  q.hist = p.counted ? hist : nullptr;
+  q.vocab = g.vocab;
+  q.n = g.n;
+  q.tile = p.tile;
+  q.tiles = p.tiles;
+  q.bits = p.bits;
+  q.some = p.zero_early ? (int *)(g.ws + p.off_some) : nullptr;
+  q.zero = {(char *)g.out, g.ld_out * (int64_t)sizeof(TO), g.channels * (int64_t)sizeof(TO), 0, 0};
+  auto grid = [&](bool clears) {
+    if (!clears || !shares) return dim3(p.tiles);
+    q.zero.row0 = (int)((int64_t)share * per_share < g.vocab ? (int64_t)share * per_share : g.vocab);
+    q.zero.row1 = g.vocab - q.zero.row0 < per_share ? g.vocab : q.zero.row0 + per_share;
+    ++share;
+    return dim3(p.tiles + (q.zero.row1 - q.zero.row0 + kSortWaves * kZeroRows - 1) / (kSortWaves * kZeroRows));
+  };
   for (int k = 0; k < p.passes; ++k) {
-    Pair *out = (Pair *)(g.ws + p.off_pair[k & 1]);
-    const SortArgs q{a.sorted, out, g.tokens, counted ? hist : nullptr, k == 0 ? a.n_long : nullptr,
-                     g.vocab, g.n, p.tile, k * p.bits, p.bits};
-    if (counted) hipLaunchKernelGGL(hist_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
-    hipLaunchKernelGGL(scatter_kernel, dim3(p.tiles), dim3(1024), 0, s, q);
-    a.sorted = out;
+    q.in = a.sorted;
+    q.out = (Pair *)(g.ws + p.off_pair[k & 1]);
+    q.clear = k == 0 ? a.n_long : nullptr;
+    q.shift = k * p.bits;
+    if (p.counted) {
+      const dim3 blocks = grid(k > 0);
+      hipLaunchKernelGGL(hist_kernel, blocks, dim3(1024), 0, s, q);
+    }
+    const dim3 blocks = grid(true);
+    hipLaunchKernelGGL(scatter_kernel, blocks, dim3(1024), 0, s, q);
+    a.sorted = q.out;
   }
   const int64_t tasks = (int64_t)p.parts * a.slices;
-  const int sum_blocks = (int)((tasks + 3) / 4), zero_blocks = (int)(((int64_t)g.vocab + 63) / 64);
+  const int sum_blocks = (int)((tasks + 3) / 4), zero_blocks = p.zero_early ? 0 : (int)(((int64_t)g.vocab + 63) / 64);
   hipLaunchKernelGGL((sum_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, a, sum_blocks);
   if (p.parts > 1) {
     const int64_t most = (int64_t)p.parts * ((g.channels + 255) / 256);

@@ -139,7 +139,8 @@ def token_pattern(kind, n, V, seed):
     (511, 300, 520, "frequent"), (512, 70000, 100, "padded"), (513, 40, 1024, "frequent"), (512, 9, 300, "same"),
     (500, 17, 1031, "descending"), (1024, 256, 512, "frequent"), (1024, 4096, 250, "same"), (1024, 1, 1030, "same"),
     (1025, 31, 20, "padded"), (1024, 4097, 64, "frequent"), (700, 900, 3, "padded"), (512, 2049, 256, "same"),
-    (511, 2048, 256, "descending"), (66, 5000, 2, "frequent"), (1, 1, 2056, "uniform"),
+    (511, 2048, 256, "descending"), (66, 5000, 2, "frequent"), (1, 1, 2056, "uniform"), (20000, 300000, 67, "frequent"),
+    (16385, 5, 64, "padded"), (17000, 511, 65, "same"), (30000, 66000, 64, "descending"),
 ])
 def test_embed_grad(n, V, D, kind, dtype):
     tok = token_pattern(kind, n, V, n + V)
@@ -169,6 +170,21 @@ def test_embed_grad_nothing_and_broadcast():
     wide = torch.full((40, 14), 5.0, device="cuda")
     ops.embed_grad(row.expand(5, 30, 10), tok, 40, scale=2.0, out=wide[:, 3:13])
     assert torch.equal(wide[:, 3:13], got) and bool((wide[:, :3] == 5).all()) and bool((wide[:, 13:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,V,D", [(17000, 700, 67), (20000, 150001, 90), (40000, 400, 1030)])
+def test_embed_grad_clears_between(n, V, D, dtype):
+    """Rows named by one call and not by the next are cleared, and nothing is written beside the rows."""
+    grad, even = randn(1, n, D), ints(2, 0, V // 2, n) * 2
+    wide = torch.full((V, D + 5), 7.0, dtype=dtype, device="cuda")
+    for tok in (even, even + 1, even, torch.full_like(even, V), even + 1):
+        wide[:, 1:D + 1] = 9.0
+        ops.embed_grad(grad, tok, V, out=wide[:, 1:D + 1])
+        want, mag, count = plain_embed_grad(grad, tok, V, 1.0)
+        got = wide[:, 1:D + 1].double()
+        assert bool(((got - want).abs() <= (count[:, None] + 4) * U * mag + out_rounding(dtype) * want.abs()).all())
+        assert bool((got[count == 0] == 0).all()) and bool((wide[:, 0] == 7).all()) and bool((wide[:, D + 1:] == 7).all())
 
 
 def test_embed_grad_against_differences():
