@@ -523,7 +523,7 @@ constexpr int kScanWaves = 16, kScan = 64 * kScanWaves;
 template <typename T, typename TO>
 __global__ void __launch_bounds__(64 * kScanWaves) scan_kernel(EmbedGradArgs a) {
   constexpr int VEC = El<T>::kVec, B = 8;
-  __shared__ float red[kScanWaves][64 * VEC];
+  __shared__ __align__(16) float red[kScanWaves][64 * VEC];
   __shared__ int some[kScanWaves];  // waves that found positions
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = a.channels;
   const int row = blockIdx.x, c0 = ((int)blockIdx.y * 64 + lane) * VEC, i0 = wave * 64;
@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(64 * kScanWaves) scan_kernel(EmbedGradArgs a) 
 #pragma unroll
       for (int x = 0; x < VEC; ++x) acc[x] += b < k ? v[b][x] : 0.f;
   }
-  if (mine) store(&red[wave][lane * VEC], acc);
+  if (mine) store_aligned(&red[wave][lane * VEC], acc);
   __syncthreads();
   if (wave != 0) return;
   for (unsigned long long w = __ballot(lane > 0 && lane < kScanWaves && some[lane & (kScanWaves - 1)]); w; w &= w - 1)

@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulArgs a
                   v[e] = (float)acc[i][j0 + jj][4 * g + e] * sx * ws[e];
                   if (a.bias) v[e] += b[e];
                 }
-                store((TO *)to, v);
+                store_aligned((TO *)to, v);
               }
             }
           }

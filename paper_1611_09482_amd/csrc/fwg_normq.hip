@@ -101,8 +101,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_quant_kernel(NormA
       uint32_t w[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < kE; ++i) w[i / 4] |= ((uint32_t)(int)v[i] & 0xffu) << (8 * (i % 4));
-      typedef unsigned int u32x2_b __attribute__((ext_vector_type(2), aligned(1)));
-      put_vector<STREAM>((u32x2_b *)q, u32x2_b{w[0], w[1]});
+      store_bytes<STREAM>(q, w[0], w[1]);
     } else {
       for (int i = 0; i < kE; ++i)
         if (i < have) q[i] = (int8_t)(int)v[i];

@@ -23,6 +23,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 typedef float f32x4_el __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned int u32x4_el __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned int u32x2_el __attribute__((ext_vector_type(2), aligned(2)));
+typedef unsigned int u32x2_b __attribute__((ext_vector_type(2), aligned(1)));
 
 // Elements of one 16-byte access.
 template <typename T> struct El;
@@ -62,24 +63,46 @@ template <int N> __device__ __forceinline__ void load(const uint16_t *p, float (
     }
   }
 }
-// STREAM: past the caches (outputs too large to be found there by whoever reads them next).
-template <bool STREAM, typename V> __device__ __forceinline__ void put_vector(V *p, V v) {
-  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
-  else *p = v;
+// Vectors to an element's address.  STREAM: past the caches (outputs too large to be found there by whoever reads them
+// next).  Each vector type is named at its store: as a template's argument a type loses its alignment attribute, and
+// the store would promise the vector's own.
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+template <bool STREAM> __device__ __forceinline__ void put_vector(float *p, f32x4 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, (f32x4_el *)p);
+  else *(f32x4_el *)p = v;
+}
+template <bool STREAM> __device__ __forceinline__ void put_vector(uint16_t *p, u32x4 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, (u32x4_el *)p);
+  else *(u32x4_el *)p = v;
+}
+template <bool STREAM> __device__ __forceinline__ void put_vector(uint16_t *p, u32x2 v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, (u32x2_el *)p);
+  else *(u32x2_el *)p = v;
+}
+// Eight bytes, first to last in (lo, hi).
+template <bool STREAM> __device__ __forceinline__ void store_bytes(int8_t *p, uint32_t lo, uint32_t hi) {
+  if constexpr (STREAM) __builtin_nontemporal_store(u32x2{lo, hi}, (u32x2_b *)p);
+  else *(u32x2_b *)p = u32x2{lo, hi};
 }
 template <bool STREAM = false, int N> __device__ __forceinline__ void store(float *p, const float (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N / 4; ++i)
-    put_vector<STREAM>((f32x4_el *)(p + 4 * i), f32x4_el{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]});
+    put_vector<STREAM>(p + 4 * i, f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]});
 }
 template <bool STREAM = false, int N> __device__ __forceinline__ void store(uint16_t *p, const float (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N / 8; ++i)
-    put_vector<STREAM>((u32x4_el *)(p + 8 * i),
-                       u32x4_el{pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
-                                pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7])});
-  if constexpr (N % 8 == 4)
-    put_vector<STREAM>((u32x2_el *)(p + N - 4), u32x2_el{pack2(v[N - 4], v[N - 3]), pack2(v[N - 2], v[N - 1])});
+    put_vector<STREAM>(p + 8 * i, u32x4{pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
+                                        pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7])});
+  if constexpr (N % 8 == 4) put_vector<STREAM>(p + N - 4, u32x2{pack2(v[N - 4], v[N - 3]), pack2(v[N - 2], v[N - 1])});
+}
+// To an address that is a multiple of the vector's size, as rows in LDS are.
+template <int N> __device__ __forceinline__ void store_aligned(float *p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) *(f32x4 *)(p + 4 * i) = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+}
+__device__ __forceinline__ void store_aligned(uint16_t *p, const float (&v)[4]) {
+  *(u32x2 *)p = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
 
 // The same where only the first `have` elements exist (have may be <= 0 or >= N); absent ones read as `fill`.
