@@ -317,8 +317,10 @@ int fwg_quant_rows(int32_t dtype, int64_t rows, int32_t channels, const void *x,
                    int64_t q_stride, float *scale, void *hip_stream);
 
 /* Residual addition, RMS norm and rows in 8 bits: h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain, q and
- * scale of y as in fwg_quant_rows (zero also where every |h gain| is below 2^-120; NaN also where the sum of
- * squares leaves float32's range).  residual NULL: none; gain (float32 [channels]) NULL: ones.  Optional outputs:
+ * scale of y as in fwg_quant_rows (zero also where every |h gain| is below 2^-120, eps of 0 included; else NaN also
+ * where the sum of squares passes float32's largest value, or is 0 in float32 and eps is too).  With eps of 0 the scale
+ * has fewer correct bits where squares lie below float32's normal numbers (2^-126).
+ * residual NULL: none; gain (float32 [channels]) NULL: ones.  Optional outputs:
  * summed, h rounded to dtype (may be x or residual itself: the residual stream in place), and values, q * scale
  * in bf16, for consumers that read bf16.  The norm is taken of the unrounded sum. */
 int fwg_norm_quant(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride,

@@ -84,8 +84,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_quant_kernel(NormA
   }
   const float rs = a.norm ? rsqrtf(ss / (float)a.channels + a.eps) : 1.f;
   const float amax = top * rs;
-  const bool bad = !(ss < kInf) || !(amax < kInf);
-  const bool zero = bad || !(amax >= kTiny) || !(top >= kTinyIn);
+  // a row of (nearly) nothing is zero whatever 1 / rms is: it may be infinite where eps is 0
+  const bool nothing = !(top >= kTinyIn);
+  const bool bad = !(ss < kInf) || (!nothing && !(amax < kInf));
+  const bool zero = bad || nothing || !(amax >= kTiny);
   const float inv = zero ? 0.f : 127.f / top;
   const float scale = bad ? __builtin_nanf("") : zero ? 0.f : amax / 127.f;
   if (t == 0) a.scale[r] = scale;

@@ -1,0 +1,51 @@
+"""The token operators at arguments and sizes where only one of their kernels' paths, or none of the ordinary ones, runs.
+
+Plain evaluations, helpers and bars are those of test_gpu_operators.py."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_1611_09482_amd import ops  # noqa: E402
+from test_gpu_operators import F32, TYPES, check_rows, randn  # noqa: E402
+
+
+# ---- 8-bit rows ----
+
+@pytest.mark.parametrize("channels", [5, 300, 3000, 9000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_quant_without_eps(channels, dtype):
+    """eps = 0: rows whose every |h gain| is below 2^-120 are zero, whatever 1 / sqrt(mean h^2) is."""
+    x = randn(channels, 7, channels).to(dtype)
+    x[1] = 0
+    x[2] = 2.0 ** -121
+    x[3] = (x[3].float() * 2.0 ** -50).to(dtype)  # small, and the squares are normal numbers
+    x[4, channels // 2] = math.nan
+    x[5] = 0
+    x[5, channels - 1] = -3.0
+    gain = 1 + 0.1 * randn(1, channels).clamp(-3, 3)
+    got = ops.norm_quant(x, gain, eps=0.0, values=True)
+    assert torch.isnan(got.scale).tolist() == [False, False, False, False, True, False, False]
+    for r in (1, 2):
+        assert got.scale[r] == 0 and not got.q[r].any() and not got.values[r].any()
+    h = x[[0, 3, 5, 6]].double()
+    check_rows(h / torch.sqrt((h * h).mean(-1, keepdim=True)) * gain.double(), got.q[[0, 3, 5, 6]], got.scale[[0, 3, 5, 6]])
+    gone = ops.norm_quant(x[:2], gain, residual=-x[:2], eps=0.0)  # the residual takes all of the row away
+    assert not gone.scale.any() and not gone.q.any() and not gone.summed.any()
+    for rows in (x[:1], x[1:2]):  # a gain of zero
+        got = ops.norm_quant(rows, torch.zeros_like(gain), eps=0.0)
+        assert got.scale[0] == 0 and not got.q.any()
+
+
+def test_padding_tokens_rows_through_the_product():
+    """The zero row of a padding token stays one: its outputs are the bias."""
+    table, tok = randn(1, 50, 256), torch.tensor([3, -1, 7], dtype=torch.int32, device="cuda")
+    w, bias = ops.quant_rows(randn(2, 40, 256)), randn(3, 40)
+    x = ops.norm_quant(ops.embed(table, tok), eps=0.0)
+    y = ops.matmul_quant(x.q, x.scale, w.q, w.scale, bias=bias, dtype=F32)
+    assert torch.equal(y[1], bias) and not torch.isnan(y).any()
