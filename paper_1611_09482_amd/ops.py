@@ -17,7 +17,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import FWG_BF16, FWG_F32, FwgError, _check, load_library  # noqa: F401 (FwgError: what calls raise)
+from .binding import FWG_BF16, FWG_EINVAL, FWG_EUNSUPPORTED, FWG_F32, FwgError, _check, load_library
 
 _TYPES = {torch.float32: FWG_F32, torch.bfloat16: FWG_BF16}
 _lib = None
@@ -48,6 +48,18 @@ def _typed(name: str, t, dtype, device: int) -> None:
         raise TypeError(f"{name} is {t.dtype}: {dtype} is wanted")
 
 
+_MOST = 2 ** 31 - 1
+
+
+def _int32(name: str, n: int) -> int:
+    """A size that the library takes in 32 bits: ctypes would pass on the low 32 bits of a larger one."""
+    if n > _MOST:
+        raise FwgError(FWG_EUNSUPPORTED, f"{name} is {n}: at most 2^31 - 1 is supported")
+    if n < -_MOST:
+        raise FwgError(FWG_EINVAL, f"{name} is {n}")
+    return n
+
+
 def _matrix(name: str, t, device: int, out: bool = False):
     """(element type, rows, width, stride) of a float32 or bfloat16 tensor seen as rows."""
     if not isinstance(t, torch.Tensor) or t.get_device() != device:
@@ -58,9 +70,18 @@ def _matrix(name: str, t, device: int, out: bool = False):
     shape = t.shape
     if len(shape) == 2 and t.is_contiguous():
         rows, width = shape
+        if width > _MOST:
+            _int32(f"{name}'s width", width)
         return kind, rows, width, width
     rows, width, stride = _rows(name, t, out)
     return kind, rows, width, stride
+
+
+def _table(name: str, t, device: int):
+    """_matrix() of a tensor of two dimensions whose rows are tokens."""
+    kind, vocab, width, stride = _matrix(name, t, device)
+    _flat(name, t)
+    return kind, _int32(f"{name}'s length", vocab), width, stride
 
 
 def _rows(name: str, t, out: bool = False):
@@ -68,7 +89,7 @@ def _rows(name: str, t, out: bool = False):
     shape, strides = t.shape, t.stride()
     if not shape:
         raise ValueError(f"{name} has no dimensions: rows are wanted")
-    width = shape[-1]
+    width = _int32(f"{name}'s width", shape[-1])
     if width > 1 and strides[-1] != 1:
         raise ValueError(f"{name}: the elements of a row have to be consecutive (stride {strides[-1]})")
     if len(shape) == 2:
@@ -134,7 +155,11 @@ def _workspace(need: int):
 def _bytes(call: str, *sizes) -> int:
     """Workspace bytes: a pure function of the sizes."""
     n = ctypes.c_size_t(0)
-    _check(getattr(_library(), call)(*sizes, ctypes.byref(n)))
+    function = getattr(_library(), call)
+    for size, kind in zip(sizes, function.argtypes):
+        if kind is ctypes.c_int32:
+            _int32("a size", size)
+    _check(function(*sizes, ctypes.byref(n)))
     return n.value
 
 
@@ -143,8 +168,7 @@ def embed(table, tokens, scale: float = 1.0, out=None):
     a token outside [0, vocab) is padding and gives a zero row.  out: [*tokens.shape][channels], float32 or bfloat16
     (default: of the table's type)."""
     dev = _device()
-    kind, vocab, channels, stride = _matrix("table", table, dev)
-    _flat("table", table)
+    kind, vocab, channels, stride = _table("table", table, dev)
     n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
     ids = _vector("tokens", tokens, n, torch.int32, dev)
     shape = tokens.shape + (channels,)
@@ -242,6 +266,7 @@ def matmul_quant(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=No
     rows, inner, stride = _rows("x", x)
     _flat("w", w)
     outputs, winner, wstride = _rows("w", w)
+    _int32("w's length", outputs)
     if winner != inner:
         raise ValueError(f"w has {winner} inner elements: {inner} are wanted")
     shape = x.shape[:-1] + (outputs,)

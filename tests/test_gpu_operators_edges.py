@@ -49,3 +49,18 @@ def test_padding_tokens_rows_through_the_product():
     x = ops.norm_quant(ops.embed(table, tok), eps=0.0)
     y = ops.matmul_quant(x.q, x.scale, w.q, w.scale, bias=bias, dtype=F32)
     assert torch.equal(y[1], bias) and not torch.isnan(y).any()
+
+
+# ---- sizes past 32 bits ----
+
+def test_sizes_past_32_bits():
+    """Refused before anything is allocated or enqueued."""
+    x, tok, n = randn(1, 4, 6), torch.zeros(4, dtype=torch.int32, device="cuda"), 2 ** 32 + 6
+    wide = torch.empty((1, n), dtype=torch.int8, device="cuda")
+    one = torch.ones(1, device="cuda")
+    before = torch.cuda.max_memory_allocated()
+    for call in (lambda: ops.embed_grad(x, tok, n), lambda: ops.log_probs(x, tok, top=2 ** 32 + 3),
+                 lambda: ops.matmul_quant(wide, one, wide, one), lambda: ops.matmul_quant(wide[:, :1], one, wide.t(), one)):
+        with pytest.raises(ops.FwgError):
+            call()
+    assert torch.cuda.max_memory_allocated() == before

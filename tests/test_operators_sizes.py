@@ -1,0 +1,52 @@
+"""Sizes past 32 bits are refused by the functions on tensors; they do not reach the library cut short (no GPU needed)."""
+import pytest
+
+from paper_1611_09482_amd import binding as B
+
+torch = pytest.importorskip("torch")
+from paper_1611_09482_amd import ops  # noqa: E402
+
+PAST = [2 ** 31, 2 ** 32 + 3, 2 ** 32 + 256, 2 ** 40 + 5]  # the low 32 bits of most are sizes that would pass
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    from paper_1611_09482_amd import build
+    if build.is_stale():
+        build.build()
+    return B.load_library()
+
+
+def refused(call, code=B.FWG_EUNSUPPORTED):
+    with pytest.raises(ops.FwgError) as e:
+        call()
+    assert e.value.code == code
+
+
+@pytest.mark.parametrize("n", PAST)
+def test_workspace_sizes(n):
+    refused(lambda: ops._bytes("fwg_embed_grad_workspace", 5000, n, 64))
+    refused(lambda: ops._bytes("fwg_embed_grad_workspace", 5000, 256, n))
+    refused(lambda: ops._bytes("fwg_matmul_quant_workspace", 5000, n, 64))
+    refused(lambda: ops._bytes("fwg_matmul_quant_workspace", 5000, 64, n))
+    refused(lambda: ops._bytes("fwg_log_probs_workspace", 0, 5, n, 3))
+    refused(lambda: ops._bytes("fwg_log_probs_workspace", 0, 5, 256, n))
+    refused(lambda: ops._bytes("fwg_log_probs_workspace", 0, 5, 256, -2 ** 32 + 3), B.FWG_EINVAL)
+    assert ops._bytes("fwg_embed_grad_workspace", 5000, 256, 64) > 0  # what fits still does
+
+
+@pytest.mark.parametrize("n", PAST)
+def test_rows_and_tables(n):
+    """Tensors without memory: only shapes and strides are looked at."""
+    row = torch.empty((1, n), dtype=torch.bfloat16, device="meta")
+    for out in (False, True):
+        refused(lambda: ops._matrix("x", row, row.get_device(), out))
+        refused(lambda: ops._matrix("x", row.view(1, 1, n), row.get_device(), out))
+    refused(lambda: ops._rows("x", torch.empty((3, n), dtype=torch.int8, device="meta")))
+    table = torch.empty((n, 2), dtype=torch.float32, device="meta")
+    assert ops._matrix("logits", table, table.get_device()) == (B.FWG_F32, n, 2, 2)  # rows are counted in 64 bits
+    refused(lambda: ops._table("table", table, table.get_device()))
+    small = torch.empty((7, 2), dtype=torch.float32, device="meta")
+    assert ops._table("table", small, small.get_device()) == (B.FWG_F32, 7, 2, 2)
+    with pytest.raises(ValueError):
+        ops._table("table", small.view(1, 7, 2), small.get_device())
