@@ -478,10 +478,22 @@ template <typename TO, int T> hipError_t run_cut(const MatmulArgs &a, const Cut 
 }
 
 template <typename TO, int MT, int NT, int U> hipError_t run_rows(const MatmulArgs &a, hipStream_t s) {
-  const dim3 grid((a.N + 16 * NT - 1) / (16 * NT));
-  if (aligned_to(a, 4)) hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U, false>), grid, dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U, true>), grid, dim3(1024), 0, s, a);
-  return hipGetLastError();
+  const bool words = aligned_to(a, 4);
+  constexpr int64_t kSlice = ((int64_t)16 * NT) << 21;  // outputs of a launch: it has at most 2^32 threads
+  for (int64_t n = 0; n < a.N; n += kSlice) {
+    MatmulArgs b = a;
+    b.N = (int)(a.N - n < kSlice ? a.N - n : kSlice);
+    b.w = a.w + n * a.ld_w;
+    b.w_scale = a.w_scale + n;
+    if (a.bias) b.bias = a.bias + n;
+    b.out = (TO *)a.out + n;
+    const dim3 grid((b.N + 16 * NT - 1) / (16 * NT));
+    if (words) hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U, false>), grid, dim3(1024), 0, s, b);
+    else hipLaunchKernelGGL((rows_kernel<TO, MT, NT, U, true>), grid, dim3(1024), 0, s, b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename TO> hipError_t run(const MatmulArgs &a, hipStream_t s) {

@@ -64,3 +64,30 @@ def test_sizes_past_32_bits():
         with pytest.raises(ops.FwgError):
             call()
     assert torch.cuda.max_memory_allocated() == before
+
+
+# ---- 8-bit product ----
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_matmul_quant_outputs_past_one_launch(dtype):
+    """Few rows and 2^27 outputs and more: more blocks of 16 or 32 outputs than one launch has threads for.  Scales are
+    powers of two and sums below 256, so every result is exact in both types."""
+    rows, N, K = 2, (1 << 27) + 45, 4
+    w = torch.randint(-3, 4, (N, K), dtype=torch.int8, device="cuda")
+    x = torch.tensor([[1, -2, 3, 1], [2, 0, -1, 3]], dtype=torch.int8, device="cuda")
+    sx, sw = torch.tensor([2.0, 0.5], device="cuda"), torch.ones(N, device="cuda")
+    sw[::3] = 4.0
+    got = ops.matmul_quant(x, sx, w, sw, dtype=dtype)
+    for r in range(rows):
+        total = torch.zeros(N, device="cuda")
+        for k in range(K):
+            total += w[:, k] * float(x[r, k])
+        assert torch.equal(got[r], (total * sx[r] * sw).to(dtype))
+    # the last slice's bias and outputs, rows at odd bytes
+    tail = 1 << 26
+    bias = (torch.arange(N, device="cuda") % 64).float()
+    odd = torch.empty(N * K + 1, dtype=torch.int8, device="cuda")[1:].view(N, K)
+    odd.copy_(w)
+    again = ops.matmul_quant(x, sx, odd, torch.ones_like(sw), bias=bias, dtype=F32)
+    plain = (got.float() / sw + bias)[:, -tail:]
+    assert torch.equal(again[:, -tail:], plain)
