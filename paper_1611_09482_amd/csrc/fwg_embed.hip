@@ -278,11 +278,11 @@ __device__ __forceinline__ void expand(const u32x4 &r, float (&v)[8]) {
 // begin, which sums it whole, past the part's end too; only rows of more than a part's positions (long) are summed part
 // by part and joined.
 template <typename T, typename TO>
-__global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
+__global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int first_block, int sum_blocks) {
   constexpr int VEC = El<T>::kVec;
-  const int lane = threadIdx.x & 63, D = a.g.channels, n = a.g.n, V = a.g.vocab;
-  if ((int)blockIdx.x < sum_blocks) {
-    const int task = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63, D = a.g.channels, n = a.g.n, V = a.g.vocab, block = first_block + (int)blockIdx.x;
+  if (block < sum_blocks) {
+    const int task = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6));
     // the lane's columns; a vector that would pass the last one is the last whole vector instead, and two lanes then sum
     // and store the same columns, alike
     const int P = a.part, part = task / a.slices, c0 = ((task % a.slices) * 64 + lane) * VEC;
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a, int sum_blocks) {
     return;
   }
   // rows that no token names: each wave looks 16 rows up in the sorted keys and clears the absent ones
-  const int r0 = (((int)blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 6)) * 16;
+  const int r0 = ((block - sum_blocks) * 4 + (threadIdx.x >> 6)) * 16;
   bool absent = false;
   if (lane < 16 && r0 + lane < V) {
     const unsigned row = r0 + lane;
@@ -681,7 +681,12 @@ template <typename T, typename TO> hipError_t run_grad(const EmbedGradArgs &g, h
   }
   const int64_t tasks = (int64_t)p.parts * a.slices;
   const int sum_blocks = (int)((tasks + 3) / 4), zero_blocks = p.zero_early ? 0 : (int)(((int64_t)g.vocab + 63) / 64);
-  hipLaunchKernelGGL((sum_kernel<T, TO>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, a, sum_blocks);
+  // at most 2^32 threads in a launch: repeated rows may make more tasks than that of 2^28 tokens and more
+  constexpr int kBlocks = 1 << 23;
+  for (int b = 0; b < sum_blocks + zero_blocks; b += kBlocks) {
+    const int blocks = sum_blocks + zero_blocks - b < kBlocks ? sum_blocks + zero_blocks - b : kBlocks;
+    hipLaunchKernelGGL((sum_kernel<T, TO>), dim3((unsigned)blocks), dim3(256), 0, s, a, b, sum_blocks);
+  }
   if (p.parts > 1) {
     const int64_t most = (int64_t)p.parts * ((g.channels + 255) / 256);
     int log_lanes = 0;

@@ -91,3 +91,23 @@ def test_matmul_quant_outputs_past_one_launch(dtype):
     again = ops.matmul_quant(x, sx, odd, torch.ones_like(sw), bias=bias, dtype=F32)
     plain = (got.float() / sw + bias)[:, -tail:]
     assert torch.equal(again[:, -tail:], plain)
+
+
+# ---- the table's gradient ----
+
+def test_embed_grad_tasks_past_one_launch():
+    """As many tokens as are supported, one repeated row of gradients: more blocks than one launch has threads for.
+    Sums are whole numbers below 2^24, so they are exact."""
+    n, V, D = 1 << 30, 256, 769
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GB of free memory: the workspace holds two partial sums of 64 tokens each")
+    tok = torch.arange(n, dtype=torch.int32, device="cuda")
+    tok.bitwise_and_(V - 1)
+    tok[:V] = 7
+    row = torch.arange(D, device="cuda").remainder_(4).float()
+    got = ops.embed_grad(row.expand(n, D), tok, V)
+    count = torch.full((V,), float(n // V - 1), device="cuda")
+    count[7] += V
+    del tok
+    torch.cuda.empty_cache()
+    assert torch.equal(got, count[:, None] * row)
