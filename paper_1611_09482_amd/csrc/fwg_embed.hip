@@ -231,13 +231,13 @@ __global__ void __launch_bounds__(1024) scatter_kernel(SortArgs a) {
       same &= (d >> k) & 1 ? one : ~one;
     }
     const int rank = __popcll(same & ((1ull << lane) - 1));
+    const int at = in_share ? place[wave][d] : 0;
+    in_order();  // every lane has read its digit's place before that place moves on
     if (in_share) {
-      const int at = place[wave][d];
       a.out[at + rank] = p;
-      // after the reads of every lane: the wave runs in step
       if (rank == 0) place[wave][d] = at + __popcll(same);
     }
-    __builtin_amdgcn_wave_barrier();
+    in_order();
   };
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)

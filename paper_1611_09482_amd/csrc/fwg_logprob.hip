@@ -93,9 +93,6 @@ struct Select {
   int2 slot[kSlots];
   double cand[64], place[kMaxTop];
 };
-// A wave's LDS accesses are in order; this keeps the compiler to the order of the source.
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
-
 // Floats as whole numbers of the same order, and back (no NaN).
 __device__ __forceinline__ int ordered(float v) {
   const int b = __float_as_int(v);

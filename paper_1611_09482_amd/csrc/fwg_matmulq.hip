@@ -27,9 +27,6 @@ using namespace opd;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4_b __attribute__((ext_vector_type(4), aligned(1)));
 
-// A wave's LDS accesses are in order; this keeps the compiler to the order of the source.
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
-
 __device__ __forceinline__ i32x4 mma(const i32x4 &a, const i32x4 &b, const i32x4 &c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }

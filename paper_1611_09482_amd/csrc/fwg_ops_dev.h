@@ -126,6 +126,9 @@ __device__ __forceinline__ void store_part(T *p, int have, const float (&v)[N]) 
     if (i < have) put(p + i, v[i]);
 }
 
+// A wave's LDS accesses are in order; this keeps the compiler to the order of the source.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Reductions over the wavefront: inside rows of 16 lanes by DPP moves, the four rows by lane reads.
 // The result is the same in every lane.
 template <int CTRL> __device__ __forceinline__ float dpp_f(float v) { return mfd::dpp<CTRL>(v); }

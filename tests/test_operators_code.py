@@ -52,3 +52,11 @@ def test_no_access_claims_more_alignment_than_its_type(name):
     r = subprocess.run([B.HIPCC] + B.FLAGS + ["--cuda-device-only", "-fsyntax-only", "-Werror=align-mismatch",
                                               os.path.join(B.CSRC, name)], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_lanes_of_the_sort_see_each_others_places(tmp_path):
+    """The radix sort's lanes read places in LDS that other lanes of the wave have just moved on: a wavefront fence has
+    to stand between, or the compiler may exchange the two."""
+    ir = device_ir(os.path.join(B.CSRC, "fwg_embed.hip"), str(tmp_path / "embed.ll"))
+    body = re.search(r"define [^\n]*scatter_kernel.*?\n}", ir, re.S).group(0)
+    assert 'syncscope("wavefront")' in body
