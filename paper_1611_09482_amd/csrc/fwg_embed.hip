@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(256) few_kernel(EmbedGradArgs a, int slices, i
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n, V = a.vocab, D = a.channels;
   for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 256) {
     const int t = i < n ? a.tokens[i] : -1;
-    tok[i] = t < V ? t : -1;
+    tok[i] = t >= 0 && t < V ? t : -1;  // -1 for all padding: differences below stay inside 32 bits
   }
   if (threadIdx.x < 4) named[threadIdx.x] = 0u;
   __syncthreads();

@@ -12,7 +12,7 @@ if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
 from paper_1611_09482_amd import ops  # noqa: E402
-from test_gpu_operators import F32, TYPES, check_rows, randn  # noqa: E402
+from test_gpu_operators import F32, TYPES, U, check_rows, ints, plain_embed_grad, randn  # noqa: E402
 
 
 # ---- 8-bit rows ----
@@ -111,3 +111,18 @@ def test_embed_grad_tasks_past_one_launch():
     del tok
     torch.cuda.empty_cache()
     assert torch.equal(got, count[:, None] * row)
+
+
+@pytest.mark.parametrize("n,V", [(5, 9), (300, 9), (300, 5000), (512, 70000), (513, 9), (1024, 5000), (3000, 700), (20000, 700)])
+def test_padding_at_the_ends_of_32_bits(n, V):
+    """The largest and smallest tokens are padding like any other, in every form of the gradient."""
+    tok = ints(n, 0, V, n)
+    far = torch.tensor([-2 ** 31, -2 ** 31 + 1, 2 ** 31 - 1, 2 ** 31 - 16, V, -1], dtype=torch.int32, device="cuda")
+    tok[::2] = far.repeat(n)[:n][::2]
+    grad = randn(V, n, 72)
+    want, mag, count = plain_embed_grad(grad, tok, V, 1.0)
+    got = ops.embed_grad(grad, tok, V, out=torch.full((V, 72), 9.0, device="cuda"))
+    assert bool(((got.double() - want).abs() <= (count[:, None] + 4) * U * mag).all()) and bool((got[count == 0] == 0).all())
+    rows = ops.embed(got, tok)
+    inside = (tok >= 0) & (tok < V)
+    assert torch.equal(rows, torch.where(inside[:, None], got[torch.where(inside, tok, 0).long()], 0.0))
