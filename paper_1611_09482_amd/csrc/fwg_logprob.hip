@@ -612,8 +612,13 @@ template <typename T, bool TOP> hipError_t run(const LogProbArgs &a, bool in_par
   }
   if (a.vocab <= batch) {
     const dim3 grid((unsigned)((a.rows + kWaves - 1) / kWaves));
-    if (a.vocab <= batch_of<T>(1)) hipLaunchKernelGGL((rows_kernel<T, TOP, 1>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((rows_kernel<T, TOP, 4>), grid, block, 0, s, a);
+    if constexpr (batch_of<T>(1) > kShort) {  // float32 rows of one batch are short rows
+      if (a.vocab <= batch_of<T>(1)) {
+        hipLaunchKernelGGL((rows_kernel<T, TOP, 1>), grid, block, 0, s, a);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((rows_kernel<T, TOP, 4>), grid, block, 0, s, a);
     return hipGetLastError();
   }
   const int parts = in_parts ? parts_of(a.rows, a.vocab, batch) : 1;

@@ -149,14 +149,6 @@ __device__ __forceinline__ float wave_sum(float s) {
   s += dpp_f<0x140>(s);
   return (mfd::lane_f(s, 0) + mfd::lane_f(s, 16)) + (mfd::lane_f(s, 32) + mfd::lane_f(s, 48));
 }
-__device__ __forceinline__ int wave_min(int m) {
-  m = min(m, dpp_i<0xB1>(m));
-  m = min(m, dpp_i<0x4E>(m));
-  m = min(m, dpp_i<0x141>(m));
-  m = min(m, dpp_i<0x140>(m));
-  return min(min(__builtin_amdgcn_readlane(m, 0), __builtin_amdgcn_readlane(m, 16)),
-             min(__builtin_amdgcn_readlane(m, 32), __builtin_amdgcn_readlane(m, 48)));
-}
 
 }  // namespace opd
 }  // namespace fwg

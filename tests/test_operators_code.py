@@ -60,3 +60,11 @@ def test_lanes_of_the_sort_see_each_others_places(tmp_path):
     ir = device_ir(os.path.join(B.CSRC, "fwg_embed.hip"), str(tmp_path / "embed.ll"))
     body = re.search(r"define [^\n]*scatter_kernel.*?\n}", ir, re.S).group(0)
     assert 'syncscope("wavefront")' in body
+
+
+def test_every_kernel_of_log_probs_is_reached(tmp_path):
+    """Rows of one float32 batch are short rows, so the kernel that takes one batch a wave is there for bf16 only."""
+    ir = device_ir(os.path.join(B.CSRC, "fwg_logprob.hip"), str(tmp_path / "logprob.ll"))
+    names = set(re.findall(r"define [^\n]*@(\S*rows_kernelI\S*?)\(", ir))
+    batches = sorted((n[n.index("rows_kernelI") + 12], re.search(r"Li(\d+)E", n).group(1)) for n in names)
+    assert batches == [("f", "4"), ("f", "4"), ("t", "1"), ("t", "1"), ("t", "4"), ("t", "4")], names
