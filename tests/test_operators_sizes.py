@@ -50,3 +50,21 @@ def test_rows_and_tables(n):
     assert ops._table("table", small, small.get_device()) == (B.FWG_F32, 7, 2, 2)
     with pytest.raises(ValueError):
         ops._table("table", small.view(1, 7, 2), small.get_device())
+
+
+LIMIT = 1 << 29  # of vocabularies and outputs, as include/fwg.h says
+
+
+@pytest.mark.parametrize("size,code", [(LIMIT, B.FWG_OK), (LIMIT + 1, B.FWG_EUNSUPPORTED)])
+def test_limits_of_vocabularies_and_outputs(lib, size, code):
+    """No rows: what passes the checks does nothing."""
+    import ctypes
+    at, n = 1 << 30, ctypes.c_size_t(0)
+    f32 = B.FWG_F32
+    assert lib.fwg_embed(f32, f32, 0, size, 4, at, 4, at, 1.0, at, 4, None) == code
+    assert lib.fwg_embed_grad_workspace(5, size, 4, ctypes.byref(n)) == code
+    assert lib.fwg_matmul_quant(f32, 0, size, 4, at, 4, at, at, 4, at, None, at, size, None, 0, None) == code
+    assert lib.fwg_matmul_quant_workspace(5, size, 4, ctypes.byref(n)) == code
+    assert lib.fwg_log_probs(f32, 0, size, at, size, at, 0, at, at, at, None, None, None, 0, None) == code
+    assert lib.fwg_log_probs_workspace(f32, 5, size, 4, ctypes.byref(n)) == code
+    assert lib.fwg_log_probs_grad(f32, 0, size, at, size, at, at, at, at, at, at, size, None) == code
