@@ -12,7 +12,8 @@ if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
 from paper_1611_09482_amd import ops  # noqa: E402
-from test_gpu_operators import F32, TYPES, U, check_rows, ints, plain_embed_grad, randn  # noqa: E402
+from test_gpu_operators import (BF16, F32, TYPES, U, bytes_, check_matmul, check_rows, ints, odd_view,  # noqa: E402
+                                plain_embed_grad, randn)
 
 
 # ---- 8-bit rows ----
@@ -126,3 +127,105 @@ def test_padding_at_the_ends_of_32_bits(n, V):
     rows = ops.embed(got, tok)
     inside = (tok >= 0) & (tok < V)
     assert torch.equal(rows, torch.where(inside[:, None], got[torch.where(inside, tok, 0).long()], 0.0))
+
+
+# ---- kernels that only large sizes reach ----
+
+@pytest.mark.parametrize("M,N,K", [(3001, 4203, 400), (3001, 4203, 1024), (3001, 4096, 656), (4099, 8193, 272)])
+def test_matmul_quant_large_tiles_over_k(M, N, K):
+    """Rows on 16 bytes in 256 x 256 tiles: several stages of k, the last one whole or ragged, one tile or several for a
+    block.  K ends inside a piece of 16 bytes where rows are longer than it."""
+    x, w, b = bytes_(1, M, K), bytes_(2, N, K), randn(3, N)
+    check_matmul(x, w, b, 4, BF16)
+    check_matmul(x[:, :K - 7], w[:, :K - 7], None, 4, F32)
+
+
+@pytest.mark.parametrize("M", [1, 5, 16])
+@pytest.mark.parametrize("K", [64, 2048, 2176, 4096, 4500, 6148])
+def test_matmul_quant_few_rows_many_outputs(M, K):
+    """Two tiles of outputs for a block; k ends before, at and after what the sixteen waves take in one and two turns."""
+    N = 8205
+    x, w, b = bytes_(M, M, K + 1), bytes_(K, N, K + 1), randn(3, N)
+    check_matmul(x[:, :K].contiguous(), w[:, :K].contiguous(), b, 4, F32)      # words
+    check_matmul(x, w, None, 4, BF16)                                          # any byte, k one longer
+    check_matmul(odd_view(x[:, :K - 1], 3), odd_view(w[:, :K - 1]), b, 4, F32)
+
+
+@pytest.mark.parametrize("M", [17, 31, 32, 33, 64])
+@pytest.mark.parametrize("K", [2176, 4097, 6149])
+def test_matmul_quant_rows_at_any_byte(M, K):
+    """Random bytes through the shifted loads, where several turns of k are in flight."""
+    x, w = bytes_(M, M, K), bytes_(K, 515, K)
+    check_matmul(odd_view(x), odd_view(w, 2), randn(3, 515), 4, F32)
+    check_matmul(odd_view(x, 3), w, None, 4, BF16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels", [31, 1031, 2048])
+def test_embed_past_the_caches(channels, dtype):
+    """Outputs of 192 MB and more have a store of their own: the same values, nothing beside the rows."""
+    n, V = (200 << 20) // (channels * dtype.itemsize), 301
+    table, tok = randn(channels, V, channels).to(dtype), ints(2, -2, V + 2, n)
+    inside = (tok >= 0) & (tok < V)
+    wide = torch.full((n, channels + 3), 7.0, dtype=dtype, device="cuda")
+    got = ops.embed(table, tok, scale=3.25, out=wide[:, 1:1 + channels])
+    want = ((table.float() * 3.25).to(dtype))[torch.where(inside, tok, 0).long()]
+    want[~inside] = 0
+    assert torch.equal(got, want) and bool((wide[:, 0] == 7).all()) and bool((wide[:, 1 + channels:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels", [300, 900, 2048, 3001, 5001, 9001, 20001])
+def test_norm_quant_past_the_caches(channels, dtype):
+    """Outputs of 192 MB and more: the bits of smaller calls, whose rows are compared in 64 bits."""
+    n = (200 << 20) // (channels * (3 + dtype.itemsize)) + 1
+    x, r, gain = randn(1, n, channels).to(dtype), (2 * randn(2, n, channels)).to(dtype), 1 + 0.1 * randn(3, channels)
+    got = ops.norm_quant(x, gain, residual=r, values=True)
+    for i in range(0, n, n // 5):
+        part = slice(i, min(n, i + n // 5))
+        for a, b in zip(got, ops.norm_quant(x[part], gain, residual=r[part], values=True)):
+            assert torch.equal(a[part], b)
+    h = x[-9:].double() + r[-9:].double()
+    check_rows(h / torch.sqrt((h * h).mean(-1, keepdim=True) + 1e-6) * gain.double(), got.q[-9:], got.scale[-9:])
+
+
+# ---- more rows than one launch takes ----
+
+MANY = (1 << 23) + 5  # of up to 256 elements: two launches, the second of five rows
+
+
+def test_embed_of_many_rows():
+    table, tok = randn(1, 9, 3), ints(2, -1, 10, MANY)
+    inside = (tok >= 0) & (tok < 9)
+    got = ops.embed(table, tok, scale=0.5)
+    assert torch.equal(got, torch.where(inside[:, None], (table * 0.5)[torch.where(inside, tok, 0).long()], 0.0))
+
+
+def halves(call, *tensors):
+    """The results of a call on the first rows and on the others, put together."""
+    cut = 1 << 22
+    first, rest = call(*(t[:cut] for t in tensors)), call(*(t[cut:] for t in tensors))
+    return [None if a is None else torch.cat([a, b]) for a, b in zip(first, rest)]
+
+
+def test_rows_of_many_rows():
+    x, r, gain = randn(1, MANY, 5), randn(2, MANY, 5), 1 + 0.1 * randn(3, 5)
+
+    def norm(x, r):
+        return ops.norm_quant(x, gain, residual=r, values=True)
+
+    for call, tensors in ((norm, (x, r)), (ops.quant_rows, (x,))):
+        for a, b in zip(call(*tensors), halves(call, *tensors)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_log_probs_of_many_rows(dtype):
+    z, tok, g, gh = randn(1, MANY, 5).to(dtype), ints(2, -1, 6, MANY), randn(3, MANY), randn(4, MANY)
+
+    def both(z, tok, g, gh):
+        s = ops.log_probs(z, tok, top=3)
+        return list(s) + [ops.log_probs_grad(z, tok, s.lse, s.entropy, g, gh)]
+
+    for a, b in zip(both(z, tok, g, gh), halves(both, z, tok, g, gh)):
+        assert torch.equal(a, b)
