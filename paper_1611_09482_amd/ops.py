@@ -79,9 +79,12 @@ def _matrix(name: str, t, device: int, out: bool = False):
 
 def _table(name: str, t, device: int):
     """_matrix() of a tensor of two dimensions whose rows are tokens."""
-    kind, vocab, width, stride = _matrix(name, t, device)
-    _flat(name, t)
-    return kind, _int32(f"{name}'s length", vocab), width, stride
+    sizes = _matrix(name, t, device)
+    if t.dim() != 2:
+        _flat(name, t)
+    if sizes[1] > _MOST:
+        _int32(f"{name}'s length", sizes[1])
+    return sizes
 
 
 def _rows(name: str, t, out: bool = False):
@@ -89,7 +92,9 @@ def _rows(name: str, t, out: bool = False):
     shape, strides = t.shape, t.stride()
     if not shape:
         raise ValueError(f"{name} has no dimensions: rows are wanted")
-    width = _int32(f"{name}'s width", shape[-1])
+    width = shape[-1]
+    if width > _MOST:
+        _int32(f"{name}'s width", width)
     if width > 1 and strides[-1] != 1:
         raise ValueError(f"{name}: the elements of a row have to be consecutive (stride {strides[-1]})")
     if len(shape) == 2:
@@ -266,7 +271,8 @@ def matmul_quant(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=No
     rows, inner, stride = _rows("x", x)
     _flat("w", w)
     outputs, winner, wstride = _rows("w", w)
-    _int32("w's length", outputs)
+    if outputs > _MOST:
+        _int32("w's length", outputs)
     if winner != inner:
         raise ValueError(f"w has {winner} inner elements: {inner} are wanted")
     shape = x.shape[:-1] + (outputs,)
