@@ -278,8 +278,9 @@ int fwg_device_status(fwg_handle *h);
  *
  *   tokens -> fwg_embed -> (a stack) -> fwg_norm_quant -> fwg_matmul_quant -> logits -> fwg_log_probs
  *
- * and, for training, fwg_log_probs_grad and fwg_embed_grad.  fwg_log_probs takes the logits of
- * fwg_teacher_forced and its like as they are.  The calls need no handle.  As above, everything is checked on
+ * and, for training, fwg_log_probs_grad and fwg_embed_grad.  The stack is the caller's own: the models of the handles
+ * above take tokens and give logits.  Those logits (fwg_teacher_forced and its like) go into fwg_log_probs as they
+ * are.  The calls need no handle.  As above, everything is checked on
  * the host before anything is enqueued, nothing is allocated and nothing waits: the work is enqueued on
  * hip_stream (a hipStream_t, NULL = default stream) of the current device, and a call may be captured into a
  * HIP graph.  A workspace holds nothing between calls; it must be 256-byte aligned and stay untouched until the
@@ -290,7 +291,8 @@ int fwg_device_status(fwg_handle *h);
  * start at any element; an input's stride may be 0 (one row repeated), an output's rows must not overlap.
  * Outputs must not overlap inputs except where a call says so.  Zero rows are a no-op.  Sums, softmax statistics
  * and norms are float32 (8-bit products: exact 32-bit integers), rounded once, to nearest even, where an output is
- * bf16, and are added up in an order that depends on the sizes only: the same call gives the same bits.
+ * bf16, and are added up in an order that the sizes (in fwg_embed_grad the tokens too) fix: the same call gives the
+ * same bits.
  * A token outside [0, vocab) is padding: it names no row and has log probability 0.  vocab and outputs go up to 2^29,
  * channels (where nothing else is said) to 2^20, rows to 2^40.
  * ------------------------------------------------------------------------- */
@@ -302,8 +304,8 @@ int fwg_embed(int32_t dtype, int32_t out_dtype, int64_t n, int32_t vocab, int32_
               void *hip_stream);
 
 /* The table's gradient: out[v] = scale * sum over i with tokens[i] = v of grad[i], for every v in [0, vocab) (rows
- * without a token become zero).  grad: [n][channels] of dtype, out: [vocab][channels] of out_dtype.  The tokens
- * are sorted and each row's positions added up in a fixed order: no atomic additions, the same bits every time.
+ * without a token become zero).  grad: [n][channels] of dtype, out: [vocab][channels] of out_dtype.  Each row's
+ * positions are added up in an order that the tokens fix: no atomic additions, the same bits every time.
  * n <= 2^30; n = 0 clears out. */
 int fwg_embed_grad_workspace(int64_t n, int32_t vocab, int32_t channels, size_t *bytes);
 int fwg_embed_grad(int32_t dtype, int32_t out_dtype, int64_t n, int32_t vocab, int32_t channels, const void *grad,

@@ -2,13 +2,13 @@
 //
 // Lookup: out[i] = scale * table[tok[i]], a zero row for tokens outside the table.  Bound by memory: a group of
 // threads takes the 16-byte pieces of a row, several rows in flight per thread.  65,521 words out of 50,001 x 2,048 bf16 in
-// 60 us (5.6 TB/s of rows named and written); 32 rows of 512 float32 take the kernel 2.4 us and the call 6.5.
+// 60 us (5.6 TB/s of rows named and written); 32 rows of 512 float32 take the kernel 2.6 us and the call 6.6.
 //
 // Gradient: dtable[v] = scale * sum over the positions i with tok[i] = v of dy[i], in float32, in a fixed order.
-// The positions are sorted by token (a stable radix sort of at most 9 bits a pass), then equal parts of the
-// sorted order are summed, each by one wave per slice of columns: a row whose positions lie inside a part is
-// finished there, also past the part's end; rows of more positions than a part has leave partial sums that a last
-// kernel adds up in the parts' order.  So the work is even however often a token comes, no sum depends on the order in
+// Few tokens are looked through without sorting (few_kernel, scan_kernel).  Else the positions are sorted by token (a
+// stable radix sort of at most 9 bits a pass), then equal parts of the sorted order are summed, each by one wave per
+// slice of columns: a row whose positions lie inside a part is finished there, also past the part's end; rows of more
+// positions than a part has leave partial sums that a last kernel adds up in the parts' order.  So the work is even however often a token comes, no sum depends on the order in
 // which blocks run, and no float is added atomically.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(1024) hist_kernel(SortArgs a) {
   for (int b = threadIdx.x; b < bins; b += 1024) a.hist[blockIdx.x * bins + b] = cnt[b];
 }
 
-// Bound by latency, not bytes: 65,521 tokens (32 blocks) in 6.6 us a pass, and 4.6 us for hist_kernel (15 to 17 us
+// Bound by latency, not bytes: 65,521 tokens (32 blocks) in 6.6 us a pass, and 4.9 us for hist_kernel (11 to 17 us
 // each with 276 MB of zeros beside them).  Up to 16,384 tokens each block counts all tokens itself instead of reading hist:
 // 10,656 tokens in 8.7 us (2.7 + 6.9 us and a launch before).
 //
@@ -272,7 +272,8 @@ __device__ __forceinline__ void expand(const u32x4 &r, float (&v)[8]) {
 
 // Bound by memory.  65,521 tokens of 50,001 words x 2,048, bf16 into float32, in 121 us (402 MB, while zeros that the
 // launches before wrote are still on their way from the caches to the memory), of 181 for the call; 10,656 tokens of 256
-// classes x 512 float32 in 6.5 us of 21.
+// classes x 512 float32 in 7 us of 21.  Padding tokens sort behind all rows, and the parts that hold them read their
+// gradients too.
 //
 // A part's sums.  Wave task = (part, slice of 64 * VEC columns).  A row belongs to the part in which its positions
 // begin, which sums it whole, past the part's end too; only rows of more than a part's positions (long) are summed part
@@ -444,7 +445,8 @@ template <typename TO> __global__ void __launch_bounds__(64 * kJoinWaves) join_k
 // Few tokens and a table too large for scan_kernel: one launch without sorting.  A wave takes a position and a slice of
 // 64 * VEC columns; the wave of a token's first position adds up all of its positions, in order.  The remaining waves
 // clear the rows that no token names, 16 each.  Every block holds the tokens in LDS.  512 tokens of 4,000 words x 256 bf16:
-// 6.4 us (the host's time for a call), sorted 20; 460 of them alike: 46 us, since one wave per slice then adds them all.
+// 6.4 us (the host's time for a call), sorted 20; 460 of them alike: 46 us, since one wave per slice then adds them all,
+// and sorted 20.  The rule goes by the number of tokens alone: how often each comes is not known before the launch.
 constexpr int kFew = 512;
 template <typename T, typename TO>
 __global__ void __launch_bounds__(256) few_kernel(EmbedGradArgs a, int slices, int sum_blocks) {

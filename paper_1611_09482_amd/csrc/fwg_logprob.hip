@@ -10,10 +10,10 @@
 // whose largest logit does not pass the list's last entry costs one comparison per lane; otherwise the elements
 // that pass it are joined with the list.
 //
-// Measured: 4,093 rows of 50,001 float32 with 8 alternatives 148 us (5.5 TB/s), bound by memory; 192,064 rows of 256 float32
-// with 4 alternatives 52 us (3.9 TB/s; 29 us and 6.8 TB/s without alternatives), bound by instructions; 16 rows of 131,072
+// Measured: 4,093 rows of 50,001 float32 with 8 alternatives 150 us (5.4 TB/s), bound by memory; 192,064 rows of 256 float32
+// with 4 alternatives 50 us (4.1 TB/s; 29 us and 6.8 TB/s without alternatives), bound by instructions; 16 rows of 131,072
 // bf16 with 20 alternatives 13 us in two launches (5 us without alternatives), bound by latency.  The gradient of 8,190
-// rows of 50,001 bf16 takes 280 us (5.9 TB/s), bound by memory.
+// rows of 50,001 bf16 takes 280 to 286 us (5.7 to 5.9 TB/s), bound by memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -1,7 +1,7 @@
 // Product of 8-bit rows with 8-bit weights: out[m][n] = (sum_k x[m][k] w[n][k]) * x_scale[m] * w_scale[n] + bias[n].
 //
-// The sum is exact: 8-bit integer products accumulated in 32 bits on the matrix cores
-// (v_mfma_i32_16x16x64_i8), the scales and the bias in float32, one rounding where the output is bf16.  Both
+// The sum is exact: 8-bit integer products accumulated in 32 bits on the matrix cores (v_mfma_i32_32x32x32_i8 in
+// tiles, v_mfma_i32_16x16x64_i8 for few rows), the scales and the bias in float32, one rounding where the output is bf16.  Both
 // operands lie with k along their rows, which is what a lane of the instruction holds (16 consecutive k of one
 // row), so no operand is transposed.  The product is taken as D[n][m] = W X^T: a lane then holds four
 // consecutive outputs of one row and stores them together.
@@ -64,8 +64,9 @@ __device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K) {
 // while the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows (v_mfma_i32_32x32x32_i8).  A stage's rows
 // are 128 bytes; the 16-byte pieces of row r lie permuted by (r >> 1) & 7, so that the 32 rows that an instruction
 // reads at one k spread over the banks.  ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without
-// passing through registers; else they pass through registers, which takes them at any address.  TO = int: sums of a
-// part of k go to the workspace as they are.
+// passing through registers; else they pass through registers, which takes them at any address but waits for a stage's
+// memory before the products of the stage at hand (4,000 x 8,000 x 1,001 in 60 us, the products alone 31).  TO = int:
+// sums of a part of k go to the workspace as they are.
 constexpr int HK = 128;
 template <int T> struct Tile {
   static constexpr int kWaves = T / 32, kThreads = 64 * kWaves, kWM = T / 2, kJ = kWM / 32;

@@ -6,8 +6,8 @@
 // between, is read once and written once.  All of it is float32; h is rounded once where x's type is bf16.
 //
 // Bound by memory: 16,381 rows of 4,096 bf16 with residual, new residual, 8-bit rows and values (9 bytes an element, 604 MB)
-// in 101 us (6.0 TB/s).  64 rows take the kernel 3.9 us and the call 8.1.  A row is one wave's up to 1,024 elements, else
-// four waves' (sixteen's beyond 4,096): as few threads as hold it in 16 registers each, or 32 at the widest rows.
+// in 103 to 105 us (5.8 TB/s).  64 rows take the kernel 4.6 us and the call 8.2.  A row is one wave's up to 1,024 elements,
+// else four waves' (sixteen's beyond 4,096): as few threads as hold it in 16 registers each, or 32 at the widest rows.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

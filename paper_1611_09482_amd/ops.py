@@ -7,7 +7,8 @@ dimensions as long as their rows lie evenly apart (views of consecutive rows, ev
 inputs); elements of a row are consecutive.  Nothing is copied to make an argument fit: what does not fit is
 refused (TypeError, ValueError; sizes that the library refuses raise FwgError).  `out` takes the results' tensors
 of an earlier call, so that a loop allocates nothing but the workspaces that some calls take from torch's
-allocator.  The calls are no part of torch's autograd: the gradients are calls of their own.
+allocator.  The calls are no part of torch's autograd, whether or not a tensor asks for gradients: results have no
+graph, and the gradients (embed_grad, log_probs_grad) are calls of their own.
 """
 from __future__ import annotations
 
@@ -171,7 +172,7 @@ def _bytes(call: str, *sizes) -> int:
 def embed(table, tokens, scale: float = 1.0, out=None):
     """scale * table[tokens].  table: float32 or bfloat16 [vocab][channels]; tokens: int32, any shape, contiguous;
     a token outside [0, vocab) is padding and gives a zero row.  out: [*tokens.shape][channels], float32 or bfloat16
-    (default: of the table's type)."""
+    (default: of the table's type).  No part of autograd: the table's gradient is embed_grad()'s."""
     dev = _device()
     kind, vocab, channels, stride = _table("table", table, dev)
     n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
@@ -241,7 +242,8 @@ def norm_quant(x, gain=None, residual=None, eps: float = 1e-6, values: bool = Fa
     """h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain; y's rows in 8 bits as in quant_rows.  x, residual:
     float32 or bfloat16 [..., channels]; gain: float32 [channels].  Results: q, scale, `summed` (h, rounded to x's
     type; with a residual only) and, where values is true, `values` (q * scale in bfloat16).  out: a NormQuant or
-    the four tensors (None: not wanted); out's `summed` may be x or residual itself."""
+    the four tensors (None: not wanted); out's `summed` may be x or residual itself.  No part of autograd: rounding to
+    8 bits has no gradient."""
     dev = _device()
     kind, rows, width, stride = _matrix("x", x, dev)
     shape, dtype = x.shape, x.dtype
@@ -303,7 +305,8 @@ class LogProbs(NamedTuple):
 def log_probs(logits, tokens, top: int = 0, out=None) -> LogProbs:
     """Log probabilities of tokens (int32 [...]) under logits (float32 or bfloat16 [..., vocab]), with entropy, log
     sum exp and the `top` (at most 64) most probable tokens, equal logits in the order of the tokens.  -inf masks
-    a token; a token outside [0, vocab) is padding and has log probability 0."""
+    a token; a token outside [0, vocab) is padding and has log probability 0.  No part of autograd: the logits'
+    gradient is log_probs_grad()'s."""
     dev = _device()
     kind, rows, vocab, stride = _matrix("logits", logits, dev)
     lead = logits.shape[:-1]
