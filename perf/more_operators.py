@@ -1,0 +1,342 @@
+"""The operators between a served token model's last norm and its scores, as cases whose time and outputs are measured.
+
+A case names an operator (`op`) and its sizes:
+
+  quant_mx4      rows in microscaled 4-bit floating point: blocks of 32 elements that share a power of two; the values
+                 that the 4 bits stand for come back
+  norm_mx4       residual addition and RMS norm into such rows, the row's own factor beside them; the new residual, the
+                 factor and the values that the 4 bits and the factor stand for come back
+  matmul_mx4     product of such rows with such weights, a factor per row, a bias
+  adjust_logits  logits as requests want them: penalties for tokens that came before, biases, tokens that a grammar
+                 does not allow
+
+With `own` false, `run` computes them by elementary torch operations in 32 bits; with `own` true it calls
+`paper_1611_09482_amd.ops`.
+"""
+import math
+
+import torch
+
+own = False
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+BLOCK = 32
+TINY = 2.0 ** -100  # blocks whose largest magnitude lies below this are zero in 4 bits
+
+
+def _case(name, op, **sizes):
+    return dict({"op": op}, **(dict(sizes, name=name) if name else sizes))
+
+
+def listed():
+    return [
+        # the rows of one token of 64 streams for a product in 4 bits
+        _case("quant_mx4_step", "quant_mx4", rows=64, channels=4096, dtype="bf16"),
+        # an output product's weights, once after loading or after every training step
+        _case("quant_mx4_weights", "quant_mx4", rows=32000, channels=4096, dtype="f32"),
+        # the last norm before the output product, one token of each of 64 streams
+        _case("norm_mx4_step", "norm_mx4", rows=64, channels=4096, dtype="bf16"),
+        # the same over whole sequences
+        _case("norm_mx4_batch", "norm_mx4", rows=16381, channels=4096, dtype="bf16"),
+        # logits of one token of 16 streams: the weights are read for few rows
+        _case("matmul_mx4_step", "matmul_mx4", rows=16, outputs=32000, inner=4096, dtype="f32", bias=False),
+        # the same for some hundred streams, with widths that fill no tile
+        _case("matmul_mx4_streams", "matmul_mx4", rows=333, outputs=8001, inner=4080, dtype="bf16", bias=True),
+        # logits of whole sequences
+        _case("matmul_mx4_batch", "matmul_mx4", rows=4093, outputs=32000, inner=4096, dtype="bf16", bias=True),
+        # one step of 64 streams of a class model that penalises what its last 3001 samples repeat
+        _case("adjust_classes", "adjust_logits", rows=64, vocab=256, history=3001, dtype="f32", bias=False, masked=False),
+        # one token of 16 streams with a large vocabulary
+        _case("adjust_step", "adjust_logits", rows=16, vocab=131072, history=1000, dtype="bf16", bias=False, masked=False),
+        # the same under grammars that leave some rows few words, after long histories
+        _case("adjust_grammar", "adjust_logits", rows=64, vocab=131072, history=16381, dtype="bf16", bias=True, masked=True),
+        # a large batch, odd row length
+        _case("adjust_batch", "adjust_logits", rows=512, vocab=50001, history=4001, dtype="f32", bias=True, masked=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number from lo to hi, spread over its logarithm."""
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 1)) - 1e-9)))))
+
+
+def draw(rng):
+    op = rng.choice(("quant_mx4", "norm_mx4", "matmul_mx4", "matmul_mx4", "matmul_mx4", "adjust_logits", "adjust_logits"))
+    dtype = rng.choice(("f32", "bf16"))
+    if op in ("quant_mx4", "norm_mx4"):
+        channels = _log(rng, 32, 8192)
+        channels = channels if rng.random() < 0.3 else (channels + 31) // 32 * 32
+        return _case("", op, rows=_log(rng, 1, min(32000, 67000000 // channels)), channels=channels, dtype=dtype)
+    if op == "matmul_mx4":
+        inner = _log(rng, 32, 8192)
+        inner = inner if rng.random() < 0.3 else (inner + 31) // 32 * 32
+        outputs = _log(rng, 64, 32000)
+        rows = _log(rng, 1, min(8192, 530000000000 // (inner * outputs)))
+        return _case("", op, rows=rows, outputs=outputs, inner=inner, dtype=dtype, bias=rng.random() < 0.5)
+    vocab = rng.choice((256, _log(rng, 200, 131072)))
+    return _case("", op, rows=_log(rng, 1, min(2048, 25000000 // vocab)), vocab=vocab, history=_log(rng, 1, 16381), dtype=dtype,
+                 bias=rng.random() < 0.5, masked=rng.random() < 0.5)
+
+
+def _blocks_of(channels):
+    return (channels + BLOCK - 1) // BLOCK
+
+
+def _in_blocks(v):
+    """[rows][channels] -> [rows][blocks][32], the last block filled up with zeros."""
+    rows, channels = v.shape
+    return torch.nn.functional.pad(v, (0, _blocks_of(channels) * BLOCK - channels)).view(rows, -1, BLOCK)
+
+
+def _four_bits(v):
+    """(elements, exponents) of float32 rows in blocks: the elements of the 4-bit type, as float32, and each block's
+    power of two (int32 [rows][blocks]), -127 for a block of nothing."""
+    b = _in_blocks(v)
+    top = b.abs().amax(2)
+    exponent = torch.where(top < TINY, -127, torch.frexp(top).exponent - 3)
+    a = torch.where(top[:, :, None] < TINY, 0.0, torch.ldexp(b, -exponent[:, :, None].clamp(min=-120)))
+    size = a.abs()
+    step = torch.where(size < 2, 0.5, torch.where(size < 4, 1.0, 2.0))
+    return torch.copysign((torch.round(size / step) * step).clamp(max=6), a), exponent
+
+
+def _packed(v):
+    """float32 rows as bytes: (two elements a byte, the first in the low bits; exponents + 127)."""
+    e, exponent = _four_bits(v)
+    size = e.abs()
+    code = torch.where(size < 2, size * 2, torch.where(size < 4, size + 2, size / 2 + 4)).to(torch.uint8)
+    code = (code | (e < 0).to(torch.uint8) * 8).view(v.shape[0], -1)
+    return code[:, ::2] | code[:, 1::2] << 4, (exponent + 127).to(torch.uint8)
+
+
+def _values(q, scale):
+    """float32 [rows][32 blocks] that packed rows stand for."""
+    code = torch.stack((q & 15, q >> 4), 2).view(q.shape[0], -1)
+    size = (code & 7).float()
+    size = torch.where(size < 4, size / 2, torch.where(size < 6, size - 2, 2 * size - 8))
+    e = torch.where(code > 7, -size, size).view(q.shape[0], -1, BLOCK)
+    return torch.ldexp(e, scale.int()[:, :, None] - 127).view(q.shape[0], -1)
+
+
+def _probabilities(vocab):
+    """How often each token comes: mu-law classes of quiet sound for small vocabularies, word frequencies else."""
+    v = torch.arange(vocab, device="cuda", dtype=torch.float64)
+    w = torch.exp(-(v - vocab // 2).abs() / 24) + 1e-4 if vocab <= 1024 else 1 / (v + 2.7)
+    return w / w.sum()
+
+
+def _tokens(gen, shape, vocab):
+    at = torch.cumsum(_probabilities(vocab), 0)
+    u = torch.rand(shape, generator=gen, device="cuda", dtype=torch.float64)
+    return torch.searchsorted(at, u).clamp(max=vocab - 1).to(torch.int32)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7193 * seed + 31)
+    op, dtype = case["op"], TYPES[case["dtype"]]
+
+    def randn(*shape):
+        return torch.randn(shape, generator=gen, device="cuda")
+
+    def rand(*shape):
+        return torch.rand(shape, generator=gen, device="cuda")
+
+    def empty(shape, dtype):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+    def activations(rows, channels):
+        """Some channels larger than others, rows of unlike size."""
+        return randn(rows, channels) * torch.exp(0.7 * randn(channels)) * (0.5 + 2 * rand(rows, 1))
+
+    s = {"case": case}
+    if op in ("quant_mx4", "norm_mx4"):
+        n, D = case["rows"], case["channels"]
+        packed = (empty((n, _blocks_of(D) * 16), torch.uint8), empty((n, _blocks_of(D)), torch.uint8))
+        s["x"] = (0.5 * activations(n, D)).to(dtype)
+        if op == "quant_mx4":
+            s["out"] = packed + (empty((n, D), torch.bfloat16),)
+        else:
+            s["residual"] = activations(n, D).to(dtype)
+            padding = rand(n) < 0.02  # rows between sequences
+            s["x"][padding] = 0
+            s["residual"][padding] = 0
+            s["gain"] = 1 + 0.1 * randn(D)
+            s["out"] = packed + (empty((n,), torch.float32), empty((n, D), dtype), empty((n, D), torch.bfloat16))
+    elif op == "matmul_mx4":
+        M, N, K = case["rows"], case["outputs"], case["inner"]
+        s["x"], s["x_scale"] = _packed(activations(M, K))
+        s["w"], s["w_scale"] = _packed(randn(N, K) / math.sqrt(K))
+        s["row_scale"] = 0.3 + rand(M)
+        s["bias"] = 0.1 * randn(N) if case["bias"] else None
+        s["out"] = empty((M, N), dtype)
+    else:
+        n, V, H = case["rows"], case["vocab"], case["history"]
+        s["logits"] = (2.5 * randn(n, V)).to(dtype)
+        s["tokens"] = _tokens(gen, (n, H), V)
+        # histories of unlike length behind prompts of unlike length; a few rows have none yet
+        s["lengths"] = (rand(n) * (H + 1)).to(torch.int32).clamp(max=H) * (rand(n) > 0.02).to(torch.int32)
+        s["prompts"] = (rand(n) * s["lengths"]).to(torch.int32)
+        s["repetition"] = 1 + 0.3 * rand(n)
+        s["presence"] = 0.5 * rand(n)
+        s["frequency"] = 0.2 * rand(n)
+        s["bias"] = s["allowed"] = None
+        if case["bias"]:  # one for all rows: some words more or less likely, some never
+            s["bias"] = torch.where(rand(V) < 0.01, 2 * randn(V), 0.0)
+            s["bias"][rand(V) < 0.005] = -math.inf
+        if case["masked"]:  # some rows may say anything, some a part of the words, some next to nothing
+            share = torch.tensor([2.0, 2.0, 0.6, 0.02, 0.0005], device="cuda")[(rand(n) * 5).long().clamp(max=4)]
+            # groups of 64 neighbouring words are mostly allowed together
+            near = torch.nn.functional.interpolate(rand(n, 1, (V + 63) // 64), scale_factor=64, mode="nearest")[:, 0, :V]
+            bits = torch.nn.functional.pad(0.95 * near + 0.05 * rand(n, V) < share[:, None], (0, -V % 32)).view(n, -1, 32)
+            s["allowed"] = (bits.long() << torch.arange(32, device="cuda")).sum(2).to(torch.int32)
+        s["out"] = torch.empty_like(s["logits"])
+    return s
+
+
+def _quant_mx4(s):
+    e, exponent = _four_bits(s["x"].float())
+    return torch.ldexp(e, exponent[:, :, None]).view(e.shape[0], -1)[:, :s["case"]["channels"]].to(torch.bfloat16)
+
+
+def _norm_mx4(s):
+    h = s["x"].float() + s["residual"].float()
+    e, exponent = _four_bits(h * s["gain"])
+    nothing = (exponent == -127).all(1)
+    factor = torch.where(nothing, 0.0, torch.rsqrt((h * h).mean(1) + 1e-6))
+    values = torch.ldexp(e, exponent[:, :, None]).view(e.shape[0], -1)[:, :h.shape[1]] * factor[:, None]
+    return {"summed": h.to(s["x"].dtype), "row_scale": factor, "values": values.to(torch.bfloat16)}
+
+
+def _matmul_mx4(s):
+    y = (_values(s["x"], s["x_scale"]) @ _values(s["w"], s["w_scale"]).t()) * s["row_scale"][:, None]
+    return (y if s["bias"] is None else y + s["bias"]).to(s["out"].dtype)
+
+
+def _adjust_logits(s):
+    z, t, V = s["logits"].float(), s["tokens"].long(), s["case"]["vocab"]
+    at = torch.arange(t.shape[1], device="cuda")
+    there = (at < s["lengths"][:, None]) & (t >= 0) & (t < V)
+    t = torch.where(there, t, V)
+    seen = torch.zeros((z.shape[0], V + 1), device="cuda").scatter_(1, t, 1.0)[:, :V] > 0
+    made = there & (at >= s["prompts"][:, None])
+    count = torch.zeros((z.shape[0], V + 1), device="cuda").scatter_add_(1, t, made.float())[:, :V]
+    r = s["repetition"][:, None]
+    y = torch.where(seen, torch.where(z > 0, z / r, z * r), z)
+    y = torch.where(count > 0, y - s["frequency"][:, None] * count - s["presence"][:, None], y)
+    if s["bias"] is not None:
+        y = y + s["bias"]
+    if s["allowed"] is not None:
+        v = torch.arange(V, device="cuda")
+        y = torch.where(s["allowed"][:, v >> 5] >> (v & 31) & 1 == 1, y, -math.inf)
+    return torch.where(z == -math.inf, z, y).to(s["logits"].dtype)
+
+
+def _plain(s):
+    return {"quant_mx4": _quant_mx4, "norm_mx4": _norm_mx4, "matmul_mx4": _matmul_mx4,
+            "adjust_logits": _adjust_logits}[s["case"]["op"]](s)
+
+
+def run(s):
+    if not own:
+        return _plain(s)
+    from paper_1611_09482_amd import ops
+    op, out = s["case"]["op"], s["out"]
+    if op == "quant_mx4":
+        return ops.quant_mx4(s["x"], out=out).values
+    if op == "norm_mx4":
+        r = ops.norm_mx4(s["x"], s["gain"], residual=s["residual"], eps=1e-6, out=out)
+        return {"summed": r.summed, "row_scale": r.row_scale, "values": r.values}
+    if op == "matmul_mx4":
+        return ops.matmul_mx4(s["x"], s["x_scale"], s["w"], s["w_scale"], row_scale=s["row_scale"], bias=s["bias"], out=out)
+    return ops.adjust_logits(s["logits"], s["tokens"], s["lengths"], prompts=s["prompts"], repetition=s["repetition"],
+                             presence=s["presence"], frequency=s["frequency"], bias=s["bias"], allowed=s["allowed"], out=out)
+
+
+def work(case):
+    op, es = case["op"], 4 if case["dtype"] == "f32" else 2
+    if op in ("quant_mx4", "norm_mx4"):
+        n, D = case["rows"], case["channels"]
+        b = _blocks_of(D)
+        if op == "quant_mx4":
+            return {"bytes": n * (D * (es + 2) + 17 * b), "flops": 4 * n * D}
+        return {"bytes": n * (D * (3 * es + 2) + 17 * b + 4) + 4 * D, "flops": 8 * n * D}
+    if op == "matmul_mx4":
+        M, N, b = case["rows"], case["outputs"], _blocks_of(case["inner"])
+        return {"bytes": 17 * b * (M + N) + M * N * es + 4 * (M + (N if case["bias"] else 0)),
+                "flops": 2 * M * N * case["inner"]}
+    n, V = case["rows"], case["vocab"]
+    history = n * case["history"] // 2  # lengths are spread from none to all of it
+    return {"bytes": n * V * 2 * es + 4 * history + 20 * n + (4 * V if case["bias"] else 0) +
+            (n * ((V + 31) // 32) * 4 if case["masked"] else 0), "flops": 4 * n * V + 2 * history}
+
+
+def _rows_at_once(n, per):
+    return [slice(i, min(n, i + per)) for i in range(0, n, per)]
+
+
+def _exact_blocks(v):
+    """What rows in 64 bits are in 4: every magnitude goes to the grid point between whose borders it lies."""
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device="cuda")
+    border = (grid[1:] + grid[:-1]) / 2
+    rows, channels = v.shape
+    b = torch.zeros((rows, _blocks_of(channels) * BLOCK), dtype=torch.float64, device="cuda")
+    b[:, :channels] = v
+    b = b.view(rows, -1, BLOCK)
+    top = b.abs().max(2, keepdim=True).values
+    unit = torch.exp2(torch.floor(torch.log2(torch.where(top < TINY, 1.0, top))) - 2)
+    size = b.abs() / unit
+    low, high = torch.searchsorted(border, size), torch.searchsorted(border, size, right=True)
+    place = torch.where(low == high, low, low + low % 2)  # on a border: the neighbour with an even place
+    return (torch.where(top < TINY, 0.0, torch.sign(b) * grid[place] * unit)).view(rows, -1)[:, :channels]
+
+
+def _exact_unpacked(q, scale):
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+    pairs = torch.empty(q.shape + (2,), dtype=torch.float64, device="cuda")
+    pairs[:, :, 0] = grid[(q % 16).long()]
+    pairs[:, :, 1] = grid[(q // 16).long()]
+    return pairs.view(q.shape[0], -1) * torch.exp2(scale.double() - 127).repeat_interleave(BLOCK, 1)
+
+
+def exact(case, seed):
+    """The operators' definitions in 64 bits, some rows at a time."""
+    s, op = prepare(case, seed), case["op"]
+    if op == "quant_mx4":
+        return torch.cat([_exact_blocks(s["x"][r].double()).float()
+                          for r in _rows_at_once(case["rows"], max(1, (1 << 24) // case["channels"]))])
+    if op == "norm_mx4":
+        parts = []
+        for r in _rows_at_once(case["rows"], max(1, (1 << 24) // case["channels"])):
+            h = s["x"][r].double() + s["residual"][r].double()
+            factor = 1 / torch.sqrt(h.pow(2).sum(1) / case["channels"] + 1e-6)
+            b = _exact_blocks(h * s["gain"].double())
+            factor = torch.where((b == 0).all(1), 0.0, factor)
+            parts.append((h.float(), factor, (b * factor[:, None]).float()))
+        summed, factor, values = (torch.cat(p) for p in zip(*parts))
+        return {"summed": summed, "row_scale": factor, "values": values}
+    if op == "matmul_mx4":
+        w = _exact_unpacked(s["w"], s["w_scale"])
+        x, out = _exact_unpacked(s["x"], s["x_scale"]), []
+        for r in _rows_at_once(case["rows"], 1024):
+            y = torch.matmul(x[r], w.t()) * s["row_scale"][r].double()[:, None]
+            out.append(y if s["bias"] is None else y + s["bias"].double())
+        return torch.cat(out)
+    out, V = [], case["vocab"]
+    for i in range(case["rows"]):
+        z = s["logits"][i].double()
+        n, p = int(s["lengths"][i]), int(s["prompts"][i])
+        past = s["tokens"][i, :n].long()
+        came, made = torch.bincount(past, minlength=V), torch.bincount(past[p:], minlength=V)
+        r = s["repetition"][i].double()
+        y = z.clone()
+        y[came > 0] = torch.maximum(z, torch.zeros_like(z))[came > 0] / r + torch.minimum(z, torch.zeros_like(z))[came > 0] * r
+        y -= s["frequency"][i].double() * made + s["presence"][i].double() * (made > 0)
+        if s["bias"] is not None:
+            y += s["bias"].double()
+        if s["allowed"] is not None:
+            words = s["allowed"][i].long() & 0xFFFFFFFF
+            bits = (words[:, None] // 2 ** torch.arange(32, device="cuda")).view(-1)[:V] % 2
+            y[bits == 0] = -math.inf
+        out.append(y)
+    return torch.stack(out)
