@@ -2,11 +2,11 @@
 
 A case names an operator (`op`) and its sizes:
 
-  quant_mx4      rows in microscaled 4-bit floating point: blocks of 32 elements that share a power of two; the values
+  quant_mx      rows in microscaled 4-bit floating point: blocks of 32 elements that share a power of two; the values
                  that the 4 bits stand for come back
-  norm_mx4       residual addition and RMS norm into such rows, the row's own factor beside them; the new residual, the
+  norm_mx       residual addition and RMS norm into such rows, the row's own factor beside them; the new residual, the
                  factor and the values that the 4 bits and the factor stand for come back
-  matmul_mx4     product of such rows with such weights, a factor per row, a bias
+  matmul_mx     product of such rows with such weights, a factor per row, a bias
   adjust_logits  logits as requests want them: penalties for tokens that came before, biases, tokens that a grammar
                  does not allow
 
@@ -31,19 +31,19 @@ def _case(name, op, **sizes):
 def listed():
     return [
         # the rows of one token of 64 streams for a product in 4 bits
-        _case("quant_mx4_step", "quant_mx4", rows=64, channels=4096, dtype="bf16"),
+        _case("quant_mx_step", "quant_mx", rows=64, channels=4096, dtype="bf16"),
         # an output product's weights, once after loading or after every training step
-        _case("quant_mx4_weights", "quant_mx4", rows=32000, channels=4096, dtype="f32"),
+        _case("quant_mx_weights", "quant_mx", rows=32000, channels=4096, dtype="f32"),
         # the last norm before the output product, one token of each of 64 streams
-        _case("norm_mx4_step", "norm_mx4", rows=64, channels=4096, dtype="bf16"),
+        _case("norm_mx_step", "norm_mx", rows=64, channels=4096, dtype="bf16"),
         # the same over whole sequences
-        _case("norm_mx4_batch", "norm_mx4", rows=16381, channels=4096, dtype="bf16"),
+        _case("norm_mx_batch", "norm_mx", rows=16381, channels=4096, dtype="bf16"),
         # logits of one token of 16 streams: the weights are read for few rows
-        _case("matmul_mx4_step", "matmul_mx4", rows=16, outputs=32000, inner=4096, dtype="f32", bias=False),
+        _case("matmul_mx_step", "matmul_mx", rows=16, outputs=32000, inner=4096, dtype="f32", bias=False),
         # the same for some hundred streams, with widths that fill no tile
-        _case("matmul_mx4_streams", "matmul_mx4", rows=333, outputs=8001, inner=4080, dtype="bf16", bias=True),
+        _case("matmul_mx_streams", "matmul_mx", rows=333, outputs=8001, inner=4080, dtype="bf16", bias=True),
         # logits of whole sequences
-        _case("matmul_mx4_batch", "matmul_mx4", rows=4093, outputs=32000, inner=4096, dtype="bf16", bias=True),
+        _case("matmul_mx_batch", "matmul_mx", rows=4093, outputs=32000, inner=4096, dtype="bf16", bias=True),
         # one step of 64 streams of a class model that penalises what its last 3001 samples repeat
         _case("adjust_classes", "adjust_logits", rows=64, vocab=256, history=3001, dtype="f32", bias=False, masked=False),
         # one token of 16 streams with a large vocabulary
@@ -61,13 +61,13 @@ def _log(rng, lo, hi):
 
 
 def draw(rng):
-    op = rng.choice(("quant_mx4", "norm_mx4", "matmul_mx4", "matmul_mx4", "matmul_mx4", "adjust_logits", "adjust_logits"))
+    op = rng.choice(("quant_mx", "norm_mx", "matmul_mx", "matmul_mx", "matmul_mx", "adjust_logits", "adjust_logits"))
     dtype = rng.choice(("f32", "bf16"))
-    if op in ("quant_mx4", "norm_mx4"):
+    if op in ("quant_mx", "norm_mx"):
         channels = _log(rng, 32, 8192)
         channels = channels if rng.random() < 0.3 else (channels + 31) // 32 * 32
         return _case("", op, rows=_log(rng, 1, min(32000, 67000000 // channels)), channels=channels, dtype=dtype)
-    if op == "matmul_mx4":
+    if op == "matmul_mx":
         inner = _log(rng, 32, 8192)
         inner = inner if rng.random() < 0.3 else (inner + 31) // 32 * 32
         outputs = _log(rng, 64, 32000)
@@ -150,11 +150,11 @@ def prepare(case, seed):
         return randn(rows, channels) * torch.exp(0.7 * randn(channels)) * (0.5 + 2 * rand(rows, 1))
 
     s = {"case": case}
-    if op in ("quant_mx4", "norm_mx4"):
+    if op in ("quant_mx", "norm_mx"):
         n, D = case["rows"], case["channels"]
         packed = (empty((n, _blocks_of(D) * 16), torch.uint8), empty((n, _blocks_of(D)), torch.uint8))
         s["x"] = (0.5 * activations(n, D)).to(dtype)
-        if op == "quant_mx4":
+        if op == "quant_mx":
             s["out"] = packed + (empty((n, D), torch.bfloat16),)
         else:
             s["residual"] = activations(n, D).to(dtype)
@@ -163,7 +163,7 @@ def prepare(case, seed):
             s["residual"][padding] = 0
             s["gain"] = 1 + 0.1 * randn(D)
             s["out"] = packed + (empty((n,), torch.float32), empty((n, D), dtype), empty((n, D), torch.bfloat16))
-    elif op == "matmul_mx4":
+    elif op == "matmul_mx":
         M, N, K = case["rows"], case["outputs"], case["inner"]
         s["x"], s["x_scale"] = _packed(activations(M, K))
         s["w"], s["w_scale"] = _packed(randn(N, K) / math.sqrt(K))
@@ -194,12 +194,12 @@ def prepare(case, seed):
     return s
 
 
-def _quant_mx4(s):
+def _quant_mx(s):
     e, exponent = _four_bits(s["x"].float())
     return torch.ldexp(e, exponent[:, :, None]).view(e.shape[0], -1)[:, :s["case"]["channels"]].to(torch.bfloat16)
 
 
-def _norm_mx4(s):
+def _norm_mx(s):
     h = s["x"].float() + s["residual"].float()
     e, exponent = _four_bits(h * s["gain"])
     nothing = (exponent == -127).all(1)
@@ -208,7 +208,7 @@ def _norm_mx4(s):
     return {"summed": h.to(s["x"].dtype), "row_scale": factor, "values": values.to(torch.bfloat16)}
 
 
-def _matmul_mx4(s):
+def _matmul_mx(s):
     y = (_values(s["x"], s["x_scale"]) @ _values(s["w"], s["w_scale"]).t()) * s["row_scale"][:, None]
     return (y if s["bias"] is None else y + s["bias"]).to(s["out"].dtype)
 
@@ -233,7 +233,7 @@ def _adjust_logits(s):
 
 
 def _plain(s):
-    return {"quant_mx4": _quant_mx4, "norm_mx4": _norm_mx4, "matmul_mx4": _matmul_mx4,
+    return {"quant_mx": _quant_mx, "norm_mx": _norm_mx, "matmul_mx": _matmul_mx,
             "adjust_logits": _adjust_logits}[s["case"]["op"]](s)
 
 
@@ -242,26 +242,26 @@ def run(s):
         return _plain(s)
     from paper_1611_09482_amd import ops
     op, out = s["case"]["op"], s["out"]
-    if op == "quant_mx4":
-        return ops.quant_mx4(s["x"], out=out).values
-    if op == "norm_mx4":
-        r = ops.norm_mx4(s["x"], s["gain"], residual=s["residual"], eps=1e-6, out=out)
+    if op == "quant_mx":
+        return ops.quant_mx(s["x"], out=out).values
+    if op == "norm_mx":
+        r = ops.norm_mx(s["x"], s["gain"], residual=s["residual"], eps=1e-6, out=out)
         return {"summed": r.summed, "row_scale": r.row_scale, "values": r.values}
-    if op == "matmul_mx4":
-        return ops.matmul_mx4(s["x"], s["x_scale"], s["w"], s["w_scale"], row_scale=s["row_scale"], bias=s["bias"], out=out)
+    if op == "matmul_mx":
+        return ops.matmul_mx(s["x"], s["x_scale"], s["w"], s["w_scale"], row_scale=s["row_scale"], bias=s["bias"], out=out)
     return ops.adjust_logits(s["logits"], s["tokens"], s["lengths"], prompts=s["prompts"], repetition=s["repetition"],
                              presence=s["presence"], frequency=s["frequency"], bias=s["bias"], allowed=s["allowed"], out=out)
 
 
 def work(case):
     op, es = case["op"], 4 if case["dtype"] == "f32" else 2
-    if op in ("quant_mx4", "norm_mx4"):
+    if op in ("quant_mx", "norm_mx"):
         n, D = case["rows"], case["channels"]
         b = _blocks_of(D)
-        if op == "quant_mx4":
+        if op == "quant_mx":
             return {"bytes": n * (D * (es + 2) + 17 * b), "flops": 4 * n * D}
         return {"bytes": n * (D * (3 * es + 2) + 17 * b + 4) + 4 * D, "flops": 8 * n * D}
-    if op == "matmul_mx4":
+    if op == "matmul_mx":
         M, N, b = case["rows"], case["outputs"], _blocks_of(case["inner"])
         return {"bytes": 17 * b * (M + N) + M * N * es + 4 * (M + (N if case["bias"] else 0)),
                 "flops": 2 * M * N * case["inner"]}
@@ -302,10 +302,10 @@ def _exact_unpacked(q, scale):
 def exact(case, seed):
     """The operators' definitions in 64 bits, some rows at a time."""
     s, op = prepare(case, seed), case["op"]
-    if op == "quant_mx4":
+    if op == "quant_mx":
         return torch.cat([_exact_blocks(s["x"][r].double()).float()
                           for r in _rows_at_once(case["rows"], max(1, (1 << 24) // case["channels"]))])
-    if op == "norm_mx4":
+    if op == "norm_mx":
         parts = []
         for r in _rows_at_once(case["rows"], max(1, (1 << 24) // case["channels"])):
             h = s["x"][r].double() + s["residual"][r].double()
@@ -315,7 +315,7 @@ def exact(case, seed):
             parts.append((h.float(), factor, (b * factor[:, None]).float()))
         summed, factor, values = (torch.cat(p) for p in zip(*parts))
         return {"summed": summed, "row_scale": factor, "values": values}
-    if op == "matmul_mx4":
+    if op == "matmul_mx":
         w = _exact_unpacked(s["w"], s["w_scale"])
         x, out = _exact_unpacked(s["x"], s["x_scale"]), []
         for r in _rows_at_once(case["rows"], 1024):
