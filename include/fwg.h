@@ -277,6 +277,7 @@ int fwg_device_status(fwg_handle *h);
  * Token operators: the two ends of a token model, for any vocabulary and width.
  *
  *   tokens -> fwg_embed -> (a stack) -> fwg_norm_quant -> fwg_matmul_quant -> logits -> fwg_log_probs
+ *                                       fwg_norm_mx   -> fwg_matmul_mx   -> logits -> fwg_adjust_logits -> fwg_log_probs
  *
  * and, for training, fwg_log_probs_grad and fwg_embed_grad.  The stack is the caller's own: the models of the handles
  * above take tokens and give logits.  Those logits (fwg_teacher_forced and its like) go into fwg_log_probs as they
@@ -338,6 +339,54 @@ int fwg_matmul_quant(int32_t out_dtype, int64_t rows, int32_t outputs, int32_t i
                      int64_t x_stride, const float *x_scale, const int8_t *w, int64_t w_stride, const float *w_scale,
                      const float *bias, void *out, int64_t out_stride, void *workspace, size_t ws_bytes,
                      void *hip_stream);
+
+/* Rows in microscaled 4-bit floating point (the Open Compute project's MXFP4): 32 consecutive elements share a power of
+ * two, 2^e with e = floor(log2 of the largest magnitude) - 2, and each is x / 2^e to the nearest of 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives (ties to the even code, past 6: 6).  q: two elements a byte, the first in the low bits (sign,
+ * two bits of exponent, one of fraction); scale: a byte per block, e + 127.  A row has blocks = ceil(channels / 32) blocks: 16 blocks
+ * bytes of q and as many of scale as blocks; the last block is filled up with zeros.  A block whose largest magnitude
+ * is below 2^-100 has scale and q of 0; one with a NaN or an infinity has scale 255, which stands for NaN, and q of 0.
+ * Optional output values: what the 4 bits stand for, exact in bf16.  1 <= channels <= 2^20. */
+int fwg_quant_mx(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride, uint8_t *q,
+                  int64_t q_stride, uint8_t *scale, int64_t scale_stride, uint16_t *values, int64_t values_stride,
+                  void *hip_stream);
+
+/* Residual addition, RMS norm and rows in 4 bits: h = x + residual, row_scale = 1 / sqrt(mean(h^2) + eps), q and scale of
+ * h * gain as in fwg_quant_mx: the norm's rows are row_scale[r] times what the 4 bits stand for.  row_scale is 0 for a row
+ * whose blocks are all zero, and NaN where the sum of squares is no number, passes float32's largest value, or is 0 in
+ * float32 with eps of 0 while some block is not zero.  residual NULL: none; gain (float32 [channels]) NULL: ones.  Optional outputs: summed,
+ * h rounded to dtype (may be x or residual itself), and values, row_scale times what the 4 bits stand for, in bf16.  The
+ * norm is taken of the unrounded sum.  1 <= channels <= 32768. */
+int fwg_norm_mx(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride, const void *residual,
+                 int64_t residual_stride, const float *gain, float eps, void *summed, int64_t summed_stride, uint8_t *q,
+                 int64_t q_stride, uint8_t *scale, int64_t scale_stride, float *row_scale, uint16_t *values,
+                 int64_t values_stride, void *hip_stream);
+
+/* out[m][n] = row_scale[m] * (sum over k of x[m][k] w[n][k]) + bias[n], x and w in microscaled 4 bits as fwg_quant_mx and
+ * fwg_norm_mx leave them: x [rows] and w [outputs] (PyTorch's layout) rows of `blocks` blocks each, at any address.  row_scale (float32 [rows])
+ * NULL: ones; bias (float32 [outputs]) NULL: none.  Products and sums are float32.  A block with scale 255 makes its
+ * row's (or output's) results NaN.  1 <= blocks <= 32768, rows <= 2^30. */
+int fwg_matmul_mx_workspace(int64_t rows, int32_t outputs, int32_t blocks, size_t *bytes);
+int fwg_matmul_mx(int32_t out_dtype, int64_t rows, int32_t outputs, int32_t blocks, const uint8_t *x, int64_t x_stride,
+                   const uint8_t *x_scale, int64_t x_scale_stride, const uint8_t *w, int64_t w_stride,
+                   const uint8_t *w_scale, int64_t w_scale_stride, const float *row_scale, const float *bias, void *out,
+                   int64_t out_stride, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* Logits as requests want them, per row of logits [rows][vocab] (of dtype).  tokens: int32 [rows][history], the row's
+ * prompt and what was generated after it: lengths[r] tokens (NULL: history; kept to 0 .. history), the first prompts[r] of them
+ * the prompt (NULL: 0); tokens outside [0, vocab) are padding.  With c[v] the times that v comes after the prompt:
+ *   z = z > 0 ? z / repetition[r] : z * repetition[r]    where v comes anywhere in the row's tokens,
+ *   z = z - frequency[r] * c[v] - presence[r]            where c[v] > 0,
+ *   z = z + bias[r][v],    -inf where bit v % 32 of allowed[r][v / 32] is 0.
+ * A logit of -inf stays -inf, and what is not allowed is -inf whatever it was, NaN included.  repetition, presence, frequency:
+ * float32 [rows], NULL: not applied; with all three NULL tokens are not read, and tokens may be NULL where history is
+ * 0.  bias: float32 [rows][vocab], allowed: [rows][ceil(vocab / 32)], NULL: none, a stride of 0: one row for all.  out: of
+ * the logits' dtype; may be the logits themselves (the same address and stride). */
+int fwg_adjust_logits(int32_t dtype, int64_t rows, int32_t vocab, const void *logits, int64_t logits_stride,
+                      int32_t history, const int32_t *tokens, int64_t tokens_stride, const int32_t *lengths,
+                      const int32_t *prompts, const float *repetition, const float *presence, const float *frequency,
+                      const float *bias, int64_t bias_stride, const uint32_t *allowed, int64_t allowed_stride, void *out,
+                      int64_t out_stride, void *hip_stream);
 
 /* Per row of logits [rows][vocab] (of dtype): lse = log sum exp, logp = log probability of tokens[r], entropy (in
  * nats), and the `top` most probable tokens (0 <= top <= 64, <= vocab) with their log probabilities, ordered by

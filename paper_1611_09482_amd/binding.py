@@ -22,7 +22,8 @@ EXPORTED = ["fwg_workspace_size", "fwg_create", "fwg_reset_queues", "fwg_generat
             # the token operators (ops.py)
             "fwg_embed", "fwg_embed_grad_workspace", "fwg_embed_grad", "fwg_quant_rows", "fwg_norm_quant",
             "fwg_matmul_quant_workspace", "fwg_matmul_quant", "fwg_log_probs_workspace", "fwg_log_probs",
-            "fwg_log_probs_grad"]
+            "fwg_log_probs_grad", "fwg_quant_mx", "fwg_norm_mx", "fwg_matmul_mx_workspace", "fwg_matmul_mx",
+            "fwg_adjust_logits"]
 
 
 class FwgError(RuntimeError):
@@ -90,6 +91,11 @@ def load_library(path: Optional[str] = None):
     L.fwg_log_probs_workspace.argtypes = [i32, i64, i32, i32, ctypes.POINTER(sz)]
     L.fwg_log_probs.argtypes = [i32, i64, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     L.fwg_log_probs_grad.argtypes = [i32, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.fwg_quant_mx.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.fwg_norm_mx.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp]
+    L.fwg_matmul_mx_workspace.argtypes = [i64, i32, i32, ctypes.POINTER(sz)]
+    L.fwg_matmul_mx.argtypes = [i32, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+    L.fwg_adjust_logits.argtypes = [i32, i64, i32, vp, i64, i32, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp]
     for name in ["fwg_workspace_size", "fwg_create", "fwg_reset_queues", "fwg_generate", "fwg_generate_noalloc",
                  "fwg_teacher_forced",
                  "fwg_step_forced", "fwg_teacher_forced_parallel", "fwg_prime", "fwg_generate_naive",

@@ -17,7 +17,8 @@ SOURCES = [os.path.join(CSRC, "fwg_host.cpp"), os.path.join(CSRC, "fwg_kernels.h
            os.path.join(CSRC, "fwg_chain.hip"), os.path.join(CSRC, "fwg_wide.hip"),
            os.path.join(CSRC, "fwg_ops.cpp"), os.path.join(CSRC, "fwg_embed.hip"),
            os.path.join(CSRC, "fwg_normq.hip"), os.path.join(CSRC, "fwg_matmulq.hip"),
-           os.path.join(CSRC, "fwg_logprob.hip")]
+           os.path.join(CSRC, "fwg_logprob.hip"), os.path.join(CSRC, "fwg_mx.hip"),
+           os.path.join(CSRC, "fwg_matmulmx.hip"), os.path.join(CSRC, "fwg_adjust.hip")]
 HEADERS = [os.path.join(ROOT, "include", "fwg.h"), os.path.join(CSRC, "fwg_internal.h"),
            os.path.join(CSRC, "fwg_sample.h"), os.path.join(CSRC, "fwg_valu.h"),
            os.path.join(CSRC, "fwg_wave.h"), os.path.join(CSRC, "fwg_par.h"), os.path.join(CSRC, "fwg_mfma_dev.h"),

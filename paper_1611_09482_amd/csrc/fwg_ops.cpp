@@ -106,6 +106,44 @@ int norm_impl(NormArgs a, int dtype, void *hip_stream) {
   return FWG_OK;
 }
 
+int mx_impl(MxArgs a, int dtype, bool norm, void *hip_stream) {
+  CHECK(check_type("dtype", dtype));
+  CHECK(check_size("rows", a.rows, 0, kMaxRows));
+  CHECK(check_size("channels", a.channels, 1, norm ? kNormMaxChannels : kMaxChannels));
+  const int64_t blocks = (a.channels + 31) / 32;
+  CHECK(check_stride("x_stride", a.ld_x, 0));
+  CHECK(check_stride("q_stride", a.ld_q, 16 * blocks));
+  CHECK(check_stride("scale_stride", a.ld_e, blocks));
+  if (a.residual) CHECK(check_stride("residual_stride", a.ld_r, 0));
+  if (a.summed) CHECK(check_stride("summed_stride", a.ld_s, a.channels));
+  if (a.values) CHECK(check_stride("values_stride", a.ld_v, a.channels));
+  if (norm && !(a.eps >= 0.f && std::isfinite(a.eps))) return fail(FWG_EINVAL, "eps has to be finite and not negative");
+  if (a.rows == 0) return FWG_OK;
+  CHECK(check_ptr("x", a.x, size_of(dtype)));
+  if (a.residual) CHECK(check_ptr("residual", a.residual, size_of(dtype)));
+  if (a.gain) CHECK(check_ptr("gain", a.gain, 4));
+  if (a.summed) CHECK(check_ptr("summed", a.summed, size_of(dtype)));
+  CHECK(check_ptr("q", a.q, 1));
+  CHECK(check_ptr("scale", a.scale, 1));
+  if (norm) CHECK(check_ptr("row_scale", a.row_scale, 4));
+  if (a.values) CHECK(check_ptr("values", a.values, 2));
+  const int64_t rows = a.rows, per = rows_per_launch(a.channels);
+  for (int64_t r = 0; r < rows; r += per) {
+    MxArgs b = a;
+    b.rows = rows - r < per ? rows - r : per;
+    b.x = at(a.x, r * a.ld_x, dtype);
+    b.residual = at(a.residual, r * a.ld_r, dtype);
+    b.summed = at(a.summed, r * a.ld_s, dtype);
+    b.q = a.q + r * a.ld_q;
+    b.scale = a.scale + r * a.ld_e;
+    if (norm) b.row_scale = a.row_scale + r;
+    if (a.values) b.values = a.values + r * a.ld_v;
+    CHECK(norm ? done(launch_norm_mx(b, dtype, (hipStream_t)hip_stream), "norm_mx")
+               : done(launch_quant_mx(b, dtype, (hipStream_t)hip_stream), "quant_mx"));
+  }
+  return FWG_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -210,6 +248,123 @@ int fwg_matmul_quant(int32_t out_dtype, int64_t rows, int32_t outputs, int32_t i
   CHECK(check_workspace(need, workspace, ws_bytes));
   MatmulArgs a{x, w, x_scale, w_scale, bias, out, rows, x_stride, w_stride, out_stride, outputs, inner, (unsigned char *)workspace};
   return done(launch_matmul_quant(a, out_dtype, (hipStream_t)hip_stream), "matmul_quant");
+}
+
+int fwg_quant_mx(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride, uint8_t *q,
+                  int64_t q_stride, uint8_t *scale, int64_t scale_stride, uint16_t *values, int64_t values_stride,
+                  void *hip_stream) {
+  MxArgs a{};
+  a.x = x;
+  a.q = q;
+  a.scale = scale;
+  a.values = values;
+  a.rows = rows;
+  a.ld_x = x_stride;
+  a.ld_q = q_stride;
+  a.ld_e = scale_stride;
+  a.ld_v = values_stride;
+  a.channels = channels;
+  return mx_impl(a, dtype, false, hip_stream);
+}
+
+int fwg_norm_mx(int32_t dtype, int64_t rows, int32_t channels, const void *x, int64_t x_stride, const void *residual,
+                 int64_t residual_stride, const float *gain, float eps, void *summed, int64_t summed_stride, uint8_t *q,
+                 int64_t q_stride, uint8_t *scale, int64_t scale_stride, float *row_scale, uint16_t *values,
+                 int64_t values_stride, void *hip_stream) {
+  MxArgs a{x,    residual, gain,     summed,          q,             scale,    row_scale,    values,
+            rows, x_stride, residual_stride, summed_stride, q_stride, scale_stride, values_stride, channels, eps};
+  return mx_impl(a, dtype, true, hip_stream);
+}
+
+int fwg_matmul_mx_workspace(int64_t rows, int32_t outputs, int32_t blocks, size_t *bytes) {
+  if (!bytes) return fail(FWG_EINVAL, "bytes is NULL");
+  CHECK(check_size("rows", rows, 0, kMaxTokens));
+  CHECK(check_size("outputs", outputs, 1, kMaxVocab));
+  CHECK(check_size("blocks", blocks, 1, kMxMaxBlocks));
+  *bytes = rows ? matmul_mx_bytes(rows, outputs, blocks) : 0;
+  return FWG_OK;
+}
+
+int fwg_matmul_mx(int32_t out_dtype, int64_t rows, int32_t outputs, int32_t blocks, const uint8_t *x, int64_t x_stride,
+                   const uint8_t *x_scale, int64_t x_scale_stride, const uint8_t *w, int64_t w_stride,
+                   const uint8_t *w_scale, int64_t w_scale_stride, const float *row_scale, const float *bias, void *out,
+                   int64_t out_stride, void *workspace, size_t ws_bytes, void *hip_stream) {
+  CHECK(check_type("out_dtype", out_dtype));
+  size_t need = 0;
+  CHECK(fwg_matmul_mx_workspace(rows, outputs, blocks, &need));
+  CHECK(check_stride("x_stride", x_stride, 0));
+  CHECK(check_stride("x_scale_stride", x_scale_stride, 0));
+  CHECK(check_stride("w_stride", w_stride, 0));
+  CHECK(check_stride("w_scale_stride", w_scale_stride, 0));
+  CHECK(check_stride("out_stride", out_stride, outputs));
+  if (rows == 0) return FWG_OK;
+  CHECK(check_ptr("x", x, 1));
+  CHECK(check_ptr("x_scale", x_scale, 1));
+  CHECK(check_ptr("w", w, 1));
+  CHECK(check_ptr("w_scale", w_scale, 1));
+  if (row_scale) CHECK(check_ptr("row_scale", row_scale, 4));
+  if (bias) CHECK(check_ptr("bias", bias, 4));
+  CHECK(check_ptr("out", out, size_of(out_dtype)));
+  CHECK(check_workspace(need, workspace, ws_bytes));
+  MatmulMxArgs a{x,    x_scale,  w,              w_scale,  row_scale,      bias,       out,     rows,
+                  x_stride, x_scale_stride, w_stride, w_scale_stride, out_stride, outputs, blocks, (unsigned char *)workspace};
+  return done(launch_matmul_mx(a, out_dtype, (hipStream_t)hip_stream), "matmul_mx");
+}
+
+int fwg_adjust_logits(int32_t dtype, int64_t rows, int32_t vocab, const void *logits, int64_t logits_stride,
+                      int32_t history, const int32_t *tokens, int64_t tokens_stride, const int32_t *lengths,
+                      const int32_t *prompts, const float *repetition, const float *presence, const float *frequency,
+                      const float *bias, int64_t bias_stride, const uint32_t *allowed, int64_t allowed_stride, void *out,
+                      int64_t out_stride, void *hip_stream) {
+  CHECK(check_type("dtype", dtype));
+  CHECK(check_size("rows", rows, 0, kMaxRows));
+  CHECK(check_size("vocab", vocab, 1, kMaxVocab));
+  CHECK(check_size("history", history, 0, INT32_MAX));
+  CHECK(check_stride("logits_stride", logits_stride, 0));
+  CHECK(check_stride("out_stride", out_stride, vocab));
+  // without penalties the history says nothing
+  const bool penalties = repetition || presence || frequency;
+  const bool past = penalties && history > 0;
+  if (past) CHECK(check_stride("tokens_stride", tokens_stride, 0));
+  if (bias) CHECK(check_stride("bias_stride", bias_stride, 0));
+  if (allowed) CHECK(check_stride("allowed_stride", allowed_stride, 0));
+  if (rows == 0) return FWG_OK;
+  CHECK(check_ptr("logits", logits, size_of(dtype)));
+  CHECK(check_ptr("out", out, size_of(dtype)));
+  if (past) CHECK(check_ptr("tokens", tokens, 4));
+  if (lengths) CHECK(check_ptr("lengths", lengths, 4));
+  if (prompts) CHECK(check_ptr("prompts", prompts, 4));
+  if (repetition) CHECK(check_ptr("repetition", repetition, 4));
+  if (presence) CHECK(check_ptr("presence", presence, 4));
+  if (frequency) CHECK(check_ptr("frequency", frequency, 4));
+  if (bias) CHECK(check_ptr("bias", bias, 4));
+  if (allowed) CHECK(check_ptr("allowed", allowed, 4));
+  const int64_t per = rows_per_launch(vocab);
+  for (int64_t r = 0; r < rows; r += per) {
+    AdjustArgs a{};
+    a.logits = at(logits, r * logits_stride, dtype);
+    a.out = at(out, r * out_stride, dtype);
+    a.rows = rows - r < per ? rows - r : per;
+    a.vocab = vocab;
+    a.ld = logits_stride;
+    a.ld_o = out_stride;
+    if (past) {
+      a.tokens = tokens + r * tokens_stride;
+      a.ld_t = tokens_stride;
+      a.history = history;
+      a.lengths = lengths ? lengths + r : nullptr;
+      a.prompts = prompts ? prompts + r : nullptr;
+      a.repetition = repetition ? repetition + r : nullptr;
+      a.presence = presence ? presence + r : nullptr;
+      a.frequency = frequency ? frequency + r : nullptr;
+    }
+    a.bias = bias ? bias + r * bias_stride : nullptr;
+    a.ld_b = bias_stride;
+    a.allowed = allowed ? allowed + r * allowed_stride : nullptr;
+    a.ld_a = allowed_stride;
+    CHECK(done(launch_adjust(a, dtype, (hipStream_t)hip_stream), "adjust_logits"));
+  }
+  return FWG_OK;
 }
 
 int fwg_log_probs_workspace(int32_t dtype, int64_t rows, int32_t vocab, int32_t top, size_t *bytes) {

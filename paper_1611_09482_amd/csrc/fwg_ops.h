@@ -1,5 +1,5 @@
-// Launchers of the token operators (embedding, 8-bit norm and product, log probabilities), called by
-// their C entries in fwg_ops.cpp, which check every argument first.  Element types: FWG_F32 or
+// Launchers of the token operators (embedding, norms and products in 8 and 4 bits, adjusted logits, log
+// probabilities), called by their C entries in fwg_ops.cpp, which check every argument first.  Element types: FWG_F32 or
 // FWG_BF16; strides in elements.  Not part of the public ABI.
 #pragma once
 
@@ -65,6 +65,43 @@ struct MatmulArgs {
 };
 size_t matmul_quant_bytes(int64_t rows, int outputs, int inner);
 hipError_t launch_matmul_quant(const MatmulArgs &a, int out_dtype, hipStream_t s);
+
+constexpr int kMxMaxBlocks = 32768;  // of a product's rows: 2^20 elements
+struct MxArgs {
+  const void *x, *residual;  // residual may be NULL
+  const float *gain;         // NULL: ones
+  void *summed;              // may be NULL
+  uint8_t *q, *scale;
+  float *row_scale;
+  uint16_t *values;          // may be NULL
+  int64_t rows, ld_x, ld_r, ld_s, ld_q, ld_e, ld_v;
+  int channels;
+  float eps;
+};
+hipError_t launch_quant_mx(const MxArgs &a, int dtype, hipStream_t s);  // x, q, scale and values only
+hipError_t launch_norm_mx(const MxArgs &a, int dtype, hipStream_t s);
+
+struct MatmulMxArgs {
+  const uint8_t *x, *x_scale, *w, *w_scale;
+  const float *row_scale, *bias;  // each may be NULL
+  void *out;
+  int64_t M, ld_x, ld_ex, ld_w, ld_ew, ld_o;
+  int N, blocks;
+  unsigned char *ws;
+};
+size_t matmul_mx_bytes(int64_t rows, int outputs, int blocks);
+hipError_t launch_matmul_mx(const MatmulMxArgs &a, int out_dtype, hipStream_t s);
+
+struct AdjustArgs {
+  const void *logits;
+  const int32_t *tokens, *lengths, *prompts;           // each may be NULL
+  const float *repetition, *presence, *frequency, *bias;  // each may be NULL
+  const uint32_t *allowed;                             // may be NULL
+  void *out;
+  int64_t rows, ld, ld_t, ld_b, ld_a, ld_o;
+  int vocab, history;
+};
+hipError_t launch_adjust(const AdjustArgs &a, int dtype, hipStream_t s);
 
 constexpr int kMaxTop = 64;  // alternatives are held one per lane
 struct LogProbArgs {

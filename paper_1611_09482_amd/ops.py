@@ -1,5 +1,5 @@
-"""The token operators of libfwg.so (include/fwg.h) on torch tensors: embedding lookup and its gradient, 8-bit
-rows with or without RMS norm, the 8-bit product, log probabilities and their gradient.
+"""The token operators of libfwg.so (include/fwg.h) on torch tensors: embedding lookup and its gradient, rows in 8 or 4
+bits with or without RMS norm and their products, logits as requests want them, log probabilities and their gradient.
 
 Argument marshalling only, as in binding.py: every call checks its tensors, enqueues the library's kernels on the
 current stream of the current device and returns without waiting.  Matrices may have any number of leading
@@ -289,6 +289,163 @@ def matmul_quant(x, x_scale, w, w_scale, bias=None, dtype=torch.bfloat16, out=No
                                 _vector("w_scale", w_scale, outputs, torch.float32, dev),
                                 None if bias is None else _vector("bias", bias, outputs, torch.float32, dev),
                                 out.data_ptr(), ostride, None if ws is None else ws.data_ptr(), need, _stream(dev)))
+    return out
+
+
+class MxRows(NamedTuple):
+    """Rows in microscaled 4 bits (two elements a byte, [..., 16 blocks], and a scale byte per block of 32, [..., blocks]), and
+    the values that they stand for in bfloat16 (None where they were not asked for)."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    values: Optional[torch.Tensor]
+
+
+class NormMx(NamedTuple):
+    """Rows of a norm in microscaled 4 bits with a factor each, the residual stream after the addition, and the values that
+    the rows with their factors stand for in bfloat16 (None where they were not asked for)."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    row_scale: torch.Tensor
+    summed: Optional[torch.Tensor]
+    values: Optional[torch.Tensor]
+
+
+def _mx_shapes(shape):
+    blocks = (shape[-1] + 31) // 32
+    return shape[:-1] + (16 * blocks,), shape[:-1] + (blocks,)
+
+
+def quant_mx(x, values: bool = False, out=None) -> MxRows:
+    """Rows in microscaled 4-bit floating point: each block of 32 elements shares a power of two, its elements are rounded to
+    0, 0.5, 1, 1.5, 2, 3, 4 or 6 times that.  x: float32 or bfloat16 [..., channels]; the last block is filled up with zeros.
+    For weights [outputs][inner] these are matmul_mx's w and w_scale.  out: an MxRows or the three tensors (None: no
+    values).  No part of autograd: rounding to 4 bits has no gradient."""
+    dev = _device()
+    kind, rows, width, stride = _matrix("x", x, dev)
+    qshape, eshape = _mx_shapes(x.shape)
+    if out is None:
+        out = MxRows(torch.empty(qshape, dtype=torch.uint8, device=x.device),
+                      torch.empty(eshape, dtype=torch.uint8, device=x.device),
+                      torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
+    q, scale, vals = out
+    qp, qstride = _like("out.q", q, torch.uint8, qshape, dev, True)
+    ep, estride = _like("out.scale", scale, torch.uint8, eshape, dev, True)
+    vp, vstride = (None, 0) if vals is None else _like("out.values", vals, torch.bfloat16, x.shape, dev, True)
+    _check(_library().fwg_quant_mx(kind, rows, width, x.data_ptr(), stride, qp, qstride, ep, estride, vp, vstride,
+                                    _stream(dev)))
+    return out if isinstance(out, MxRows) else MxRows(*out)
+
+
+def norm_mx(x, gain=None, residual=None, eps: float = 1e-6, values: bool = False, out=None) -> NormMx:
+    """h = x + residual; row_scale = 1 / sqrt(mean(h^2) + eps); rows of h * gain in microscaled 4 bits as in quant_mx: the
+    norm is row_scale times what they stand for, and matmul_mx takes the three together.  x, residual: float32 or bfloat16
+    [..., channels]; gain: float32 [channels].  Results: q, scale, row_scale, `summed` (h, rounded to x's type; with a
+    residual only) and, where values is true, `values` (the norm in bfloat16).  out: a NormMx or the five tensors (None: not
+    wanted); out's `summed` may be x or residual itself.  No part of autograd: rounding to 4 bits has no gradient."""
+    dev = _device()
+    kind, rows, width, stride = _matrix("x", x, dev)
+    shape, dtype = x.shape, x.dtype
+    rp, rstride = (None, 0) if residual is None else _like("residual", residual, dtype, shape, dev)
+    qshape, eshape = _mx_shapes(shape)
+    if out is None:
+        out = NormMx(torch.empty(qshape, dtype=torch.uint8, device=x.device),
+                      torch.empty(eshape, dtype=torch.uint8, device=x.device),
+                      torch.empty(shape[:-1], dtype=torch.float32, device=x.device),
+                      None if residual is None else torch.empty(shape, dtype=dtype, device=x.device),
+                      torch.empty(shape, dtype=torch.bfloat16, device=x.device) if values else None)
+    q, scale, row_scale, summed, vals = out
+    qp, qstride = _like("out.q", q, torch.uint8, qshape, dev, True)
+    ep, estride = _like("out.scale", scale, torch.uint8, eshape, dev, True)
+    sp, sstride = (None, 0) if summed is None else _like("out.summed", summed, dtype, shape, dev, True)
+    vp, vstride = (None, 0) if vals is None else _like("out.values", vals, torch.bfloat16, shape, dev, True)
+    gp = None if gain is None else _vector("gain", gain, width, torch.float32, dev)
+    _check(_library().fwg_norm_mx(kind, rows, width, x.data_ptr(), stride, rp, rstride, gp, eps, sp, sstride, qp, qstride,
+                                   ep, estride, _vector("out.row_scale", row_scale, rows, torch.float32, dev), vp, vstride,
+                                   _stream(dev)))
+    return out if isinstance(out, NormMx) else NormMx(*out)
+
+
+def matmul_mx(x, x_scale, w, w_scale, row_scale=None, bias=None, dtype=torch.bfloat16, out=None):
+    """row_scale[:, None] * (x @ w.T) + bias of rows in microscaled 4 bits (quant_mx, norm_mx), products and sums in float32.
+    x: uint8 [..., 16 blocks] with x_scale uint8 [..., blocks]; w: uint8 [outputs][16 blocks] with w_scale uint8
+    [outputs][blocks]; row_scale: float32 [...]; bias: float32 [outputs].  out: [..., outputs] of dtype (float32 or bfloat16)."""
+    dev = _device()
+    _typed("x", x, torch.uint8, dev)
+    _typed("w", w, torch.uint8, dev)
+    rows, width, stride = _rows("x", x)
+    _flat("w", w)
+    outputs, wwidth, wstride = _rows("w", w)
+    if outputs > _MOST:
+        _int32("w's length", outputs)
+    if wwidth != width:
+        raise ValueError(f"w has rows of {wwidth} bytes: {width} are wanted")
+    blocks = width // 16
+    if width % 16:
+        raise ValueError(f"x has rows of {width} bytes: a block is 16 bytes")
+    lead = x.shape[:-1]
+    xe, xestride = _like("x_scale", x_scale, torch.uint8, lead + (blocks,), dev)
+    we, westride = _like("w_scale", w_scale, torch.uint8, (outputs, blocks), dev)
+    shape = lead + (outputs,)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+    okind, _, _, ostride = _matrix("out", out, dev, True)
+    _shaped("out", out, shape)
+    need = _bytes("fwg_matmul_mx_workspace", rows, outputs, blocks)
+    ws = _workspace(need)
+    _check(_library().fwg_matmul_mx(okind, rows, outputs, blocks, x.data_ptr(), stride, xe, xestride, w.data_ptr(), wstride,
+                              we, westride,
+                              None if row_scale is None else _vector("row_scale", row_scale, rows, torch.float32, dev),
+                              None if bias is None else _vector("bias", bias, outputs, torch.float32, dev),
+                              out.data_ptr(), ostride, None if ws is None else ws.data_ptr(), need, _stream(dev)))
+    return out
+
+
+def _per_row(name: str, t, rows: int, dtype, dev: int):
+    return None if t is None else _vector(name, t, rows, dtype, dev)
+
+
+def _one_or_each(name: str, t, dtype, lead, width: int, dev: int):
+    """(address, stride) of one row for all (stride 0) or a row for each."""
+    if t is None:
+        return None, 0
+    if isinstance(t, torch.Tensor) and t.dim() == 1:
+        return _vector(name, t, width, dtype, dev), 0
+    return _like(name, t, dtype, lead + (width,), dev)
+
+
+def adjust_logits(logits, tokens=None, lengths=None, prompts=None, repetition=None, presence=None, frequency=None, bias=None,
+                  allowed=None, out=None):
+    """Logits (float32 or bfloat16 [..., vocab]) as requests want them.  tokens: int32 [..., history], each row's prompt and
+    what was generated after it, lengths int32 [...] (default: all) tokens, the first prompts int32 [...] (default: none) of
+    them the prompt; tokens outside [0, vocab) are padding.  Each of float32 [...]: repetition divides positive and
+    multiplies other logits of tokens that came anywhere before, frequency (times how often) and presence are subtracted from
+    those of tokens that were generated.  Then bias (float32 [vocab] or [..., vocab]) is added, and where a bit of allowed
+    (int32 [words] or [..., words], words = ceil(vocab / 32), token v in bit v % 32 of word v // 32) is 0 the logit becomes
+    -inf.  -inf stays -inf.  out: of the logits' shape and type; may be the logits themselves.  No part of autograd."""
+    dev = _device()
+    kind, rows, vocab, stride = _matrix("logits", logits, dev)
+    lead = logits.shape[:-1]
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    op, ostride = _like("out", out, logits.dtype, logits.shape, dev, True)
+    if tokens is None:
+        if not (lengths is None and prompts is None and repetition is None and presence is None and frequency is None):
+            raise ValueError("lengths, prompts, repetition, presence or frequency are given without tokens")
+        tp, tstride, history = None, 0, 0
+    else:
+        if not isinstance(tokens, torch.Tensor) or tokens.dim() == 0:
+            raise TypeError("tokens is not a tensor of rows")
+        history = tokens.shape[-1]
+        tp, tstride = _like("tokens", tokens, torch.int32, lead + (history,), dev)
+        if history > _MOST:
+            _int32("the history's length", history)
+    bp, bstride = _one_or_each("bias", bias, torch.float32, lead, vocab, dev)
+    ap, astride = _one_or_each("allowed", allowed, torch.int32, lead, (vocab + 31) // 32, dev)
+    _check(_library().fwg_adjust_logits(
+        kind, rows, vocab, logits.data_ptr(), stride, history, tp, tstride, _per_row("lengths", lengths, rows, torch.int32, dev),
+        _per_row("prompts", prompts, rows, torch.int32, dev), _per_row("repetition", repetition, rows, torch.float32, dev),
+        _per_row("presence", presence, rows, torch.float32, dev), _per_row("frequency", frequency, rows, torch.float32, dev),
+        bp, bstride, ap, astride, op, ostride, _stream(dev)))
     return out
 
 

@@ -1,0 +1,695 @@
+"""The 4-bit operators and adjust_logits on the GPU against plain evaluations in 64 bits.
+
+Bars, with u = 2^-24 (float32) and a final rounding to bf16 of 2^-8 of the value where the output is bf16:
+  * 4-bit rows and their scales: equal, bit by bit: the elements come from the input by one rounding.  In the norm's rows
+    h = x + residual and h * gain are one float32 operation each, which torch's float32 does alike;
+  * values: exact in bf16; of a norm one product with row_scale and one rounding;
+  * row_scale: at most 32 squares in a row per thread, then 6 + 16 additions over lanes and waves, halved by the root, and
+    four more roundings: (54 / 2 + 4) u < 2e-6; 4e-6 is allowed;
+  * product: where all scales lie within a factor of 4 every product is a multiple of 1/16 and every sum below 2^24 of
+    those (36 * 4 * 16 inner < 2^24 up to 7,281 elements), so float32 holds it exactly, whatever the order: the sums
+    are equal, and row_scale, bias and output round once each: 3 u of the magnitudes.  Else (inner + 4) u of the sum of the magnitudes;
+  * adjusted logits: one rounding each of the division or product, frequency * count, two subtractions and the bias: 5 u of the
+    sum of the magnitudes; -inf exactly where it belongs.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_1611_09482_amd import ops  # noqa: E402
+
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = [F32, BF16]
+INF = math.inf
+GRID = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(seed, *shape):
+    return torch.randn(shape, generator=gen(seed), device="cuda")
+
+
+def rand(seed, *shape):
+    return torch.rand(shape, generator=gen(seed), device="cuda")
+
+
+def ints(seed, lo, hi, *shape, dtype=torch.int32):
+    return torch.randint(lo, hi, shape, generator=gen(seed), device="cuda", dtype=dtype)
+
+
+def odd_view(t, off=1, more=3):
+    """The same values as rows of a wider array that start at an odd element."""
+    wide = torch.zeros(t.shape[:-1] + (t.shape[-1] + more,), dtype=t.dtype, device=t.device)
+    v = wide[..., off:off + t.shape[-1]]
+    v.copy_(t)
+    return v
+
+
+# ---- rows in 4 bits ----
+
+def plain_rows(v):
+    """(codes [rows][32 blocks], scale bytes [rows][blocks], values [rows][channels] in 64 bits) of float32 rows, by distance
+    to the grid: the nearest point, of two as near the one with the even code."""
+    rows, channels = v.shape
+    blocks = (channels + 31) // 32
+    b = torch.zeros((rows, blocks * 32), dtype=torch.float64, device=v.device)
+    b[:, :channels] = v.double()
+    b = b.view(rows, blocks, 32)
+    top = b.abs().amax(2)
+    nan = ~torch.isfinite(b).all(2)
+    zero = (top < 2.0 ** -100) & ~nan
+    byte = torch.where(nan, 255, torch.where(zero, 0, torch.frexp(torch.where(nan | zero, 1.0, top)).exponent + 124))
+    unit = torch.exp2(torch.where(nan | zero, 0.0, byte.double() - 127))
+    size = torch.where((nan | zero)[:, :, None], 0.0, b.abs() / unit[:, :, None])
+    grid = torch.tensor(GRID, dtype=torch.float64, device=v.device)
+    far = (size[..., None] - grid).abs()
+    best = far.amin(3, keepdim=True)
+    at = torch.arange(8, device=v.device)
+    # of the nearest points the first with an even code, else the first
+    code = torch.where(far == best, at + 8 * (at % 2), 99).amin(3) % 8
+    sign = torch.signbit(b) & ~(nan | zero)[:, :, None]
+    value = torch.where(sign, -grid[code], grid[code]) * unit[:, :, None]
+    value = torch.where(nan[:, :, None], math.nan, value).view(rows, -1)[:, :channels]
+    return (code + 8 * sign).view(rows, -1), byte, value
+
+
+def pack(code):
+    return (code[:, ::2] | code[:, 1::2] << 4).to(torch.uint8)
+
+
+def same(a, b):
+    a, b = a.double(), b.double()
+    return bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())
+
+
+def check_rows(x):
+    """x: a matrix of any strides."""
+    code, byte, value = plain_rows(x.float())
+    r = ops.quant_mx(x, values=True)
+    assert r.q.shape == (x.shape[0], code.shape[1] // 2) and r.scale.shape == byte.shape and r.values.shape == x.shape
+    assert torch.equal(r.scale.long(), byte.long())
+    assert torch.equal(r.q, pack(code))
+    assert same(r.values, value)
+    return r
+
+
+def hard_rows(seed, rows, channels, dtype):
+    """Rows with what a block can meet: ties of every kind, largest elements at both ends of a power of two, blocks of nothing,
+    of tiny and of huge numbers, NaN and infinities."""
+    x = randn(seed, rows, channels) * torch.exp2(6 * randn(seed + 1, rows, 1).round())
+    blocks = [x[:, i:i + 32] for i in range(0, channels, 32)]
+    middles = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, -0.25, -5.0, 4.0, 7.75], device="cuda")
+    for i, b in enumerate(blocks):
+        for r in range(rows):
+            kind = (i + 5 * r) % 11
+            if kind == 0:
+                b[r] = middles[ints(seed + i, 0, 12, b.shape[1]).long()] * 2.0 ** (i % 7 - 3)
+            elif kind == 1:
+                b[r] = 0.0
+            elif kind == 2:
+                b[r] *= 2.0 ** -60
+            elif kind == 3:
+                b[r] = b[r].sign() * 2.0 ** -100
+                b[r, 0] = 2.0 ** -101
+            elif kind == 4:
+                b[r] = b[r].clamp(-1, 1) * 2.0 ** -101
+            elif kind == 5:
+                b[r] = b[r].sign() * torch.finfo(dtype).max
+            elif kind == 6 and (i + r) % 3 == 0:
+                b[r, -1] = math.nan
+            elif kind == 7 and (i + r) % 3 == 0:
+                b[r, 0] = -INF
+            elif kind == 8:
+                b[r] = -0.0
+    return x.to(dtype)
+
+
+CHANNELS = [1, 2, 7, 31, 32, 33, 63, 64, 100, 255, 256, 512, 513, 1000, 1024, 2047, 2049, 4096, 5000, 8200, 16384, 32768]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels", CHANNELS)
+def test_quant(channels, dtype):
+    for rows in (1, 2, 9):
+        x = hard_rows(channels + rows, rows, channels, dtype)
+        check_rows(x)
+        check_rows(odd_view(x))
+        check_rows(x[:1].expand(3, channels))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quant_every_rounding(dtype):
+    """All multiples of 1/64 below 7.9 and their neighbours in float32, in blocks whose scale is 1."""
+    v = torch.arange(0, 504, device="cuda") / 64.0
+    v = torch.cat([v, torch.nextafter(v, v + 1), torch.nextafter(v, v - 1)])
+    v = torch.cat([v, -v])
+    x = torch.zeros((v.numel(), 32), device="cuda")
+    x[:, 5] = v
+    x[:, 31] = 4.0
+    r = check_rows(x.to(dtype))
+    assert bool((r.scale == 127).all())
+
+
+def test_quant_wide_and_many_rows():
+    x = randn(3, 3, (1 << 20) - 5).to(BF16)
+    check_rows(x)
+    check_rows(randn(4, 70001, 40))
+    r = ops.quant_mx(randn(5, 4, 6, 50).to(BF16))
+    assert r.q.shape == (4, 6, 32) and r.scale.shape == (4, 6, 2) and r.values is None
+    assert ops.quant_mx(randn(5, 0, 50)).q.shape == (0, 32)
+
+
+def test_quant_into_views():
+    """Outputs whose rows start at odd bytes; what lies between the rows stays."""
+    x = randn(6, 9, 77)
+    want = ops.quant_mx(x, values=True)
+    q = torch.full((9, 60), 7, dtype=torch.uint8, device="cuda")
+    e = torch.full((9, 8), 7, dtype=torch.uint8, device="cuda")
+    v = torch.full((9, 90), 7, dtype=BF16, device="cuda")
+    ops.quant_mx(x, out=(q[:, 5:53], e[:, 3:6], v[:, 1:78]))
+    assert torch.equal(q[:, 5:53], want.q) and torch.equal(e[:, 3:6], want.scale) and torch.equal(v[:, 1:78], want.values)
+    for t, lo, hi in ((q, 5, 53), (e, 3, 6), (v, 1, 78)):
+        assert bool((t[:, :lo] == 7).all()) and bool((t[:, hi:] == 7).all())
+
+
+def test_quant_rows_past_four_gigabytes():
+    x = torch.empty((1100, 1 << 21), dtype=BF16, device="cuda")[:, :500]
+    x.copy_(randn(7, 1100, 500))
+    check_rows(x)
+
+
+# ---- norm ----
+
+def check_norm(x, gain, residual, eps, summed=True):
+    h = x.float() if residual is None else x.float() + residual.float()
+    hg = h if gain is None else h * gain
+    code, byte, value = plain_rows(hg)
+    ss = h.double().square().mean(1)
+    factor = 1 / torch.sqrt(ss + eps)
+    nothing = (byte == 0).all(1)
+    bad = ~torch.isfinite(h.double().square().sum(1).float()) | ((h.double().square().sum(1) < 2.0 ** -149) & (eps == 0))
+    factor = torch.where(torch.isnan(ss) | (bad & ~nothing), math.nan, torch.where(nothing, 0.0, factor))
+    r = ops.norm_mx(x, gain, residual=residual, eps=eps, values=True)
+    assert torch.equal(r.scale.long(), byte.long()) and torch.equal(r.q, pack(code))
+    near = ((r.row_scale.double() - factor).abs() <= 4e-6 * factor) | (torch.isnan(r.row_scale) & torch.isnan(factor))
+    assert bool(near.all()), (r.row_scale[~near], factor[~near])
+    want = value * factor[:, None]
+    got = r.values.double()
+    ok = ((got - want).abs() <= (2.0 ** -8 + 5e-6) * want.abs() + 2.0 ** -134) | (torch.isnan(got) & torch.isnan(want))
+    assert bool(ok.all()), (got[~ok][:4], want[~ok][:4])
+    if residual is None:
+        assert r.summed is None
+    else:
+        assert same(r.summed, h.to(x.dtype))
+    return r
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels", CHANNELS)
+def test_norm(channels, dtype):
+    gain = 1 + 0.2 * randn(1, channels)
+    for rows in (1, 5, 130) if channels <= 2049 else (1, 3):
+        x, res = randn(2, rows, channels).to(dtype), (3 * randn(3, rows, channels)).to(dtype)
+        check_norm(x, gain, res, 1e-6)
+        check_norm(odd_view(x), None, None, 1e-5)
+        check_norm(odd_view(x), gain, odd_view(res, 2), 0.0)
+        check_norm(x, gain, res[:1].expand(rows, channels), 1.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("channels", [40, 600, 5000])
+def test_norm_edges(channels, dtype):
+    x = randn(4, 10, channels).to(dtype)
+    x[0] = 0.0                       # a padding token's row
+    x[1] = 2.0 ** -110               # nothing in 4 bits
+    x[2, channels // 2] = math.nan
+    x[3, 0] = INF
+    x[4] = x[4].sign() * torch.finfo(dtype).max  # the sum of squares passes float32
+    x[5] *= 2.0 ** -60               # squares of denormal size: zero with eps, something without
+    x[6, 32:] = 0.0                  # blocks of nothing beside one
+    x[7] *= 2.0 ** 50
+    gain = 1 + 0.2 * randn(5, channels)
+    check_norm(x, gain, None, 1e-6)
+    check_norm(x[[0, 1, 2, 3, 4, 6, 7, 8, 9]], None, None, 0.0)
+    gain[channels - 1] = math.nan
+    r = check_norm(x[6:], gain, None, 1e-6)
+    assert bool((r.scale[:, -1] == 255).all())
+
+
+def test_norm_in_place_and_views():
+    x, res, gain = randn(6, 8, 100).to(BF16), randn(7, 8, 100).to(BF16), 1 + 0.1 * randn(8, 100)
+    want = ops.norm_mx(x, gain, residual=res, values=True)
+    for which in (0, 1):
+        a, b = x.clone(), res.clone()
+        stream = (a, b)[which]
+        got = ops.norm_mx(a, gain, residual=b, out=want._replace(summed=stream))
+        assert torch.equal(stream, (x.float() + res.float()).to(BF16)) and torch.equal(got.q, want.q)
+    row_scale = torch.empty(8, device="cuda")
+    got = ops.norm_mx(x, gain, residual=res, out=(want.q.clone(), want.scale.clone(), row_scale, None, None))
+    assert got.summed is None and got.values is None and torch.equal(row_scale, want.row_scale)
+    three = ops.norm_mx(x.view(2, 4, 100), gain, residual=res.view(2, 4, 100))
+    assert three.q.shape == (2, 4, 64) and three.row_scale.shape == (2, 4) and torch.equal(three.q.view(8, 64), want.q)
+
+
+# ---- product ----
+
+def unpacked(q, scale):
+    """Values in 64 bits of packed rows; NaN where the scale is."""
+    grid = torch.tensor(GRID + [-g for g in GRID], dtype=torch.float64, device="cuda")
+    code = torch.stack((q & 15, q >> 4), -1).view(q.shape[0], -1)
+    unit = torch.where(scale == 255, math.nan, torch.exp2(scale.double() - 127))
+    return grid[code.long()] * unit.repeat_interleave(32, 1)
+
+
+def random_rows(seed, rows, blocks, spread):
+    """Any codes, scales within 2^spread around 1."""
+    q = ints(seed, 0, 256, rows, 16 * blocks, dtype=torch.uint8)
+    return q, ints(seed + 1, 127 - spread // 2, 128 + (spread - spread // 2), rows, blocks, dtype=torch.uint8)
+
+
+def check_product(x, ex, w, ew, dtype, row_scale=None, bias=None, exact=True, out=None):
+    a, b = unpacked(x, ex), unpacked(w, ew)
+    s, mag = a @ b.t(), a.abs() @ b.abs().t()
+    want, bar = s, (0.0 if exact else (a.shape[1] + 1) * U) * mag
+    if row_scale is not None:
+        want, bar = want * row_scale.double()[:, None], bar * row_scale.double().abs()[:, None] + U * (want * row_scale.double()[:, None]).abs()
+    if bias is not None:
+        want, bar = want + bias.double(), bar + U * (want.abs() + bias.double().abs())
+    bar = bar + (2.0 ** -8 if dtype == BF16 else U) * want.abs() * 1.001 + 1e-37
+    got = ops.matmul_mx(x, ex, w, ew, row_scale=row_scale, bias=bias, dtype=dtype, out=out)
+    assert got.dtype == dtype and got.shape == (x.shape[0], w.shape[0])
+    d = got.double()
+    ok = ((d - want).abs() <= bar) | (torch.isnan(d) & torch.isnan(want))
+    assert bool(ok.all()), (int((~ok).sum()), d[~ok][:4], want[~ok][:4], (~ok).nonzero()[:4])
+    return got
+
+
+SHAPES = [(1, 1, 1), (1, 5, 2), (3, 33, 3), (16, 64, 4), (17, 40, 7), (32, 32, 8), (33, 257, 9), (64, 100, 16), (65, 130, 5),
+          (100, 1000, 15), (128, 128, 128), (129, 255, 17), (200, 513, 63), (255, 300, 12), (256, 256, 24), (257, 257, 31),
+          (300, 8001, 33), (520, 700, 127), (1, 8192, 227), (2, 20000, 10), (5, 1003, 128), (16, 8200, 64), (31, 4096, 130),
+          (40, 12000, 12), (1000, 2000, 20), (1500, 9000, 6), (3001, 1999, 9), (4100, 4100, 3), (12000, 70, 4)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,blocks", SHAPES)
+def test_product(M, N, blocks, dtype):
+    x, ex = random_rows(M, M, blocks, 2)
+    w, ew = random_rows(N + 7, N, blocks, 2)
+    check_product(x, ex, w, ew, dtype)
+    check_product(x, ex, w, ew, dtype, row_scale=randn(3, M), bias=10 * randn(4, N))
+
+
+@pytest.mark.parametrize("M,N,blocks", [(1, 300, 40), (20, 500, 33), (70, 200, 65), (300, 600, 128), (2050, 2100, 36)])
+def test_product_wide_scales(M, N, blocks):
+    """Scales 2^30 apart."""
+    x, ex = random_rows(1, M, blocks, 30)
+    w, ew = random_rows(2, N, blocks, 30)
+    check_product(x, ex, w, ew, F32, exact=False)
+    check_product(x, ex, w, ew, BF16, row_scale=rand(3, M), bias=randn(4, N), exact=False)
+
+
+@pytest.mark.parametrize("M,N,blocks", [(1, 77, 5), (15, 700, 40), (30, 130, 66), (90, 8300, 9), (400, 515, 31),
+                                        (2050, 2100, 36)])
+def test_product_views(M, N, blocks):
+    """Rows at odd bytes, scales and outputs in wider arrays, one row for all; what lies between the outputs' rows stays."""
+    x, ex = random_rows(5, M, blocks, 2)
+    w, ew = random_rows(6, N, blocks, 2)
+    bias, f = randn(7, N), randn(8, M)
+    for ax, aw in ((1, 3), (4, 8), (16, 16), (2, 16)):
+        vx, vw = odd_view(x, ax, 48), odd_view(w, aw, 32)
+        for dtype in TYPES:
+            wide = torch.full((M, N + 9), 7.0, dtype=dtype, device="cuda")
+            check_product(vx, odd_view(ex, 1, 2), vw, odd_view(ew, 2, 7), dtype, f, bias, out=wide[:, 3:3 + N])
+            assert bool((wide[:, :3] == 7).all()) and bool((wide[:, 3 + N:] == 7).all())
+    check_product(x[:1].expand(M, -1), ex[:1].expand(M, -1), w, ew, F32)
+    check_product(x, ex, w[:1].expand(N, -1), ew[:1].expand(N, -1), F32)
+    check_product(x, ex[:1].expand(M, -1), w, ew[:1].expand(N, -1), F32)
+
+
+@pytest.mark.parametrize("M,N,blocks", [(3, 70, 4), (40, 300, 9), (300, 400, 20), (2050, 2100, 5)])
+def test_product_nan_blocks_and_zero_blocks(M, N, blocks):
+    x, ex = random_rows(9, M, blocks, 2)
+    w, ew = random_rows(10, N, blocks, 2)
+    x[0], ex[0] = 0, 0            # a row of nothing
+    w[1, :16], ew[1, 0] = 0, 0
+    ex[M - 1, blocks - 1], x[M - 1, -16:] = 255, 0  # as quant_mx leaves a block with a NaN
+    ew[N // 2, 0], w[N // 2, :16] = 255, 0
+    got = check_product(x, ex, w, ew, F32)
+    assert bool(torch.isnan(got[M - 1]).all()) and bool(torch.isnan(got[:, N // 2]).all())
+    assert int(torch.isnan(got).sum()) == M + N - 1
+    f = torch.zeros(M, device="cuda")
+    got = ops.matmul_mx(x[:2], ex[:2], w[:8], ew[:8], row_scale=f[:2], dtype=F32)
+    assert not bool(got[:, :1].any())
+
+
+def test_product_rows_past_four_gigabytes():
+    """Operands and outputs whose rows lie further apart than 32 bits reach."""
+    blocks = 6
+    x, ex = random_rows(11, 1100, blocks, 2)
+    w, ew = random_rows(12, 1200, blocks, 2)
+    far = torch.empty((1200, 1 << 22), dtype=torch.uint8, device="cuda")
+    vx, vw = far[:1100, :96], far[:, 128:224]
+    vx.copy_(x)
+    vw.copy_(w)
+    out = torch.empty((1100, 1 << 21), dtype=BF16, device="cuda")[:, 7:1207]
+    check_product(vx, ex, vw, ew, BF16, out=out)
+    check_product(vx[:9], ex[:9], vw, ew, F32)
+    check_product(vx[::137], ex[::137], vw[::150], ew[::150], F32)
+
+
+def test_product_many_outputs_and_rows():
+    x, ex = random_rows(13, 3, 1, 2)
+    w, ew = random_rows(14, 300001, 1, 2)
+    check_product(x, ex, w, ew, F32)
+    check_product(w, ew, x, ex, BF16)
+    got = ops.matmul_mx(x.view(1, 3, 16), ex.view(1, 3, 1), w[:50], ew[:50], dtype=F32)
+    assert got.shape == (1, 3, 50)
+    assert ops.matmul_mx(x[:0], ex[:0], w, ew).shape == (0, 300001)
+
+
+# ---- adjusted logits ----
+
+def plain_adjust(z, tokens=None, lengths=None, prompts=None, repetition=None, presence=None, frequency=None, bias=None,
+                 allowed=None):
+    """(adjusted logits, bars) in 64 bits, a row at a time."""
+    V, out, bars = z.shape[1], [], []
+    for r in range(z.shape[0]):
+        row = z[r].double()
+        came = made = torch.zeros(V, dtype=torch.long, device="cuda")
+        if tokens is not None:
+            n = tokens.shape[1] if lengths is None else min(max(int(lengths[r]), 0), tokens.shape[1])
+            t = tokens[r, :n].long()
+            p = 0 if prompts is None else min(max(int(prompts[r]), 0), n)
+            came = torch.bincount(t[(t >= 0) & (t < V)], minlength=V)
+            t = t[p:]
+            made = torch.bincount(t[(t >= 0) & (t < V)], minlength=V)
+        y = row.clone()
+        if repetition is not None:
+            k = repetition[r].double()
+            y = torch.where(came > 0, torch.where(row > 0, row / k, row * k), row)
+        mag = y.abs()
+        if frequency is not None:
+            f = frequency[r].double() * made
+            y, mag = y - f, mag + 2 * f.abs()
+        if presence is not None:
+            p = torch.where(made > 0, presence[r].double(), 0.0)
+            y, mag = y - p, mag + p.abs()
+        if bias is not None:
+            b = (bias if bias.dim() == 1 else bias[r]).double()
+            y, mag = y + b, mag + b.abs()
+        if allowed is not None:
+            words = (allowed if allowed.dim() == 1 else allowed[r]).long()
+            v = torch.arange(V, device="cuda")
+            y = torch.where(words[v // 32] >> v % 32 & 1 == 1, y, -INF)
+        out.append(torch.where(row == -INF, -INF, y))
+        bars.append(5 * U * mag)
+    return torch.stack(out), torch.stack(bars)
+
+
+def check_adjust(z, out=None, **kw):
+    want, bar = plain_adjust(z, **kw)
+    bar = bar + (2.0 ** -8 * (want.abs() + bar) if z.dtype == BF16 else 0.0)
+    limit = torch.finfo(z.dtype)
+    want = torch.where(want.abs() > limit.max * (1 + limit.eps / 4), torch.sign(want) * INF, want)  # past the type's numbers
+    got = ops.adjust_logits(z, out=out, **kw)
+    assert got.dtype == z.dtype and got.shape == z.shape
+    d = got.double()
+    ok = (d == want) | (torch.isnan(d) & torch.isnan(want)) | ((d - want).abs() <= bar)
+    assert bool(ok.all()), (int((~ok).sum()), d[~ok][:4], want[~ok][:4], (~ok).nonzero()[:4])
+    return got
+
+
+def request(seed, rows, V, H, shared=False):
+    """Everything at once: histories of unlike lengths behind prompts, padding tokens, biases, grammars."""
+    bias = torch.where(rand(seed, *(V,) if shared else (rows, V)) < 0.1, 3.0, 0.0)
+    bias[..., V // 2] = -INF
+    words = (V + 31) // 32
+    allowed = ints(seed + 1, -2 ** 31, 2 ** 31 - 1, *((words,) if shared else (rows, words)))
+    if not shared:
+        allowed[0] = -1
+        allowed[rows - 1] = 0  # nothing is left
+    lengths = ints(seed + 3, -1, H + 3, rows)
+    return dict(tokens=ints(seed + 2, -2, V + 2, rows, H), lengths=lengths,
+                prompts=(rand(seed + 4, rows) * (H + 1)).int() - 1, repetition=0.5 + rand(seed + 5, rows),
+                presence=randn(seed + 6, rows), frequency=0.3 * randn(seed + 7, rows), bias=bias, allowed=allowed)
+
+
+VOCABS = [1, 2, 7, 8, 31, 32, 33, 100, 256, 257, 1000, 2048, 4097, 8191, 8192, 8193, 16385, 50001]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", VOCABS)
+def test_adjust(V, dtype):
+    for rows, H, shared in [(1, 1, False), (5, 40, True), (3, 1000, False), (4, 5000, True)]:
+        z = (3 * randn(V + rows, rows, V)).to(dtype)
+        kw = request(V, rows, V, H, shared)
+        check_adjust(z, **kw)
+        check_adjust(odd_view(z), **kw)
+        mine = z.clone()
+        check_adjust(z, out=mine, **kw)
+        again = z.clone()
+        assert torch.equal(ops.adjust_logits(again, out=again, **kw).float().nan_to_num(), mine.float().nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [40, 9000])
+@pytest.mark.parametrize("names", ["", "repetition", "presence", "frequency", "bias", "allowed", "repetition allowed",
+                                   "frequency bias", "tokens", "presence lengths", "repetition frequency prompts",
+                                   "allowed bias"])
+def test_adjust_parts(names, V, dtype):
+    """Each request alone and some pairs, in place too."""
+    names = set(names.split())
+    kw = request(77, 6, V, 300)
+    if names & {"repetition", "presence", "frequency"}:
+        names.add("tokens")
+    kw = {k: v for k, v in kw.items() if k in names}
+    z = (3 * randn(V, 6, V)).to(dtype)
+    want = check_adjust(z, **kw)
+    mine = odd_view(z)
+    assert ops.adjust_logits(mine, out=mine, **kw) is mine and torch.equal(mine, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [70, 10000])
+def test_adjust_edges(V, dtype):
+    z = (3 * randn(V, 8, V)).to(dtype)
+    z[0] = -INF
+    z[1, ::2] = -INF
+    z[2, 5] = math.nan
+    z[2, 6] = math.nan
+    z[3, 7] = INF
+    z[4] = torch.finfo(dtype).min
+    z[5] = 0.0
+    z[5, ::2] = -0.0
+    z[6] = torch.finfo(dtype).max / 4
+    kw = request(5, 8, V, 600)
+    kw["bias"][2, 6] = 0.0
+    kw["allowed"][2] = -1
+    kw["allowed"][2, 0] = -1 - (1 << 5)  # token 5, a NaN, is not allowed
+    kw["allowed"][3] = -1
+    got = check_adjust(z, **kw)
+    assert got[2, 5] == -INF and math.isnan(got[2, 6])
+    mine = z.clone()
+    ops.adjust_logits(mine, out=mine, **kw)
+    assert same(mine, got)
+
+
+@pytest.mark.parametrize("V,H", [(256, 200001), (50001, 70000), (300, 16384), (3, 4097), (131072, 33000)])
+def test_adjust_long_histories(V, H):
+    """Long histories, some of one token over and over, as silence is."""
+    z = randn(V, 3, V)
+    tokens = ints(H, 0, V, 3, H)
+    tokens[1] = V // 3
+    tokens[2, H // 2:] = V - 1
+    kw = dict(tokens=tokens, prompts=torch.tensor([H // 2, 5, 0], dtype=torch.int32, device="cuda"),
+              repetition=1 + rand(1, 3), presence=rand(2, 3), frequency=rand(3, 3))
+    check_adjust(z, **kw)
+
+
+def test_adjust_many_rows_and_shapes():
+    z = randn(1, 3000, 256)
+    kw = request(2, 3000, 256, 20)
+    got = check_adjust(z[:200], **{k: v[:200] for k, v in kw.items()})
+    full = ops.adjust_logits(z, **kw)
+    assert torch.equal(full[:200], got)
+    shaped = ops.adjust_logits(z.view(30, 100, 256), **{k: v.view((30, 100) + v.shape[1:]) for k, v in kw.items()})
+    assert torch.equal(shaped.view(3000, 256), full)
+    check_adjust(z[::99], **{k: v[::99].contiguous() if v.dim() == 1 else v[::99] for k, v in kw.items()})
+    one = {k: v[:1] for k, v in kw.items()}
+    check_adjust(z[:1].expand(5, 256), **{k: v.expand((5,) + v.shape[1:]) if v.dim() > 1 else v.expand(5).contiguous()
+                                          for k, v in one.items()})
+    assert ops.adjust_logits(z[:0], tokens=kw["tokens"][:0], presence=kw["presence"][:0]).shape == (0, 256)
+    check_adjust(z[:4], tokens=kw["tokens"][:4, :0], presence=kw["presence"][:4])
+
+
+def test_adjust_rows_past_four_gigabytes():
+    V = 5000
+    far = torch.empty((600, 1 << 22), dtype=BF16, device="cuda")
+    z, out = far[:, :V], far[:, 100000:100000 + V]
+    z.copy_(2 * randn(7, 600, V))
+    kw = request(8, 600, V, 50)
+    last = {k: v[590:] for k, v in kw.items()}
+    want, bar = plain_adjust(z[590:], **last)
+    ops.adjust_logits(z, out=out, **kw)
+    ok = (out[590:].double() == want) | ((out[590:].double() - want).abs() <= 2.0 ** -8 * (want.abs() + bar) + bar)
+    assert bool(ok.all())
+
+
+# ---- together, on other streams, in graphs ----
+
+def served(x, res, gain, w, kw, tok):
+    """One step of a served model's end: norm, product, what the requests ask, scores."""
+    n = ops.norm_mx(x, gain, residual=res, values=True)
+    z = ops.matmul_mx(n.q, n.scale, w.q, w.scale, row_scale=n.row_scale, dtype=F32)
+    y = ops.adjust_logits(z, **kw)
+    s = ops.log_probs(y, tok, top=3)
+    again = ops.quant_mx(n.values, values=True)
+    return [n.q, n.scale, n.row_scale, n.summed, n.values, z, y] + list(s) + list(again)
+
+
+def served_inputs(seed, rows=60, V=3000, D=288):
+    w = ops.quant_mx(randn(seed, V, D) / math.sqrt(D))
+    return (randn(seed + 1, rows, D), randn(seed + 2, rows, D), 1 + 0.1 * randn(seed + 3, D), w,
+            request(seed + 4, rows, V, 100), ints(seed + 5, -1, V, rows))
+
+
+def test_served_step_against_64_bits():
+    x, res, gain, w, kw, tok = served_inputs(50)
+    got = served(x, res, gain, w, kw, tok)
+    h = x + res
+    code, byte, value = plain_rows(h * gain)
+    factor = 1 / torch.sqrt(h.double().square().mean(1) + 1e-6)
+    b = unpacked(w.q, w.scale)
+    z = (value @ b.t()) * factor[:, None]
+    mag = (value.abs() @ b.abs().t()) * factor[:, None]
+    bar_z = ((value.shape[1] + 3) * U + 4e-6) * mag
+    assert bool(((got[5].double() - z).abs() <= bar_z).all())
+    y, bar = plain_adjust(z, **kw)
+    grow = torch.maximum(kw["repetition"], 1 / kw["repetition"]).double()[:, None]
+    ok = (got[6].double() == y) | ((got[6].double() - y).abs() <= bar + grow * bar_z)
+    assert bool(ok.all())
+    # the scores are those of the adjusted logits: what is not allowed is no alternative
+    assert bool((got[11].isneginf() | (got[6].gather(1, got[10].long()) > -INF)).all())
+
+
+def flat(args):
+    for a in args:
+        yield from flat(a.values() if isinstance(a, dict) else a) if not torch.is_tensor(a) else [a]
+
+
+def test_another_stream_and_the_same_bits():
+    args = served_inputs(20)
+    want = served(*args)
+    for a, b in zip(want, served(*args)):
+        assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        x, res, gain, w, kw, tok = args
+        got = served(x.clone(), res.clone(), gain.clone(), ops.MxRows(w.q.clone(), w.scale.clone(), None),
+                     {k: v.clone() for k, v in kw.items()}, tok.clone())
+    side.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+def test_graph_replays():
+    args = served_inputs(30)
+    args = args[:3] + (ops.MxRows(args[3].q, args[3].scale, args[3].q.new_empty(0)),) + args[4:]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        served(*args)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):  # two graphs of one program: their workspaces are their own
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = served(*args)
+        graphs.append((graph, got))
+    for seed in (40, 50, 60):
+        new = served_inputs(seed)
+        new = new[:3] + (ops.MxRows(new[3].q, new[3].scale, args[3].values),) + new[4:]
+        for a, b in zip(flat(args), flat(new)):
+            a.copy_(b)
+        want = served(*args)
+        torch.cuda.synchronize()
+        for graph, got in graphs + graphs[:1]:
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(want, got):
+                assert torch.equal(a, b)
+
+
+def test_products_in_parts_on_two_streams():
+    """Two calls at once, each with a workspace of its own."""
+    x, ex = random_rows(1, 100, 128, 2)
+    w, ew = random_rows(2, 600, 128, 2)
+    want = ops.matmul_mx(x, ex, w, ew, dtype=F32)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for side in sides:
+        side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for side in sides:
+            with torch.cuda.stream(side):
+                got.append(ops.matmul_mx(x, ex, w, ew, dtype=F32))
+    torch.cuda.synchronize()
+    for g in got:
+        assert torch.equal(g, want)
+
+
+def test_refusals():
+    x, f = randn(1, 4, 64), torch.zeros(4, device="cuda")
+    r = ops.quant_mx(x)
+    z, tok = randn(2, 4, 6), ints(3, 0, 6, 4, 5)
+    words = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for error, call in [
+        (TypeError, lambda: ops.quant_mx(x.half())),
+        (ValueError, lambda: ops.quant_mx(x.cpu())),
+        (ValueError, lambda: ops.quant_mx(x.t())),
+        (ValueError, lambda: ops.quant_mx(x, out=(r.q[:3], r.scale, None))),
+        (TypeError, lambda: ops.quant_mx(x, out=(r.q.char(), r.scale, None))),
+        (ValueError, lambda: ops.quant_mx(x, out=(r.q, r.scale[:1].expand(4, 2), None))),
+        (ValueError, lambda: ops.norm_mx(x, f)),
+        (TypeError, lambda: ops.norm_mx(x, residual=x.to(BF16))),
+        (ValueError, lambda: ops.norm_mx(x, residual=x[:2])),
+        (ops.FwgError, lambda: ops.norm_mx(x, eps=-1.0)),
+        (ops.FwgError, lambda: ops.norm_mx(torch.zeros((1, 32769), device="cuda"))),
+        (TypeError, lambda: ops.matmul_mx(x, r.scale, r.q, r.scale)),
+        (ValueError, lambda: ops.matmul_mx(r.q[:, :24], r.scale, r.q, r.scale)),
+        (ValueError, lambda: ops.matmul_mx(r.q[:, :24], r.scale, r.q[:, :24], r.scale)),
+        (ValueError, lambda: ops.matmul_mx(r.q, r.scale[:, :1], r.q, r.scale)),
+        (ValueError, lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale[:3])),
+        (ValueError, lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale, row_scale=f[:3])),
+        (ValueError, lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale, bias=f[:3])),
+        (TypeError, lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale, dtype=torch.float16)),
+        (ops.FwgError, lambda: ops.matmul_mx(r.q[:, :0], r.scale[:, :0], r.q[:, :0], r.scale[:, :0])),
+        (TypeError, lambda: ops.adjust_logits(z.double())),
+        (ValueError, lambda: ops.adjust_logits(z, presence=f)),
+        (ValueError, lambda: ops.adjust_logits(z, lengths=f.int())),
+        (TypeError, lambda: ops.adjust_logits(z, tok.long(), presence=f)),
+        (ValueError, lambda: ops.adjust_logits(z, tok[:3], presence=f)),
+        (TypeError, lambda: ops.adjust_logits(z, tok, lengths=f)),
+        (ValueError, lambda: ops.adjust_logits(z, tok, presence=f[:2])),
+        (ValueError, lambda: ops.adjust_logits(z, bias=f)),
+        (TypeError, lambda: ops.adjust_logits(z, bias=z.to(BF16))),
+        (TypeError, lambda: ops.adjust_logits(z, allowed=z[0, :1])),
+        (ValueError, lambda: ops.adjust_logits(z, allowed=torch.cat([words, words]))),
+        (ValueError, lambda: ops.adjust_logits(z[:1].expand(4, 6), out=z[:1].expand(4, 6))),
+        (TypeError, lambda: ops.adjust_logits(z, out=z.to(BF16))),
+    ]:
+        with pytest.raises(error):
+            call()
