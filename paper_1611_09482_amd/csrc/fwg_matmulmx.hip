@@ -7,6 +7,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+#include <type_traits>
+
 #include "fwg.h"
 #include "fwg_ops.h"
 #include "fwg_ops_dev.h"
@@ -21,77 +24,507 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4_b __attribute__((ext_vector_type(4), aligned(1)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// One product of 32 outputs x 32 rows x 64 elements; byte A of sa and byte B of sb are the scales of the lane's blocks.
-template <int A, int B>
-__device__ __forceinline__ f32x16 mma(const i32x4 &w, const i32x4 &x, const f32x16 &c, int sa, int sb) {
+// One product of 32 outputs x 32 rows x 64 elements, or of 16 x 16 x 128; byte B of sw and of sx is the scale of the lane's block.
+template <int B> __device__ __forceinline__ f32x16 mma(const i32x4 &w, const i32x4 &x, const f32x16 &c, int sw, int sx) {
   const i32x8 a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, b = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, A, sa, B, sb);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, B, sw, B, sx);
+}
+__device__ __forceinline__ f32x4 mma(const i32x4 &w, const i32x4 &x, const f32x4 &c, int sw, int sx) {
+  const i32x8 a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, b = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, sw, 0, sx);
 }
 
-// A wave per 32 outputs x 32 rows, operands straight from memory.
-template <typename TO> __global__ void __launch_bounds__(256) plain_kernel(MatmulMxArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 31, half = lane >> 5;
-  const int64_t m0 = (int64_t)blockIdx.x * 32;
-  const int n0 = (blockIdx.y * 4 + wave) * 32;
-  if (n0 >= a.N) return;
-  const int64_t m = m0 + row;
-  const int n = min(n0 + row, a.N - 1);
-  const int64_t mc = m < a.M ? m : a.M - 1;
-  const uint8_t *w = a.w + (int64_t)n * a.ld_w, *x = a.x + mc * a.ld_x;
-  const uint8_t *ew = a.w_scale + (int64_t)n * a.ld_ew, *ex = a.x_scale + mc * a.ld_ex;
-  f32x16 acc = {};
-  for (int b = 0; b < a.blocks; b += 2) {
-    i32x4 vw = {0, 0, 0, 0}, vx = {0, 0, 0, 0};
-    int sw = 127, sx = 127;
-    if (b + half < a.blocks) {
-      vw = *(const i32x4_b *)(w + (b + half) * 16);
-      vx = *(const i32x4_b *)(x + (b + half) * 16);
-      sw = ew[b + half];
-      sx = ex[b + half];
-    }
-    acc = mma<0, 0>(vw, vx, acc, sw, sx);
+// 16 bytes of a row of n bytes from byte k on; bytes from n on are 0.
+__device__ __forceinline__ i32x4 load16(const uint8_t *row, int k, int n) {
+  i32x4 v = {0, 0, 0, 0};
+  if (k >= n) return v;
+  if (k + 16 <= n) return *(const i32x4_b *)(row + k);
+  if (n >= 16) {  // the row's last 16 bytes, shifted down
+    const unsigned __int128 last = __builtin_bit_cast(unsigned __int128, (i32x4)*(const i32x4_b *)(row + n - 16));
+    return __builtin_bit_cast(i32x4, last >> (8 * (k + 16 - n)));
   }
-  if (m >= a.M) return;
-  const float f = a.row_scale ? a.row_scale[m] : 1.f;
+  unsigned __int128 part = 0;
+#pragma unroll 1
+  for (int i = n - 1; i >= k; --i) part = part << 8 | row[i];
+  return __builtin_bit_cast(i32x4, part);
+}
+
+// The same of 8 bytes.
+__device__ __forceinline__ u32x2 load8(const uint8_t *row, int k, int n) {
+  uint64_t v = 0;
+  if (k + 8 <= n) {
+    return *(const u32x2_b *)(row + k);
+  } else if (n >= 8) {
+    v = __builtin_bit_cast(uint64_t, (u32x2)*(const u32x2_b *)(row + n - 8)) >> (8 * (k + 8 - n));
+  } else {
+#pragma unroll 1
+    for (int i = n - 1; i >= k; --i) v = v << 8 | row[i];
+  }
+  return __builtin_bit_cast(u32x2, v);
+}
+
+// From memory to LDS without registers: lane l's bytes land at the (uniform) address + 16 l.
+__device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
+                                   (__attribute__((address_space(3))) void *)l, 16, 0, 0);
+}
+
+// Tiles of T outputs x T rows (256: eight waves; 128: four), eight blocks (256 elements, 128 bytes) of k per stage, two
+// stages in LDS: one is filled while the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows.
+//
+// A step of a stage multiplies 64 elements: which of the stage's blocks they are is free as long as both operands agree, so lanes
+// 0 .. 31 hold block s at step s and lanes 32 .. 63 block 4 + s.  The scales of a lane's four blocks are then four
+// neighbouring bytes, one word, of which step s names byte s.  Scales come through registers, which take them at any address.
+constexpr int HK = 128, HB = HK / 16;
+template <int T> struct Tile {
+  static constexpr int kWaves = T / 32, kThreads = 64 * kWaves, kWM = T / 2, kJ = kWM / 32;
+  static constexpr int kStage = 2 * T * HK;      // bytes of a stage: weights, then rows
+  static constexpr int kScales = 2 * T * HB;     // weights', then rows'
+  static constexpr int kLds = 2 * kStage + 2 * kScales + 2 * 2 * T * (int)sizeof(float);
+};
+
+// The 16-byte pieces of a stage's row r lie permuted, so that the 32 rows that an instruction reads at one k spread over the banks.
+__device__ __forceinline__ int piece_of(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+
+struct Cut {
+  int tiles_m, tiles_n, splits, per;  // k is cut into `splits` parts of `per` blocks (a multiple of HB)
+};
+
+// ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without passing through registers.  SUMS: of a part of k,
+// to the workspace.
+template <typename TO, bool ALIGNED, bool SUMS, int T>
+__global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs a, Cut cut) {
+  constexpr int I = 2, J = Tile<T>::kJ, kStage = Tile<T>::kStage, kScales = Tile<T>::kScales;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t *const scales = smem + 2 * kStage;
+  float *const vectors = (float *)(scales + 2 * kScales);  // [2]: bias, row_scale of the tile
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T>::kWM, row = lane & 31, half = lane >> 5;
+  const int tiles_m = cut.tiles_m, tiles_n = cut.tiles_n;
+  const int b_at = (int)blockIdx.y * cut.per, b_end = min(a.blocks, b_at + cut.per);  // blocks of k
+  TO *const result = (TO *)a.out + (SUMS ? (int64_t)blockIdx.y * a.M * a.ld_o : 0);
+  // Each XCD (blocks go to the eight in turn) takes a contiguous share of the tiles, eight rows of tiles at a time;
+  // its blocks go through the share together.
+  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = gridDim.x >> 3;
+  int tile = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
+  const int end = min(tiles, (int)(blockIdx.x & 7) * share + share);
+  if (tile >= end) return;
+
+  // Copies: a wave brings 32 rows of each operand, 8 rows of 8 pieces at a time; rows past the end are the last one, and so
+  // are blocks: any elements will do there, since both operands' scales are 2^-127 and the products vanish.
+  constexpr int C = 4;
+  int n0;
+  int64_t m0;
+  const uint8_t *bw, *bx;                   // the tile's first rows
+  int rows_w, rows_x;
+  const int cr = wave * 32 + (lane >> 3);   // the first of the lane's rows; the others follow 8 apart
+  const unsigned ow = cr * (unsigned)a.ld_w, ox = cr * (unsigned)a.ld_x;  // ALIGNED: its bytes from there (below 2^31)
+  const int piece = piece_of(cr, lane & 7) * 16, last = (a.blocks - 1) * 16;  // the others' pieces: 8 rows on, ^ 4
+  auto go_to = [&](int t) {
+    constexpr int G = 8;
+    const int band = t / (G * tiles_n), in_band = t - band * G * tiles_n, high = min(G, tiles_m - band * G);
+    n0 = in_band / high * T;
+    m0 = (int64_t)(band * G + in_band % high) * T;
+    bw = a.w + n0 * a.ld_w;
+    bx = a.x + m0 * a.ld_x;
+    rows_w = min(T, a.N - n0);
+    rows_x = (int)min((int64_t)T, a.M - m0);
+  };
+  auto copy = [&](int b0, int buf) {
+    uint8_t *w = smem + buf * kStage + wave * 32 * HK, *x = w + T * HK;
+    const int p[2] = {min(b0 * 16 + piece, last), min(b0 * 16 + (piece ^ 64), last)};
+    if constexpr (ALIGNED) {
+      const unsigned ld_w = (unsigned)a.ld_w, ld_x = (unsigned)a.ld_x;
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int at = n0 + 8 * g + 4 * half;
+      for (int i = 0; i < C; ++i) {
+        copy_16(bw + (min(ow + i * 8 * ld_w, (rows_w - 1) * ld_w) + p[i & 1]), w + i * 8 * HK);
+        copy_16(bx + (min(ox + i * 8 * ld_x, (rows_x - 1) * ld_x) + p[i & 1]), x + i * 8 * HK);
+      }
+    } else {
+      i32x4 vw[C], vx[C];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (at + e >= a.N) break;
-      float v = acc[4 * g + e] * f;
-      if (a.bias) v += a.bias[at + e];
-      put((TO *)a.out + m * a.ld_o + at + e, v);
+      for (int i = 0; i < C; ++i) {
+        vw[i] = *(const i32x4_b *)(bw + min(cr + i * 8, rows_w - 1) * a.ld_w + p[i & 1]);
+        vx[i] = *(const i32x4_b *)(bx + min(cr + i * 8, rows_x - 1) * a.ld_x + p[i & 1]);
+      }
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        *(i32x4 *)(w + i * 8 * HK + lane * 16) = vw[i];
+        *(i32x4 *)(x + i * 8 * HK + lane * 16) = vx[i];
+      }
+    }
+  };
+  // The scales of 8 blocks from b0 on, a row per thread.
+  u32x2 held;
+  auto load_scales = [&](int b0) {
+    const int r = threadIdx.x;
+    held = load8(r < T ? a.w_scale + (int64_t)(n0 + min(r, rows_w - 1)) * a.ld_ew
+                       : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex,
+                 b0, a.blocks);
+  };
+  auto store_scales = [&](int buf) { *(u32x2 *)(scales + buf * kScales + threadIdx.x * HB) = held; };
+  auto copy_vectors = [&](int which) {
+    if constexpr (!SUMS) {
+      const int t = threadIdx.x;
+      if (t < T) {
+        vectors[which * 2 * T + t] = a.bias ? a.bias[n0 + min(t, rows_w - 1)] : 0.f;
+        vectors[which * 2 * T + T + t] = a.row_scale ? a.row_scale[m0 + min(t, rows_x - 1)] : 1.f;
+      }
+    }
+  };
+
+  // the operands of one step, read while the step before is multiplied
+  f32x16 acc[I][J] = {};
+  i32x4 fw[2][I], fx[2][J];
+  int sw[I], sx[J], sw_next[I], sx_next[J];  // the stage's scales
+  auto read = [&](int buf, int step, int slot) {
+    const uint8_t *w = smem + buf * kStage + (wn + row) * HK, *x = smem + buf * kStage + T * HK + (wm + row) * HK;
+    const int p = piece_of(row, 4 * half + step) * 16;  // wn, wm and 32 leave (r >> 1) & 7 as it is
+#pragma unroll
+    for (int i = 0; i < I; ++i) fw[slot][i] = *(const i32x4 *)(w + i * 32 * HK + p);
+#pragma unroll
+    for (int j = 0; j < J; ++j) fx[slot][j] = *(const i32x4 *)(x + j * 32 * HK + p);
+  };
+  auto read_scales = [&](int buf) {
+    const uint8_t *w = scales + buf * kScales + (wn + row) * HB + half * 4, *x = w + (T + wm - wn) * HB;
+#pragma unroll
+    for (int i = 0; i < I; ++i) sw_next[i] = *(const int *)(w + i * 32 * HB);
+#pragma unroll
+    for (int j = 0; j < J; ++j) sx_next[j] = *(const int *)(x + j * 32 * HB);
+  };
+  auto take_scales = [&] {
+#pragma unroll
+    for (int i = 0; i < I; ++i) sw[i] = sw_next[i];
+#pragma unroll
+    for (int j = 0; j < J; ++j) sx[j] = sx_next[j];
+  };
+  auto multiply = [&](auto step) {
+    constexpr int K = decltype(step)::value;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < I; ++i) acc[i][j] = mma<K>(fw[K & 1][i], fx[K & 1][j], acc[i][j], sw[i], sx[j]);
+  };
+  // one read between two products
+  auto interleave = [] {
+#pragma unroll
+    for (int i = 0; i < min(I + J, I * J); ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    if constexpr (I * J > I + J) __builtin_amdgcn_sched_group_barrier(0x008, I * J - I - J, 0);
+  };
+
+  // Results: a wave's 64 outputs x T / 2 rows pass through 8 KB of LDS (of the stage that was multiplied last), 32 or 64
+  // rows at a time, so that they go out in whole lines of 128 (bf16) or 256 bytes; pieces of 16 bytes are permuted by the row.
+  auto write = [&](uint8_t *mine, const float *vec, int n_at, int64_t m_at) {
+    constexpr int kLine = 64 * (int)sizeof(TO), kPieces = kLine / 16;
+    constexpr int JP = sizeof(TO) == 2 ? 2 : 1, E = 16 / (int)sizeof(TO);
+    // places in LDS are worked out here: outside the loop over tiles they would hold 40 registers, more than there are left
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int row = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int j0 = 0; j0 < J; j0 += JP) {
+      in_order();
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int n = i * 32 + g * 8 + half * 4, at = n * (int)sizeof(TO);
+          f32x4 b;
+          if constexpr (!SUMS) b = *(const f32x4 *)(vec + wn + n);
+#pragma unroll
+          for (int jj = 0; jj < JP; ++jj) {
+            const int r = jj * 32 + row;
+            uint8_t *to = mine + r * kLine + (((at >> 4) ^ (r & (kPieces - 1))) << 4) + (at & 15);
+            float v[4], f = 1.f;
+            if constexpr (!SUMS) f = vec[T + wm + (j0 + jj) * 32 + row];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = acc[i][j0 + jj][4 * g + e];
+              if constexpr (!SUMS) v[e] = v[e] * f + b[e];
+            }
+            store_aligned((TO *)to, v);
+          }
+        }
+      }
+      in_order();
+      const int p = lane % kPieces, n = n_at + wn + p * E;
+#pragma unroll
+      for (int q = 0; q < JP * 32 * kPieces / 64; ++q) {
+        const int r = q * (64 / kPieces) + lane / kPieces;
+        const int64_t m = m_at + wm + j0 * 32 + r;
+        const uint8_t *line = mine + r * kLine + ((p ^ (r & (kPieces - 1))) << 4);
+        if (m >= a.M) continue;
+        TO *out = result + m * a.ld_o + n;
+        if (n + E <= a.N) {
+          *(u32x4_el *)out = *(const u32x4 *)line;
+        } else {
+          for (int k = 0; k < E; ++k)
+            if (n + k < a.N) out[k] = ((const TO *)line)[k];
+        }
+      }
+    }
+  };
+
+  go_to(tile);
+  copy(b_at, 0);
+  load_scales(b_at);
+  store_scales(0);
+  copy_vectors(0);
+  __syncthreads();
+  int buf = 0, which = 0;
+  while (true) {
+    const int n_at = n0, next = tile + stride;
+    const int64_t m_at = m0;
+    read(buf, 0, 0);
+    read_scales(buf);
+    take_scales();
+    auto three_steps = [&] {
+      read(buf, 1, 1);
+      multiply(std::integral_constant<int, 0>{});
+      interleave();
+      read(buf, 2, 0);
+      multiply(std::integral_constant<int, 1>{});
+      interleave();
+      read(buf, 3, 1);
+      multiply(std::integral_constant<int, 2>{});
+      interleave();
+      store_scales(buf ^ 1);  // also where no stage follows: a branch here would keep the reads above from their places
+      __syncthreads();        // the next stage has arrived, and this one has been read
+    };
+    for (int b = b_at; b + HB < b_end; b += HB) {
+      load_scales(b + HB);
+      copy(b + HB, buf ^ 1);
+      three_steps();
+      buf ^= 1;
+      read(buf, 0, 0);
+      read_scales(buf);
+      multiply(std::integral_constant<int, 3>{});
+      interleave();
+      take_scales();
+    }
+    // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
+    if (next < end) {
+      go_to(next);
+      load_scales(b_at);
+      copy(b_at, buf ^ 1);
+      copy_vectors(which ^ 1);
+    }
+    three_steps();
+    multiply(std::integral_constant<int, 3>{});
+    write(smem + buf * kStage + wave * 8192, vectors + which * 2 * T, n_at, m_at);
+    if (next >= end) break;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
+    tile = next;
+    buf ^= 1;
+    which ^= 1;
+    // the LDS just used may be copied over now; the results on their way out are not waited for
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  }
+}
+
+// Adds the parts of k up, in their order.
+template <typename TO> __global__ void __launch_bounds__(256) add_kernel(MatmulMxArgs a, int splits) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = a.M * a.N;
+  if (i >= all) return;
+  const float *sums = (const float *)a.ws;
+  if (i + 4 <= all && a.N % 4 == 0) {
+    f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) c += *(const f32x4 *)(sums + s * all + i);
+    const int64_t m = i / a.N;
+    const int n = (int)(i - m * a.N);
+    const float f = a.row_scale ? a.row_scale[m] : 1.f;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = c[e] * f + (a.bias ? a.bias[n + e] : 0.f);
+    store((TO *)a.out + m * a.ld_o + n, v);
+    return;
+  }
+  for (int64_t e = i; e < i + 4 && e < all; ++e) {
+    float c = 0.f;
+    for (int s = 0; s < splits; ++s) c += sums[s * all + e];
+    const int64_t m = e / a.N;
+    const int n = (int)(e - m * a.N);
+    put((TO *)a.out + m * a.ld_o + n, c * (a.row_scale ? a.row_scale[m] : 1.f) + (a.bias ? a.bias[n] : 0.f));
+  }
+}
+
+// Few rows (M <= 16 MT): the weights are read once, straight into registers, by one block per 16 NT outputs; the rows
+// come from the caches.  The W waves of a block take 16 blocks of k (256 bytes of a row) in turn, and their sums meet in LDS,
+// where they are added in the waves' order.  Four lanes hold four neighbouring blocks of a row at each of a turn's four steps.
+template <typename TO, int MT, int NT> __global__ void __launch_bounds__(512) rows_kernel(MatmulMxArgs a) {
+  constexpr int W = 8;
+  __shared__ float sums[W][MT * 16][NT * 16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, p = lane >> 4;
+  const int n0 = blockIdx.x * (16 * NT);
+  const uint8_t *w[NT], *ew[NT], *x[MT], *ex[MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int64_t n = min(n0 + i * 16 + r, a.N - 1);
+    w[i] = a.w + n * a.ld_w + p * 16;
+    ew[i] = a.w_scale + n * a.ld_ew;
+  }
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int64_t m = min(j * 16 + r, (int)a.M - 1);
+    x[j] = a.x + m * a.ld_x + p * 16;
+    ex[j] = a.x_scale + m * a.ld_ex;
+  }
+  f32x4 acc[NT][MT] = {};
+  for (int b = wave * 16; b < a.blocks; b += 16 * W) {
+    i32x4 vw[4][NT], vx[4][MT], sw[NT], sx[MT];
+    if (b + 16 <= a.blocks) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) vw[s][i] = *(const i32x4_b *)(w[i] + (b + 4 * s) * 16);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) vx[s][j] = *(const i32x4_b *)(x[j] + (b + 4 * s) * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) sw[i] = *(const i32x4_b *)(ew[i] + b);
+#pragma unroll
+      for (int j = 0; j < MT; ++j) sx[j] = *(const i32x4_b *)(ex[j] + b);
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const bool in = b + 4 * s + p < a.blocks;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) vw[s][i] = in ? (i32x4) * (const i32x4_b *)(w[i] + (b + 4 * s) * 16) : i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < MT; ++j) vx[s][j] = in ? (i32x4) * (const i32x4_b *)(x[j] + (b + 4 * s) * 16) : i32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) sw[i] = load16(ew[i], b, a.blocks);
+#pragma unroll
+      for (int j = 0; j < MT; ++j) sx[j] = load16(ex[j], b, a.blocks);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      int cw[NT], cx[MT];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) cw[i] = sw[i][s] >> (8 * p);
+#pragma unroll
+      for (int j = 0; j < MT; ++j) cx[j] = sx[j][s] >> (8 * p);
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = mma(vw[s][i], vx[s][j], acc[i][j], cw[i], cx[j]);
     }
   }
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) *(f32x4 *)&sums[wave][j * 16 + r][i * 16 + p * 4] = acc[i][j];
+  __syncthreads();
+  for (int t = threadIdx.x; t < MT * NT * 256; t += 64 * W) {
+    const int m = t / (16 * NT), c = t % (16 * NT), n = n0 + c;
+    if (m >= a.M || n >= a.N) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) v += sums[k][m][c];
+    if (a.row_scale) v *= a.row_scale[m];
+    if (a.bias) v += a.bias[n];
+    put((TO *)a.out + m * a.ld_o + n, v);
+  }
+}
+
+bool rows_form(int64_t M, int N) { return M <= 16 || (M <= 32 && N <= 8192) || (M <= 64 && N <= 4096); }
+// How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.
+int cut_of(int64_t M, int N, int blocks, Cut *c) {
+  const int64_t big = (M + 255) / 256 * ((N + 255) / 256);
+  const int side = big >= 192 ? 256 : 128;
+  c->tiles_m = (int)((M + side - 1) / side);
+  c->tiles_n = (N + side - 1) / side;
+  const int64_t tiles = (int64_t)c->tiles_m * c->tiles_n;
+  const int stages = (blocks + HB - 1) / HB;
+  int64_t splits = side == 256 ? 1 : 256 / tiles;
+  if (splits > stages / 4) splits = stages / 4;  // a part shorter than four stages costs more than it saves
+  if (splits < 1) splits = 1;
+  c->per = (int)((stages + splits - 1) / splits) * HB;
+  c->splits = (blocks + c->per - 1) / c->per;
+  return side;
+}
+
+// Lets a kernel have its LDS, once per device (`done`: one bit each; a device past the 64th is told every time).
+hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+template <typename TO, bool ALIGNED, bool SUMS, int T> hipError_t run_tiles(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, SUMS, T>, Tile<T>::kLds, done);
+  if (e != hipSuccess) return e;
+  // a block goes through several tiles where there are more than the device holds (one of 256, or two of 128 per
+  // compute unit)
+  const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = T == 256 ? 256 : 512;
+  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, SUMS, T>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)c.splits),
+                     dim3(Tile<T>::kThreads), Tile<T>::kLds, s, a, c);
+  return hipGetLastError();
+}
+
+template <typename TO, bool SUMS, int T> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+  const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
+  const bool near = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
+  return aligned && near ? run_tiles<TO, true, SUMS, T>(a, c, s) : run_tiles<TO, false, SUMS, T>(a, c, s);
+}
+
+template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulMxArgs &a, hipStream_t s) {
+  constexpr int64_t kSlice = ((int64_t)16 * NT) << 22;  // outputs of a launch: it has at most 2^32 threads
+  for (int64_t n = 0; n < a.N; n += kSlice) {
+    MatmulMxArgs b = a;
+    b.N = (int)(a.N - n < kSlice ? a.N - n : kSlice);
+    b.w = a.w + n * a.ld_w;
+    b.w_scale = a.w_scale + n * a.ld_ew;
+    if (a.bias) b.bias = a.bias + n;
+    b.out = (TO *)a.out + n;
+    hipLaunchKernelGGL((rows_kernel<TO, MT, NT>), dim3((unsigned)((b.N + 16 * NT - 1) / (16 * NT))), dim3(512), 0, s, b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
-  constexpr int64_t kRows = (int64_t)1 << 20;  // rows of a launch
-  constexpr int kCols = 128 * 128;             // outputs of a launch
-  for (int64_t m = 0; m < a.M; m += kRows)
-    for (int64_t n = 0; n < a.N; n += kCols) {
-      MatmulMxArgs b = a;
-      b.M = a.M - m < kRows ? a.M - m : kRows;
-      b.N = (int)(a.N - n < kCols ? a.N - n : kCols);
-      b.x = a.x + m * a.ld_x;
-      b.x_scale = a.x_scale + m * a.ld_ex;
-      b.w = a.w + n * a.ld_w;
-      b.w_scale = a.w_scale + n * a.ld_ew;
-      if (a.row_scale) b.row_scale = a.row_scale + m;
-      if (a.bias) b.bias = a.bias + n;
-      b.out = (TO *)a.out + m * a.ld_o + n;
-      hipLaunchKernelGGL((plain_kernel<TO>), dim3((unsigned)((b.M + 31) / 32), (unsigned)((b.N + 127) / 128)), dim3(256), 0, s,
-                         b);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-  return hipSuccess;
+  if (rows_form(a.M, a.N)) {
+    if (a.M <= 16) return a.N >= 8192 ? run_rows<TO, 1, 2>(a, s) : run_rows<TO, 1, 1>(a, s);
+    return a.M <= 32 ? run_rows<TO, 2, 1>(a, s) : run_rows<TO, 4, 1>(a, s);
+  }
+  Cut c;
+  if (cut_of(a.M, a.N, a.blocks, &c) == 256) return run_cut<TO, false, 256>(a, c, s);
+  if (c.splits == 1) return run_cut<TO, false, 128>(a, c, s);
+  MatmulMxArgs b = a;
+  b.out = a.ws;
+  b.ld_o = a.N;
+  const hipError_t e = run_cut<float, true, 128>(b, c, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((add_kernel<TO>), dim3((unsigned)((a.M * a.N + 1023) / 1024)), dim3(256), 0, s, a, c.splits);
+  return hipGetLastError();
 }
 
 }  // namespace mmx
 
-size_t matmul_mx_bytes(int64_t, int, int) { return 0; }
+size_t matmul_mx_bytes(int64_t rows, int outputs, int blocks) {
+  if (mmx::rows_form(rows, outputs)) return 0;
+  mmx::Cut c;
+  const int side = mmx::cut_of(rows, outputs, blocks, &c);
+  return side == 128 && c.splits > 1 ? (size_t)c.splits * rows * outputs * sizeof(float) : 0;
+}
 
 hipError_t launch_matmul_mx(const MatmulMxArgs &a, int out_dtype, hipStream_t s) {
   return out_dtype == FWG_BF16 ? mmx::run<uint16_t>(a, s) : mmx::run<float>(a, s);
