@@ -63,7 +63,11 @@ __device__ __forceinline__ u32x2 load8(const uint8_t *row, int k, int n) {
   return __builtin_bit_cast(u32x2, v);
 }
 
-// From memory to LDS without registers: lane l's bytes land at the (uniform) address + 16 l.
+// From memory to LDS without registers: lane l's bytes land at the (uniform) address + 16 l, or 4 l.
+__device__ __forceinline__ void copy_4(const uint8_t *g, uint8_t *l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
+                                   (__attribute__((address_space(3))) void *)l, 4, 0, 0);
+}
 __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
                                    (__attribute__((address_space(3))) void *)l, 16, 0, 0);
@@ -74,7 +78,11 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
 //
 // A step of a stage multiplies 64 elements: which of the stage's blocks they are is free as long as both operands agree, so lanes
 // 0 .. 31 hold block s at step s and lanes 32 .. 63 block 4 + s.  The scales of a lane's four blocks are then four
-// neighbouring bytes, one word, of which step s names byte s.  Scales come through registers, which take them at any address.
+// neighbouring bytes, one word, of which step s names byte s.
+//
+// A stage's scales are 8 bytes of each row, and reading them from the rows would bring in 128 for them: 8,192^3 took
+// 313 us so, of which 67 were for the scales.  Tiles of 256 find them rearranged by stages (pack_kernel, 4 us there); those of
+// 128 take them from the rows, through registers.
 constexpr int HK = 128, HB = HK / 16;
 template <int T> struct Tile {
   static constexpr int kWaves = T / 32, kThreads = 64 * kWaves, kWM = T / 2, kJ = kWM / 32;
@@ -85,6 +93,17 @@ template <int T> struct Tile {
 
 // The 16-byte pieces of a stage's row r lie permuted, so that the 32 rows that an instruction reads at one k spread over the banks.
 __device__ __forceinline__ int piece_of(int row, int piece) { return piece ^ ((row >> 1) & 7); }
+
+// The scales of 256 rows at a time, of both operands (weights first), as [stage][row][8 bytes]: a thread 16 bytes of a row.
+__global__ void __launch_bounds__(256) pack_kernel(MatmulMxArgs a, int tiles_n) {
+  const int t = blockIdx.x, stages = (a.blocks + HB - 1) / HB, stage = 2 * blockIdx.y;
+  const int64_t r = (int64_t)(t < tiles_n ? t : t - tiles_n) * 256 + threadIdx.x;
+  const uint8_t *row = t < tiles_n ? a.w_scale + min(r, (int64_t)a.N - 1) * a.ld_ew : a.x_scale + min(r, a.M - 1) * a.ld_ex;
+  const i32x4 v = load16(row, stage * HB, a.blocks);
+  uint8_t *to = a.ws + (((int64_t)t * stages + stage) * 256 + threadIdx.x) * HB;
+  *(u32x2 *)to = u32x2{(unsigned)v[0], (unsigned)v[1]};
+  if (stage + 1 < stages) *(u32x2 *)(to + 256 * HB) = u32x2{(unsigned)v[2], (unsigned)v[3]};
+}
 
 struct Cut {
   int tiles_m, tiles_n, splits, per;  // k is cut into `splits` parts of `per` blocks (a multiple of HB)
@@ -154,15 +173,25 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
       }
     }
   };
-  // The scales of 8 blocks from b0 on, a row per thread.
+  // The scales of 8 blocks from b0 on: of 32 rows of each operand per wave, or of a row per thread.
+  constexpr bool kPacked = T == 256;
   u32x2 held;
-  auto load_scales = [&](int b0) {
+  auto load_scales = [&](int b0, int buf) {
+    if constexpr (kPacked) {
+      const int stages = (a.blocks + HB - 1) / HB, at = b0 * 256 + wave * 256 + lane * 4;
+      uint8_t *to = scales + buf * kScales + wave * 256;
+      copy_4(a.ws + (int64_t)(n0 / T) * stages * (256 * HB) + at, to);
+      copy_4(a.ws + (tiles_n + m0 / T) * stages * (256 * HB) + at, to + T * HB);
+      return;
+    }
     const int r = threadIdx.x;
     held = load8(r < T ? a.w_scale + (int64_t)(n0 + min(r, rows_w - 1)) * a.ld_ew
                        : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex,
                  b0, a.blocks);
   };
-  auto store_scales = [&](int buf) { *(u32x2 *)(scales + buf * kScales + threadIdx.x * HB) = held; };
+  auto store_scales = [&](int buf) {
+    if constexpr (!kPacked) *(u32x2 *)(scales + buf * kScales + threadIdx.x * HB) = held;
+  };
   auto copy_vectors = [&](int which) {
     if constexpr (!SUMS) {
       const int t = threadIdx.x;
@@ -270,7 +299,7 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
 
   go_to(tile);
   copy(b_at, 0);
-  load_scales(b_at);
+  load_scales(b_at, 0);
   store_scales(0);
   copy_vectors(0);
   __syncthreads();
@@ -295,7 +324,7 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
       __syncthreads();        // the next stage has arrived, and this one has been read
     };
     for (int b = b_at; b + HB < b_end; b += HB) {
-      load_scales(b + HB);
+      load_scales(b + HB, buf ^ 1);
       copy(b + HB, buf ^ 1);
       three_steps();
       buf ^= 1;
@@ -308,7 +337,7 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
     // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
     if (next < end) {
       go_to(next);
-      load_scales(b_at);
+      load_scales(b_at, buf ^ 1);
       copy(b_at, buf ^ 1);
       copy_vectors(which ^ 1);
     }
@@ -506,7 +535,12 @@ template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
     return a.M <= 32 ? run_rows<TO, 2, 1>(a, s) : run_rows<TO, 4, 1>(a, s);
   }
   Cut c;
-  if (cut_of(a.M, a.N, a.blocks, &c) == 256) return run_cut<TO, false, 256>(a, c, s);
+  if (cut_of(a.M, a.N, a.blocks, &c) == 256) {
+    const dim3 grid((unsigned)(c.tiles_n + c.tiles_m), (unsigned)((a.blocks + 2 * HB - 1) / (2 * HB)));
+    hipLaunchKernelGGL(pack_kernel, grid, dim3(256), 0, s, a, c.tiles_n);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : run_cut<TO, false, 256>(a, c, s);
+  }
   if (c.splits == 1) return run_cut<TO, false, 128>(a, c, s);
   MatmulMxArgs b = a;
   b.out = a.ws;
@@ -522,8 +556,9 @@ template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
 size_t matmul_mx_bytes(int64_t rows, int outputs, int blocks) {
   if (mmx::rows_form(rows, outputs)) return 0;
   mmx::Cut c;
-  const int side = mmx::cut_of(rows, outputs, blocks, &c);
-  return side == 128 && c.splits > 1 ? (size_t)c.splits * rows * outputs * sizeof(float) : 0;
+  if (mmx::cut_of(rows, outputs, blocks, &c) == 256)  // both operands' scales by stages
+    return (size_t)(c.tiles_n + c.tiles_m) * 256 * ((blocks + mmx::HB - 1) / mmx::HB * mmx::HB);
+  return c.splits > 1 ? (size_t)c.splits * rows * outputs * sizeof(float) : 0;
 }
 
 hipError_t launch_matmul_mx(const MatmulMxArgs &a, int out_dtype, hipStream_t s) {
