@@ -25,6 +25,11 @@ constexpr uint32_t kInfBits = 0x7f800000u;
 
 typedef unsigned int u32_b __attribute__((aligned(1)));
 
+template <bool STREAM> __device__ __forceinline__ void put_word(uint8_t *p, uint32_t v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, (u32_b *)p);
+  else *(u32_b *)p = v;
+}
+
 // Largest of the four lanes of a quad.
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   v = max(v, (uint32_t)dpp_i<0xB1>((int)v));
@@ -64,7 +69,7 @@ __device__ __forceinline__ void values_of(uint32_t q, uint32_t top, float factor
   }
 }
 
-template <typename T> __global__ void __launch_bounds__(256) quant_kernel(MxArgs a, int pieces) {
+template <typename T, bool STREAM> __global__ void __launch_bounds__(256) quant_kernel(MxArgs a, int pieces) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t r = i / pieces;
   const int c = (int)(i - r * pieces) * kE, have = a.channels - c;
@@ -73,16 +78,17 @@ template <typename T> __global__ void __launch_bounds__(256) quant_kernel(MxArgs
   load_part((const T *)a.x + r * a.ld_x + c, have, 0.f, v);
   uint32_t top;
   const uint32_t q = four_bits(v, top);
-  *(u32_b *)(a.q + r * a.ld_q + c / 2) = q;
+  put_word<STREAM>(a.q + r * a.ld_q + c / 2, q);
   if ((c & 31) == 0) a.scale[r * a.ld_e + c / 32] = (uint8_t)scale_byte(top);
   if (a.values) {
     values_of(q, top, 1.f, v);
-    store_part(a.values + r * a.ld_v + c, have, v);
+    store_part<STREAM>(a.values + r * a.ld_v + c, have, v);
   }
 }
 
 // TPR threads per row (64: a wave per row), NP pieces per thread.
-template <typename T, int TPR, int NP> __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(MxArgs a) {
+template <typename T, int TPR, int NP, bool STREAM>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(MxArgs a) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kW = TPR / 64;
   __shared__ float red[2 * kW];
   const int t = threadIdx.x % TPR;
@@ -102,7 +108,7 @@ template <typename T, int TPR, int NP> __global__ void __launch_bounds__(TPR < 2
 #pragma unroll
       for (int i = 0; i < kE; ++i) h[i] += v[i];
     }
-    if (a.summed) store_part((T *)a.summed + r * a.ld_s + c, have, h);
+    if (a.summed) store_part<STREAM>((T *)a.summed + r * a.ld_s + c, have, h);
 #pragma unroll
     for (int i = 0; i < kE; ++i) ss += h[i] * h[i];
     if (a.gain) {
@@ -114,7 +120,7 @@ template <typename T, int TPR, int NP> __global__ void __launch_bounds__(TPR < 2
     q[p] = four_bits(h, top[p]);
     if (!nothing(top[p])) some = 1.f;
     if (c < padded) {
-      *(u32_b *)(a.q + r * a.ld_q + c / 2) = q[p];
+      put_word<STREAM>(a.q + r * a.ld_q + c / 2, q[p]);
       if ((c & 31) == 0) a.scale[r * a.ld_e + c / 32] = (uint8_t)scale_byte(top[p]);
     }
   }
@@ -144,14 +150,20 @@ template <typename T, int TPR, int NP> __global__ void __launch_bounds__(TPR < 2
     const int c = (p * TPR + t) * kE;
     float v[kE];
     values_of(q[p], top[p], factor, v);
-    store_part(a.values + r * a.ld_v + c, a.channels - c, v);
+    store_part<STREAM>(a.values + r * a.ld_v + c, a.channels - c, v);
   }
+}
+
+// Bytes that a launch writes.
+template <typename T> int64_t written(const MxArgs &a) {
+  return a.rows * a.channels * ((a.summed ? (int64_t)sizeof(T) : 0) + (a.values ? 2 : 0)) + a.rows * (a.channels / 2);
 }
 
 template <typename T, int TPR, int NP> hipError_t go(const MxArgs &a, hipStream_t s) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
-  hipLaunchKernelGGL((norm_kernel<T, TPR, NP>), dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(TPR < 256 ? 256 : TPR), 0,
-                     s, a);
+  const dim3 grid((unsigned)((a.rows + kRows - 1) / kRows)), block(TPR < 256 ? 256 : TPR);
+  if (written<T>(a) < kStreamBytes) hipLaunchKernelGGL((norm_kernel<T, TPR, NP, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_kernel<T, TPR, NP, true>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
@@ -168,7 +180,9 @@ template <typename T> hipError_t run_norm(const MxArgs &a, hipStream_t s) {
 
 template <typename T> hipError_t run_quant(const MxArgs &a, hipStream_t s) {
   const int pieces = (a.channels + 31) / 32 * 4;
-  hipLaunchKernelGGL((quant_kernel<T>), dim3((unsigned)((a.rows * pieces + 255) / 256)), dim3(256), 0, s, a, pieces);
+  const dim3 grid((unsigned)((a.rows * pieces + 255) / 256));
+  if (written<T>(a) < kStreamBytes) hipLaunchKernelGGL((quant_kernel<T, false>), grid, dim3(256), 0, s, a, pieces);
+  else hipLaunchKernelGGL((quant_kernel<T, true>), grid, dim3(256), 0, s, a, pieces);
   return hipGetLastError();
 }
 

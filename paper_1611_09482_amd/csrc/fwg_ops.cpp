@@ -339,7 +339,7 @@ int fwg_adjust_logits(int32_t dtype, int64_t rows, int32_t vocab, const void *lo
   if (frequency) CHECK(check_ptr("frequency", frequency, 4));
   if (bias) CHECK(check_ptr("bias", bias, 4));
   if (allowed) CHECK(check_ptr("allowed", allowed, 4));
-  const int64_t per = rows_per_launch(vocab);
+  const int64_t quarter = rows_per_launch(vocab) / 4, per = quarter < 1 ? 1 : quarter;  // up to 1,024 threads a row
   for (int64_t r = 0; r < rows; r += per) {
     AdjustArgs a{};
     a.logits = at(logits, r * logits_stride, dtype);
