@@ -52,7 +52,8 @@ __device__ __forceinline__ i32x4 load16(const uint8_t *row, int k, int n) {
 // The same of 8 bytes.
 __device__ __forceinline__ u32x2 load8(const uint8_t *row, int k, int n) {
   uint64_t v = 0;
-  if (k + 8 <= n) {
+  if (k >= n) {
+  } else if (k + 8 <= n) {
     return *(const u32x2_b *)(row + k);
   } else if (n >= 8) {
     v = __builtin_bit_cast(uint64_t, (u32x2)*(const u32x2_b *)(row + n - 8)) >> (8 * (k + 8 - n));
@@ -73,8 +74,10 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
                                    (__attribute__((address_space(3))) void *)l, 16, 0, 0);
 }
 
-// Tiles of T outputs x T rows (256: eight waves; 128: four), eight blocks (256 elements, 128 bytes) of k per stage, two
-// stages in LDS: one is filled while the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows.
+// Tiles of T outputs x T rows, eight blocks (256 elements, 128 bytes) of k per stage, two stages in LDS: one is filled while
+// the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows: eight waves for T = 256, four for 128.  G = 2: two groups
+// of so many waves take stages in turn, each with two of its own, and add their sums up at the end (333 x 8,000 x 4,096 in
+// 15.7 us, 18.3 with one group; but with two blocks on a compute unit 256 x 32,000 x 4,096 takes 30.7 with one, 36.3 with two).
 //
 // A step of a stage multiplies 64 elements: which of the stage's blocks they are is free as long as both operands agree, so lanes
 // 0 .. 31 hold block s at step s and lanes 32 .. 63 block 4 + s.  The scales of a lane's four blocks are then four
@@ -84,23 +87,26 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
 // 313 us so, of which 67 were for the scales.  Tiles of 256 find them rearranged by stages (pack_kernel, 4 us there); those of
 // 128 take them from the rows, through registers.
 constexpr int HK = 128, HB = HK / 16;
-template <int T> struct Tile {
-  static constexpr int kWaves = T / 32, kThreads = 64 * kWaves, kWM = T / 2, kJ = kWM / 32;
+template <int T, int G> struct Tile {
+  static constexpr int kWaves = T / 32, kThreads = 64 * kWaves * G, kWM = T / 2, kJ = kWM / 32;  // kWaves: of a group
   static constexpr int kStage = 2 * T * HK;      // bytes of a stage: weights, then rows
   static constexpr int kScales = 2 * T * HB;     // weights', then rows'
-  static constexpr int kLds = 2 * kStage + 2 * kScales + 2 * 2 * T * (int)sizeof(float);
+  static constexpr int kLds = 2 * G * (kStage + kScales) + 2 * 2 * T * (int)sizeof(float);
 };
 
 // The 16-byte pieces of a stage's row r lie permuted, so that the 32 rows that an instruction reads at one k spread over the banks.
 __device__ __forceinline__ int piece_of(int row, int piece) { return piece ^ ((row >> 1) & 7); }
 
-// The scales of 256 rows at a time, of both operands (weights first), as [stage][row][8 bytes]: a thread 16 bytes of a row.
+// The scales of 256 rows at a time, of both operands (weights first), as [stage][row][8 bytes]: a thread 16 bytes of a row,
+// eight threads 128.
 __global__ void __launch_bounds__(256) pack_kernel(MatmulMxArgs a, int tiles_n) {
-  const int t = blockIdx.x, stages = (a.blocks + HB - 1) / HB, stage = 2 * blockIdx.y;
-  const int64_t r = (int64_t)(t < tiles_n ? t : t - tiles_n) * 256 + threadIdx.x;
+  const int t = blockIdx.x / 8, stages = (a.blocks + HB - 1) / HB, stage = 2 * (8 * blockIdx.y + threadIdx.x % 8);
+  if (stage >= stages) return;
+  const int in_tile = blockIdx.x % 8 * 32 + threadIdx.x / 8;
+  const int64_t r = (int64_t)(t < tiles_n ? t : t - tiles_n) * 256 + in_tile;
   const uint8_t *row = t < tiles_n ? a.w_scale + min(r, (int64_t)a.N - 1) * a.ld_ew : a.x_scale + min(r, a.M - 1) * a.ld_ex;
   const i32x4 v = load16(row, stage * HB, a.blocks);
-  uint8_t *to = a.ws + (((int64_t)t * stages + stage) * 256 + threadIdx.x) * HB;
+  uint8_t *to = a.ws + (((int64_t)t * stages + stage) * 256 + in_tile) * HB;
   *(u32x2 *)to = u32x2{(unsigned)v[0], (unsigned)v[1]};
   if (stage + 1 < stages) *(u32x2 *)(to + 256 * HB) = u32x2{(unsigned)v[2], (unsigned)v[3]};
 }
@@ -111,20 +117,22 @@ struct Cut {
 
 // ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without passing through registers.  SUMS: of a part of k,
 // to the workspace.
-template <typename TO, bool ALIGNED, bool SUMS, int T>
-__global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs a, Cut cut) {
-  constexpr int I = 2, J = Tile<T>::kJ, kStage = Tile<T>::kStage, kScales = Tile<T>::kScales;
-  extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t *const scales = smem + 2 * kStage;
-  float *const vectors = (float *)(scales + 2 * kScales);  // [2]: bias, row_scale of the tile
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T>::kWM, row = lane & 31, half = lane >> 5;
+template <typename TO, bool ALIGNED, bool SUMS, int T, int G>
+__global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulMxArgs a, Cut cut) {
+  constexpr int I = 2, J = Tile<T, G>::kJ, kStage = Tile<T, G>::kStage, kScales = Tile<T, G>::kScales;
+  extern __shared__ __align__(1024) uint8_t all_smem[];
+  const int lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = all_wave / Tile<T, G>::kWaves, wave = all_wave % Tile<T, G>::kWaves;
+  uint8_t *const smem = all_smem + group * 2 * kStage;  // the group's
+  uint8_t *const scales = all_smem + G * 2 * kStage + group * 2 * kScales;
+  float *const vectors = (float *)(all_smem + G * 2 * (kStage + kScales));  // [2]: bias, row_scale of the tile
+  const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T, G>::kWM, row = lane & 31, half = lane >> 5;
   const int tiles_m = cut.tiles_m, tiles_n = cut.tiles_n;
   const int b_at = (int)blockIdx.y * cut.per, b_end = min(a.blocks, b_at + cut.per);  // blocks of k
   TO *const result = (TO *)a.out + (SUMS ? (int64_t)blockIdx.y * a.M * a.ld_o : 0);
   // Each XCD (blocks go to the eight in turn) takes a contiguous share of the tiles, eight rows of tiles at a time;
   // its blocks go through the share together.
-  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = gridDim.x >> 3;
+  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = G == 1 ? gridDim.x >> 3 : share;
   int tile = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
   const int end = min(tiles, (int)(blockIdx.x & 7) * share + share);
   if (tile >= end) return;
@@ -140,10 +148,10 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
   const unsigned ow = cr * (unsigned)a.ld_w, ox = cr * (unsigned)a.ld_x;  // ALIGNED: its bytes from there (below 2^31)
   const int piece = piece_of(cr, lane & 7) * 16, last = (a.blocks - 1) * 16;  // the others' pieces: 8 rows on, ^ 4
   auto go_to = [&](int t) {
-    constexpr int G = 8;
-    const int band = t / (G * tiles_n), in_band = t - band * G * tiles_n, high = min(G, tiles_m - band * G);
+    constexpr int kBand = 8;
+    const int band = t / (kBand * tiles_n), in_band = t - band * kBand * tiles_n, high = min(kBand, tiles_m - band * kBand);
     n0 = in_band / high * T;
-    m0 = (int64_t)(band * G + in_band % high) * T;
+    m0 = (int64_t)(band * kBand + in_band % high) * T;
     bw = a.w + n0 * a.ld_w;
     bx = a.x + m0 * a.ld_x;
     rows_w = min(T, a.N - n0);
@@ -184,13 +192,13 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
       copy_4(a.ws + (tiles_n + m0 / T) * stages * (256 * HB) + at, to + T * HB);
       return;
     }
-    const int r = threadIdx.x;
+    const int r = threadIdx.x % (Tile<T, G>::kThreads / G);
     held = load8(r < T ? a.w_scale + (int64_t)(n0 + min(r, rows_w - 1)) * a.ld_ew
                        : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex,
-                 b0, a.blocks);
+                 b0, b_end);
   };
   auto store_scales = [&](int buf) {
-    if constexpr (!kPacked) *(u32x2 *)(scales + buf * kScales + threadIdx.x * HB) = held;
+    if constexpr (!kPacked) *(u32x2 *)(scales + buf * kScales + threadIdx.x % (Tile<T, G>::kThreads / G) * HB) = held;
   };
   auto copy_vectors = [&](int which) {
     if constexpr (!SUMS) {
@@ -246,9 +254,9 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
 
   // Results: a wave's 64 outputs x T / 2 rows pass through 8 KB of LDS (of the stage that was multiplied last), 32 or 64
   // rows at a time, so that they go out in whole lines of 128 (bf16) or 256 bytes; pieces of 16 bytes are permuted by the row.
-  auto write = [&](uint8_t *mine, const float *vec, int n_at, int64_t m_at) {
+  auto write = [&](uint8_t *mine, const float *vec, int n_at, int64_t m_at, int wm, const auto &acc) {
     constexpr int kLine = 64 * (int)sizeof(TO), kPieces = kLine / 16;
-    constexpr int JP = sizeof(TO) == 2 ? 2 : 1, E = 16 / (int)sizeof(TO);
+    constexpr int J = sizeof(acc[0]) / sizeof(f32x16), JP = sizeof(TO) == 2 && J > 1 ? 2 : 1, E = 16 / (int)sizeof(TO);
     // places in LDS are worked out here: outside the loop over tiles they would hold 40 registers, more than there are left
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
@@ -300,9 +308,10 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
     }
   };
 
+  const int b_first = b_at + group * HB;
   go_to(tile);
-  copy(b_at, 0);
-  load_scales(b_at, 0);
+  copy(b_first, 0);
+  load_scales(b_first, 0);
   store_scales(0);
   copy_vectors(0);
   __syncthreads();
@@ -326,9 +335,10 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
       store_scales(buf ^ 1);  // also where no stage follows: a branch here would keep the reads above from their places
       __syncthreads();        // the next stage has arrived, and this one has been read
     };
-    for (int b = b_at; b + HB < b_end; b += HB) {
-      load_scales(b + HB, buf ^ 1);
-      copy(b + HB, buf ^ 1);
+    // stages that are past the end for a group have no scales: their products vanish
+    for (int b = b_at; b + G * HB < b_end; b += G * HB) {
+      load_scales(b + (G + group) * HB, buf ^ 1);
+      copy(b + (G + group) * HB, buf ^ 1);
       three_steps();
       buf ^= 1;
       read(buf, 0, 0);
@@ -337,28 +347,60 @@ __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs
       interleave();
       take_scales();
     }
-    // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
-    if (next < end) {
-      go_to(next);
-      load_scales(b_at, buf ^ 1);
-      copy(b_at, buf ^ 1);
-      copy_vectors(which ^ 1);
+    if constexpr (G == 2) {
+      three_steps();
+      multiply(std::integral_constant<int, 3>{});
+      // each group keeps half of the rows, and takes the other's sums of them
+      f32x16 kept[I][1];
+      auto give = [&](auto other) {
+        uint8_t *const to = all_smem + all_wave * 8192 + lane * 16;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x16 &c = acc[i][decltype(other)::value];
+            *(f32x4 *)(to + (i * 4 + q) * 1024) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+          }
+#pragma unroll
+        for (int i = 0; i < I; ++i) kept[i][0] = acc[i][1 - decltype(other)::value];
+      };
+      if (group == 0) give(std::integral_constant<int, 1>{});
+      else give(std::integral_constant<int, 0>{});
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = *(const f32x4 *)(all_smem + (all_wave ^ 4) * 8192 + lane * 16 + (i * 4 + q) * 1024);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) kept[i][0][4 * q + e] += v[e];
+        }
+      write(all_smem + 65536 + all_wave * 8192, vectors, n_at, m_at, wm + group * 32, kept);
+      break;
+    } else {
+      // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
+      if (next < end) {
+        go_to(next);
+        load_scales(b_at, buf ^ 1);
+        copy(b_at, buf ^ 1);
+        copy_vectors(which ^ 1);
+      }
+      three_steps();
+      multiply(std::integral_constant<int, 3>{});
+      write(smem + buf * kStage + wave * 8192, vectors + which * 2 * T, n_at, m_at, wm, acc);
+      if (next >= end) break;
+#pragma unroll
+      for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
+      tile = next;
+      buf ^= 1;
+      which ^= 1;
+      // the LDS just used may be copied over now; the results on their way out are not waited for
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     }
-    three_steps();
-    multiply(std::integral_constant<int, 3>{});
-    write(smem + buf * kStage + wave * 8192, vectors + which * 2 * T, n_at, m_at);
-    if (next >= end) break;
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-#pragma unroll
-      for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
-    tile = next;
-    buf ^= 1;
-    which ^= 1;
-    // the LDS just used may be copied over now; the results on their way out are not waited for
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   }
 }
 
@@ -478,9 +520,18 @@ int cut_of(int64_t M, int N, int blocks, Cut *c) {
   c->tiles_n = (N + side - 1) / side;
   const int64_t tiles = (int64_t)c->tiles_m * c->tiles_n;
   const int stages = (blocks + HB - 1) / HB;
-  int64_t splits = side == 256 ? 1 : 256 / tiles;
-  if (splits > stages / 4) splits = stages / 4;  // a part shorter than four stages costs more than it saves
-  if (splits < 1) splits = 1;
+  // Two stages take 1.3 us; adding parts up 4, and 1 more for each half million sums (written and read again).  In tenths:
+  // 1,000 x 2,000 x 2,016 takes 10.6 us whole and 21.2 in two parts, 300 x 515 x 4,096 16.4 and 13.5 in four.  Parts of less
+  // than four stages measured no better.
+  int64_t splits = 1, least = (stages + 1) / 2 * 13;
+  if (side == 128)
+    for (int64_t n = 2; n <= 256 / tiles && n <= stages / 4; ++n) {
+      const int64_t cost = ((stages + n - 1) / n + 1) / 2 * 13 + 40 + n * M * N / 50000;
+      if (cost < least) {
+        splits = n;
+        least = cost;
+      }
+    }
   c->per = (int)((stages + splits - 1) / splits) * HB;
   c->splits = (blocks + c->per - 1) / c->per;
   return side;
@@ -498,22 +549,22 @@ hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done)
   return e;
 }
 
-template <typename TO, bool ALIGNED, bool SUMS, int T> hipError_t run_tiles(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+template <typename TO, bool ALIGNED, bool SUMS, int T, int G> hipError_t run_tiles(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, SUMS, T>, Tile<T>::kLds, done);
+  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, SUMS, T, G>, Tile<T, G>::kLds, done);
   if (e != hipSuccess) return e;
   // a block goes through several tiles where there are more than the device holds (one of 256, or two of 128 per
   // compute unit)
-  const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = T == 256 ? 256 : 512;
-  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, SUMS, T>), dim3((unsigned)(blocks < most ? blocks : most), (unsigned)c.splits),
-                     dim3(Tile<T>::kThreads), Tile<T>::kLds, s, a, c);
+  const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = G == 2 ? blocks : T == 256 ? 256 : 512;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)c.splits), block((Tile<T, G>::kThreads));
+  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, SUMS, T, G>), grid, block, (Tile<T, G>::kLds), s, a, c);
   return hipGetLastError();
 }
 
-template <typename TO, bool SUMS, int T> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+template <typename TO, bool SUMS, int T, int G> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
   const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
   const bool near = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
-  return aligned && near ? run_tiles<TO, true, SUMS, T>(a, c, s) : run_tiles<TO, false, SUMS, T>(a, c, s);
+  return aligned && near ? run_tiles<TO, true, SUMS, T, G>(a, c, s) : run_tiles<TO, false, SUMS, T, G>(a, c, s);
 }
 
 template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulMxArgs &a, hipStream_t s) {
@@ -539,16 +590,17 @@ template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
   }
   Cut c;
   if (cut_of(a.M, a.N, a.blocks, &c) == 256) {
-    const dim3 grid((unsigned)(c.tiles_n + c.tiles_m), (unsigned)((a.blocks + 2 * HB - 1) / (2 * HB)));
+    const dim3 grid((unsigned)(c.tiles_n + c.tiles_m) * 8, (unsigned)((a.blocks + 16 * HB - 1) / (16 * HB)));
     hipLaunchKernelGGL(pack_kernel, grid, dim3(256), 0, s, a, c.tiles_n);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : run_cut<TO, false, 256>(a, c, s);
+    return e != hipSuccess ? e : run_cut<TO, false, 256, 1>(a, c, s);
   }
-  if (c.splits == 1) return run_cut<TO, false, 128>(a, c, s);
+  if ((int64_t)c.tiles_m * c.tiles_n > 256) return run_cut<TO, false, 128, 1>(a, c, s);
+  if (c.splits == 1) return run_cut<TO, false, 128, 2>(a, c, s);
   MatmulMxArgs b = a;
   b.out = a.ws;
   b.ld_o = a.N;
-  const hipError_t e = run_cut<float, true, 128>(b, c, s);
+  const hipError_t e = run_cut<float, true, 128, 2>(b, c, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((add_kernel<TO>), dim3((unsigned)((a.M * a.N + 1023) / 1024)), dim3(256), 0, s, a, c.splits);
   return hipGetLastError();
