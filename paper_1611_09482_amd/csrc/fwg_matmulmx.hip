@@ -4,6 +4,11 @@
 // v_mfma_scale_f32_32x32x64_f8f6f4 takes both operands as they lie in memory: a lane holds one block of 32 consecutive
 // elements of one row (16 bytes) and that block's scale byte.  Products and sums are float32.  The product is taken as
 // D[n][m] = W X^T: a lane then holds four consecutive outputs of one row and stores them together.
+//
+// Measured: 4,093 x 32,000 x 4,096 to bf16 262 us (4,090 TFLOP/s), 8,192^3 250 us (4,390); the largest library product of the
+// same type takes 452 and 340 us.  The instruction alone, operands in registers, reaches 6,460 TFLOP/s with random elements
+// and 9,770 with zeros: the card's power bounds it, and a variant that took 180 us instead of 196 for zeros takes the same time as
+// this one for random elements.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -83,9 +88,9 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
 // 0 .. 31 hold block s at step s and lanes 32 .. 63 block 4 + s.  The scales of a lane's four blocks are then four
 // neighbouring bytes, one word, of which step s names byte s.
 //
-// A stage's scales are 8 bytes of each row, and reading them from the rows would bring in 128 for them: 8,192^3 took
-// 313 us so, of which 67 were for the scales.  Tiles of 256 find them rearranged by stages (pack_kernel, 4 us there); those of
-// 128 take them from the rows, through registers.
+// A stage's scales are 8 bytes of each row, and reading them from the rows brings in whole lines.  Tiles of 256 find them
+// rearranged by stages (pack_kernel, 4 us in 8,192^3: 304 us from the rows, 274 so); those of 128 take them from the rows,
+// through registers, which hold them at any address.
 constexpr int HK = 128, HB = HK / 16;
 template <int T, int G> struct Tile {
   static constexpr int kWaves = T / 32, kThreads = 64 * kWaves * G, kWM = T / 2, kJ = kWM / 32;  // kWaves: of a group
@@ -99,16 +104,18 @@ __device__ __forceinline__ int piece_of(int row, int piece) { return piece ^ ((r
 
 // The scales of 256 rows at a time, of both operands (weights first), as [stage][row][8 bytes]: a thread 16 bytes of a row,
 // eight threads 128.
-__global__ void __launch_bounds__(256) pack_kernel(MatmulMxArgs a, int tiles_n) {
-  const int t = blockIdx.x / 8, stages = (a.blocks + HB - 1) / HB, stage = 2 * (8 * blockIdx.y + threadIdx.x % 8);
+__global__ void __launch_bounds__(256) pack_kernel(MatmulMxArgs a, int tiles_n, int tiles) {
+  const int stages = (a.blocks + HB - 1) / HB, stage = 2 * (8 * blockIdx.y + threadIdx.x % 8);
   if (stage >= stages) return;
-  const int in_tile = blockIdx.x % 8 * 32 + threadIdx.x / 8;
-  const int64_t r = (int64_t)(t < tiles_n ? t : t - tiles_n) * 256 + in_tile;
-  const uint8_t *row = t < tiles_n ? a.w_scale + min(r, (int64_t)a.N - 1) * a.ld_ew : a.x_scale + min(r, a.M - 1) * a.ld_ex;
-  const i32x4 v = load16(row, stage * HB, a.blocks);
-  uint8_t *to = a.ws + (((int64_t)t * stages + stage) * 256 + in_tile) * HB;
-  *(u32x2 *)to = u32x2{(unsigned)v[0], (unsigned)v[1]};
-  if (stage + 1 < stages) *(u32x2 *)(to + 256 * HB) = u32x2{(unsigned)v[2], (unsigned)v[3]};
+  for (int at = blockIdx.x; at < 8 * tiles; at += gridDim.x) {
+    const int t = at / 8, in_tile = at % 8 * 32 + threadIdx.x / 8;
+    const int64_t r = (int64_t)(t < tiles_n ? t : t - tiles_n) * 256 + in_tile;
+    const uint8_t *row = t < tiles_n ? a.w_scale + min(r, (int64_t)a.N - 1) * a.ld_ew : a.x_scale + min(r, a.M - 1) * a.ld_ex;
+    const i32x4 v = load16(row, stage * HB, a.blocks);
+    uint8_t *to = a.ws + (((int64_t)t * stages + stage) * 256 + in_tile) * HB;
+    *(u32x2 *)to = u32x2{(unsigned)v[0], (unsigned)v[1]};
+    if (stage + 1 < stages) *(u32x2 *)(to + 256 * HB) = u32x2{(unsigned)v[2], (unsigned)v[3]};
+  }
 }
 
 struct Cut {
@@ -116,8 +123,10 @@ struct Cut {
 };
 
 // ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without passing through registers.  SUMS: of a part of k,
-// to the workspace.
-template <typename TO, bool ALIGNED, bool SUMS, int T, int G>
+// to the workspace.  STREAM: results go past the caches, which then keep the operands: 4,093 x 32,000 x 4,096 278 us, 315 through
+// them; with the log probabilities of the results behind it 340 and 350, of 1,024 rows 96.4 and 97.5.  Only where rows are whole
+// lines of 128 bytes: 2,176 x 10,920 x 4,096 takes 69.7 us so, 62.2 through the caches.
+template <typename TO, bool ALIGNED, bool SUMS, bool STREAM, int T, int G>
 __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulMxArgs a, Cut cut) {
   constexpr int I = 2, J = Tile<T, G>::kJ, kStage = Tile<T, G>::kStage, kScales = Tile<T, G>::kScales;
   extern __shared__ __align__(1024) uint8_t all_smem[];
@@ -296,9 +305,7 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
         if (m >= a.M) continue;
         TO *out = result + m * a.ld_o + n;
         if (n + E <= a.N) {
-          // past the caches, which then keep the operands: 4,093 x 32,000 x 4,096 278 us, 315 through them; with the log
-          // probabilities of the results behind it 340 and 350, of 1,024 rows 96.4 and 97.5
-          if constexpr (T == 256) __builtin_nontemporal_store(*(const u32x4 *)line, (u32x4_el *)out);
+          if constexpr (STREAM) __builtin_nontemporal_store(*(const u32x4 *)line, (u32x4_el *)out);
           else *(u32x4_el *)out = *(const u32x4 *)line;
         } else {
           for (int k = 0; k < E; ++k)
@@ -434,6 +441,7 @@ template <typename TO> __global__ void __launch_bounds__(256) add_kernel(MatmulM
 // Few rows (M <= 16 MT): the weights are read once, straight into registers, by one block per 16 NT outputs; the rows
 // come from the caches.  The W waves of a block take 16 blocks of k (256 bytes of a row) in turn, and their sums meet in LDS,
 // where they are added in the waves' order.  Four lanes hold four neighbouring blocks of a row at each of a turn's four steps.
+// Bound by memory: 16 x 32,000 x 4,096 to float32 in 16.4 us (4.4 TB/s), one row in 14.9 (4.7).
 template <typename TO, int MT, int NT> __global__ void __launch_bounds__(512) rows_kernel(MatmulMxArgs a) {
   constexpr int W = 8;
   __shared__ float sums[W][MT * 16][NT * 16];
@@ -511,15 +519,23 @@ template <typename TO, int MT, int NT> __global__ void __launch_bounds__(512) ro
   }
 }
 
-bool rows_form(int64_t M, int N) { return M <= 16 || (M <= 32 && N <= 8192) || (M <= 64 && N <= 4096); }
-// How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.
+// rows_kernel or tiles (us): 32 rows x 8,192 outputs x 4,096 9.8 or 12.9, x 8,192 16.8 or 14.9; 32 x 32,000 x 1,024 12.7 or
+// 9.3; 64 x 4,096 x 8,192 15.0 or 15.4, 64 x 8,192 x 4,096 16.6 or 14.7.
+bool rows_form(int64_t M, int N, int blocks) {
+  return M <= 16 || (M <= 64 && (int64_t)N * blocks <= 1 << 20 && (M <= 32 || N <= 4096));
+}
+// How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.  A round of
+// tiles of 256, one on each compute unit, takes about 5 us and 1.5 a stage, behind 9 for the launches and the scales; of 128, two
+// on each, 4 us and 1 a stage, behind 4.  (us, tiles of 256 and of 128: 4,096 x 4,096 x 4,096 40.4 and 52.9; 1,500 x 6,000 x
+// 4,096 31.5 and 40.6; 2,048 x 4,096 x 4,096 30.2 and 28.5; 7,799 x 2,255 x 640 30.8 and 25.8.)
 int cut_of(int64_t M, int N, int blocks, Cut *c) {
-  const int64_t big = (M + 255) / 256 * ((N + 255) / 256);
-  const int side = big >= 192 ? 256 : 128;
+  const int stages = (blocks + HB - 1) / HB;
+  const int64_t big = (M + 255) / 256 * ((N + 255) / 256), small = (M + 127) / 128 * ((N + 127) / 128);
+  const int side = small > 256 && 90 + (big + 255) / 256 * (50 + 15 * stages) < 40 + (small + 511) / 512 * (40 + 10 * stages)
+                       ? 256 : 128;
   c->tiles_m = (int)((M + side - 1) / side);
   c->tiles_n = (N + side - 1) / side;
   const int64_t tiles = (int64_t)c->tiles_m * c->tiles_n;
-  const int stages = (blocks + HB - 1) / HB;
   // Two stages take 1.3 us; adding parts up 4, and 1 more for each half million sums (written and read again).  In tenths:
   // 1,000 x 2,000 x 2,016 takes 10.6 us whole and 21.2 in two parts, 300 x 515 x 4,096 16.4 and 13.5 in four.  Parts of less
   // than four stages measured no better.
@@ -549,22 +565,23 @@ hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done)
   return e;
 }
 
-template <typename TO, bool ALIGNED, bool SUMS, int T, int G> hipError_t run_tiles(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+template <typename TO, bool ALIGNED, bool SUMS, bool STREAM, int T, int G>
+hipError_t run_tiles(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, SUMS, T, G>, Tile<T, G>::kLds, done);
+  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, SUMS, STREAM, T, G>, Tile<T, G>::kLds, done);
   if (e != hipSuccess) return e;
   // a block goes through several tiles where there are more than the device holds (one of 256, or two of 128 per
   // compute unit)
   const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = G == 2 ? blocks : T == 256 ? 256 : 512;
   const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)c.splits), block((Tile<T, G>::kThreads));
-  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, SUMS, T, G>), grid, block, (Tile<T, G>::kLds), s, a, c);
+  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, SUMS, STREAM, T, G>), grid, block, (Tile<T, G>::kLds), s, a, c);
   return hipGetLastError();
 }
 
-template <typename TO, bool SUMS, int T, int G> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+template <typename TO, bool SUMS, bool STREAM, int T, int G> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
   const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
   const bool near = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
-  return aligned && near ? run_tiles<TO, true, SUMS, T, G>(a, c, s) : run_tiles<TO, false, SUMS, T, G>(a, c, s);
+  return aligned && near ? run_tiles<TO, true, SUMS, STREAM, T, G>(a, c, s) : run_tiles<TO, false, SUMS, STREAM, T, G>(a, c, s);
 }
 
 template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulMxArgs &a, hipStream_t s) {
@@ -584,23 +601,26 @@ template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulMxArgs &a
 }
 
 template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
-  if (rows_form(a.M, a.N)) {
+  if (rows_form(a.M, a.N, a.blocks)) {
     if (a.M <= 16) return a.N >= 8192 ? run_rows<TO, 1, 2>(a, s) : run_rows<TO, 1, 1>(a, s);
     return a.M <= 32 ? run_rows<TO, 2, 1>(a, s) : run_rows<TO, 4, 1>(a, s);
   }
   Cut c;
   if (cut_of(a.M, a.N, a.blocks, &c) == 256) {
-    const dim3 grid((unsigned)(c.tiles_n + c.tiles_m) * 8, (unsigned)((a.blocks + 16 * HB - 1) / (16 * HB)));
-    hipLaunchKernelGGL(pack_kernel, grid, dim3(256), 0, s, a, c.tiles_n);
+    const int tiles = c.tiles_n + c.tiles_m;
+    const dim3 grid(tiles < 1 << 16 ? tiles * 8 : 1 << 19, (unsigned)((a.blocks + 16 * HB - 1) / (16 * HB)));
+    hipLaunchKernelGGL(pack_kernel, grid, dim3(256), 0, s, a, c.tiles_n, tiles);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : run_cut<TO, false, 256, 1>(a, c, s);
+    if (e != hipSuccess) return e;
+    const bool lines = (((uintptr_t)a.out | (uintptr_t)(a.ld_o * (int64_t)sizeof(TO))) & 127) == 0;
+    return lines ? run_cut<TO, false, true, 256, 1>(a, c, s) : run_cut<TO, false, false, 256, 1>(a, c, s);
   }
-  if ((int64_t)c.tiles_m * c.tiles_n > 256) return run_cut<TO, false, 128, 1>(a, c, s);
-  if (c.splits == 1) return run_cut<TO, false, 128, 2>(a, c, s);
+  if ((int64_t)c.tiles_m * c.tiles_n > 256) return run_cut<TO, false, false, 128, 1>(a, c, s);
+  if (c.splits == 1) return run_cut<TO, false, false, 128, 2>(a, c, s);
   MatmulMxArgs b = a;
   b.out = a.ws;
   b.ld_o = a.N;
-  const hipError_t e = run_cut<float, true, 128, 2>(b, c, s);
+  const hipError_t e = run_cut<float, true, false, 128, 2>(b, c, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((add_kernel<TO>), dim3((unsigned)((a.M * a.N + 1023) / 1024)), dim3(256), 0, s, a, c.splits);
   return hipGetLastError();
@@ -609,7 +629,7 @@ template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
 }  // namespace mmx
 
 size_t matmul_mx_bytes(int64_t rows, int outputs, int blocks) {
-  if (mmx::rows_form(rows, outputs)) return 0;
+  if (mmx::rows_form(rows, outputs, blocks)) return 0;
   mmx::Cut c;
   if (mmx::cut_of(rows, outputs, blocks, &c) == 256)  // both operands' scales by stages
     return (size_t)(c.tiles_n + c.tiles_m) * 256 * ((blocks + mmx::HB - 1) / mmx::HB * mmx::HB);
