@@ -1,4 +1,4 @@
-"""Scoring recordings, and training and serving a small token model, with the token operators (one MI355X).
+"""Scoring recordings, and training, serving and continuing with a small token model, with the token operators (one MI355X).
 
   python examples/score_tokens.py
 
@@ -7,6 +7,8 @@
    recordings: embed -> norm and product (plain torch, with its backward) -> log_probs, then log_probs_grad and
    embed_grad for the gradients of the logits and of the table.
 3. The trained model is served in 8 bits: embed -> norm_quant -> matmul_quant -> log_probs.
+4. It is served in 4 bits, and continues recordings: embed -> norm_mx -> matmul_mx -> adjust_logits (what came often lately is
+   less likely, and only neighbouring classes are allowed) -> log_probs.
 """
 import math
 import os
@@ -88,6 +90,39 @@ class TokenModel:
         return score
 
 
+    def serve_four_bits(self):
+        """The model in 4 bits: a function of (now, before) that returns its logits."""
+        q = ops.quant_mx(self.product)
+
+        def logits(now, before):
+            x = ops.norm_mx(ops.embed(self.table, now), self.gain, residual=ops.embed(self.table, before, scale=0.5),
+                            eps=self.eps)
+            return ops.matmul_mx(x.q, x.scale, q.q, q.scale, row_scale=x.row_scale, dtype=torch.float32)
+        return logits
+
+
+def neighbours(now, reach: int = 16):
+    """Grammar of quiet sound, a row of bits each: the next class lies at most `reach` from this one."""
+    at = torch.arange(CLASSES, device="cuda")
+    near = ((at - now[:, None]).abs() <= reach).view(-1, CLASSES // 32, 32).long()
+    return (near << torch.arange(32, device="cuda")).sum(2).to(torch.int32)
+
+
+def continue_recordings(logits, start, steps: int, frequency: float = 0.02):
+    """The most likely continuation of int32 [streams][prompt] under requests: [streams][prompt + steps]."""
+    streams, prompt = start.shape
+    tokens = torch.cat([start, torch.full((streams, steps), -1, dtype=torch.int32, device="cuda")], 1)
+    prompts = torch.full((streams,), prompt, dtype=torch.int32, device="cuda")
+    often = torch.full((streams,), frequency, device="cuda")
+    none = torch.full((streams,), -1, dtype=torch.int32, device="cuda")
+    for t in range(prompt, prompt + steps):
+        now, before = tokens[:, t - 1].contiguous(), tokens[:, t - 2].contiguous()
+        z = logits(now, before)
+        ops.adjust_logits(z, tokens, torch.full_like(prompts, t), prompts=prompts, frequency=often, allowed=neighbours(now), out=z)
+        tokens[:, t] = ops.log_probs(z, none, top=1).top_ids[:, 0]
+    return tokens
+
+
 def main(streams: int = 32, length: int = 2000, steps: int = 200):
     classes = recordings(streams, length)
     wavenet = score_wavenet(classes)
@@ -107,6 +142,11 @@ def main(streams: int = 32, length: int = 2000, steps: int = 200):
     hit = (served.top_ids == after[:, None]).any(1).float().mean().item()
     print(f"token model: {first / math.log(2):.3f} bits before, {full / math.log(2):.3f} after training, "
           f"{eight / math.log(2):.3f} in 8 bits; the class is among the first three {100 * hit:.0f}% of the time", flush=True)
+    logits = model.serve_four_bits()
+    four = -ops.log_probs(logits(now, before), after).logp.mean().item()
+    more = continue_recordings(logits, classes[:, :64], 64)
+    jumps = (more[:, 64:] - more[:, 63:-1]).abs().max().item()
+    print(f"in 4 bits: {four / math.log(2):.3f} bits; recordings continued by 64 samples, no step larger than {jumps}", flush=True)
     return first, full, eight
 
 

@@ -693,3 +693,15 @@ def test_refusals():
     ]:
         with pytest.raises(error):
             call()
+
+
+# ---- the example: recordings continued under requests ----
+
+def test_example_continues_recordings():
+    import examples.score_tokens as example
+    classes = example.recordings(5, 40)
+    model = example.TokenModel(channels=96)
+    tokens = example.continue_recordings(model.serve_four_bits(), classes, 30)
+    assert torch.equal(tokens[:, :40], classes) and tokens.shape == (5, 70)
+    assert bool((tokens >= 0).all()) and bool((tokens < example.CLASSES).all())
+    assert int((tokens[:, 40:] - tokens[:, 39:-1]).abs().max()) <= 16  # as the grammar says
