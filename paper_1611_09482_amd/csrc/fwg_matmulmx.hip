@@ -54,21 +54,6 @@ __device__ __forceinline__ i32x4 load16(const uint8_t *row, int k, int n) {
   return __builtin_bit_cast(i32x4, part);
 }
 
-// The same of 8 bytes.
-__device__ __forceinline__ u32x2 load8(const uint8_t *row, int k, int n) {
-  uint64_t v = 0;
-  if (k >= n) {
-  } else if (k + 8 <= n) {
-    return *(const u32x2_b *)(row + k);
-  } else if (n >= 8) {
-    v = __builtin_bit_cast(uint64_t, (u32x2)*(const u32x2_b *)(row + n - 8)) >> (8 * (k + 8 - n));
-  } else {
-#pragma unroll 1
-    for (int i = n - 1; i >= k; --i) v = v << 8 | row[i];
-  }
-  return __builtin_bit_cast(u32x2, v);
-}
-
 // From memory to LDS without registers: lane l's bytes land at the (uniform) address + 16 l, or 4 l.
 __device__ __forceinline__ void copy_4(const uint8_t *g, uint8_t *l) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
@@ -89,14 +74,15 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
 // neighbouring bytes, one word, of which step s names byte s.
 //
 // A stage's scales are 8 bytes of each row, and reading them from the rows brings in whole lines.  Tiles of 256 find them
-// rearranged by stages (pack_kernel, 4 us in 8,192^3: 304 us from the rows, 274 so); those of 128 take them from the rows,
-// through registers, which hold them at any address.
+// rearranged by stages (pack_kernel, 4 us in 8,192^3: 304 us from the rows, 274 so); those of 128 take 16 bytes for two
+// stages of each group at a time from the rows, through registers, which hold them at any address.
 constexpr int HK = 128, HB = HK / 16;
 template <int T, int G> struct Tile {
   static constexpr int kWaves = T / 32, kThreads = 64 * kWaves * G, kWM = T / 2, kJ = kWM / 32;  // kWaves: of a group
   static constexpr int kStage = 2 * T * HK;      // bytes of a stage: weights, then rows
-  static constexpr int kScales = 2 * T * HB;     // weights', then rows'
-  static constexpr int kLds = 2 * G * (kStage + kScales) + 2 * 2 * T * (int)sizeof(float);
+  static constexpr int kScales = 2 * T * HB;     // of a stage: weights', then rows'
+  static constexpr int kChunk = T == 256 ? kScales : 2 * G * kScales;  // of the stages whose scales come together
+  static constexpr int kLds = 2 * (G * kStage + kChunk) + 2 * 2 * T * (int)sizeof(float);
 };
 
 // The 16-byte pieces of a stage's row r lie permuted, so that the 32 rows that an instruction reads at one k spread over the banks.
@@ -128,13 +114,13 @@ struct Cut {
 // lines of 128 bytes: 2,176 x 10,920 x 4,096 takes 69.7 us so, 62.2 through the caches.
 template <typename TO, bool ALIGNED, bool SUMS, bool STREAM, int T, int G>
 __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulMxArgs a, Cut cut) {
-  constexpr int I = 2, J = Tile<T, G>::kJ, kStage = Tile<T, G>::kStage, kScales = Tile<T, G>::kScales;
+  constexpr int I = 2, J = Tile<T, G>::kJ, kStage = Tile<T, G>::kStage, kScales = Tile<T, G>::kScales, kChunk = Tile<T, G>::kChunk;
   extern __shared__ __align__(1024) uint8_t all_smem[];
   const int lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = all_wave / Tile<T, G>::kWaves, wave = all_wave % Tile<T, G>::kWaves;
   uint8_t *const smem = all_smem + group * 2 * kStage;  // the group's
-  uint8_t *const scales = all_smem + G * 2 * kStage + group * 2 * kScales;
-  float *const vectors = (float *)(all_smem + G * 2 * (kStage + kScales));  // [2]: bias, row_scale of the tile
+  uint8_t *const scales = all_smem + G * 2 * kStage;    // two chunks
+  float *const vectors = (float *)(scales + 2 * kChunk);  // [2]: bias, row_scale of the tile
   const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T, G>::kWM, row = lane & 31, half = lane >> 5;
   const int tiles_m = cut.tiles_m, tiles_n = cut.tiles_n;
   const int b_at = (int)blockIdx.y * cut.per, b_end = min(a.blocks, b_at + cut.per);  // blocks of k
@@ -190,24 +176,28 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       }
     }
   };
-  // The scales of 8 blocks from b0 on: of 32 rows of each operand per wave, or of a row per thread.
+  // T = 256: the scales of a stage from block b0 on, of 32 rows of each operand per wave, to chunk `to`.  T = 128: of two stages of
+  // each group, 16 bytes per thread; the first stage's go to LDS with the stage at hand, the second's with the one behind it.
   constexpr bool kPacked = T == 256;
-  u32x2 held;
-  auto load_scales = [&](int b0, int buf) {
+  const int scale_row = threadIdx.x / G, scale_part = threadIdx.x % G;
+  i32x4 held;
+  auto load_scales = [&](int b0, int to) {
     if constexpr (kPacked) {
       const int stages = (a.blocks + HB - 1) / HB, at = b0 * 256 + wave * 256 + lane * 4;
-      uint8_t *to = scales + buf * kScales + wave * 256;
-      copy_4(a.ws + (int64_t)(n0 / T) * stages * (256 * HB) + at, to);
-      copy_4(a.ws + (tiles_n + m0 / T) * stages * (256 * HB) + at, to + T * HB);
-      return;
+      uint8_t *e = scales + to * kChunk + wave * 256;
+      copy_4(a.ws + (int64_t)(n0 / T) * stages * (256 * HB) + at, e);
+      copy_4(a.ws + (tiles_n + m0 / T) * stages * (256 * HB) + at, e + T * HB);
+    } else {
+      const int r = scale_row;
+      held = load16(r < T ? a.w_scale + (int64_t)(n0 + min(r, rows_w - 1)) * a.ld_ew
+                          : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex,
+                    b0 + scale_part * 2 * HB, b_end);
     }
-    const int r = threadIdx.x % (Tile<T, G>::kThreads / G);
-    held = load8(r < T ? a.w_scale + (int64_t)(n0 + min(r, rows_w - 1)) * a.ld_ew
-                       : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex,
-                 b0, b_end);
   };
-  auto store_scales = [&](int buf) {
-    if constexpr (!kPacked) *(u32x2 *)(scales + buf * kScales + threadIdx.x % (Tile<T, G>::kThreads / G) * HB) = held;
+  auto store_scales = [&](int to, int second) {
+    if constexpr (!kPacked)
+      *(u32x2 *)(scales + to * kChunk + (2 * scale_part + second) * kScales + scale_row * HB) =
+          second ? u32x2{(unsigned)held[2], (unsigned)held[3]} : u32x2{(unsigned)held[0], (unsigned)held[1]};
   };
   auto copy_vectors = [&](int which) {
     if constexpr (!SUMS) {
@@ -231,8 +221,9 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
 #pragma unroll
     for (int j = 0; j < J; ++j) fx[slot][j] = *(const i32x4 *)(x + j * 32 * HK + p);
   };
-  auto read_scales = [&](int buf) {
-    const uint8_t *w = scales + buf * kScales + (wn + row) * HB + half * 4, *x = w + (T + wm - wn) * HB;
+  auto read_scales = [&](int chunk, int second) {
+    const uint8_t *w = scales + chunk * kChunk + (second * G + group) * kScales + (wn + row) * HB + half * 4;
+    const uint8_t *x = w + (T + wm - wn) * HB;
 #pragma unroll
     for (int i = 0; i < I; ++i) sw_next[i] = *(const int *)(w + i * 32 * HB);
 #pragma unroll
@@ -317,17 +308,19 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
 
   const int b_first = b_at + group * HB;
   go_to(tile);
+  load_scales(b_at, 0);
   copy(b_first, 0);
-  load_scales(b_first, 0);
-  store_scales(0);
+  store_scales(0, 0);
+  store_scales(0, 1);
   copy_vectors(0);
   __syncthreads();
-  int buf = 0, which = 0;
+  int buf = 0, which = 0, chunk = 0;
   while (true) {
     const int n_at = n0, next = tile + stride;
     const int64_t m_at = m0;
+    int second = 0;  // whether the stage at hand is the second of its chunk (T = 128)
     read(buf, 0, 0);
-    read_scales(buf);
+    read_scales(chunk, 0);
     take_scales();
     auto three_steps = [&] {
       read(buf, 1, 1);
@@ -339,23 +332,31 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       read(buf, 3, 1);
       multiply(std::integral_constant<int, 2>{});
       interleave();
-      store_scales(buf ^ 1);  // also where no stage follows: a branch here would keep the reads above from their places
-      __syncthreads();        // the next stage has arrived, and this one has been read
+      store_scales(chunk ^ 1, second);  // also where no stage follows: a branch here would keep the reads above from their places
     };
     // stages that are past the end for a group have no scales: their products vanish
     for (int b = b_at; b + G * HB < b_end; b += G * HB) {
-      load_scales(b + (G + group) * HB, buf ^ 1);
+      if constexpr (kPacked) load_scales(b + HB, chunk ^ 1);
+      else if (!second) load_scales(b + 2 * G * HB, 0);
       copy(b + (G + group) * HB, buf ^ 1);
       three_steps();
+      __syncthreads();  // the next stage has arrived, and this one has been read
       buf ^= 1;
+      if constexpr (kPacked) {
+        chunk ^= 1;
+      } else {
+        chunk ^= second;
+        second ^= 1;
+      }
       read(buf, 0, 0);
-      read_scales(buf);
+      read_scales(chunk, second);
       multiply(std::integral_constant<int, 3>{});
       interleave();
       take_scales();
     }
     if constexpr (G == 2) {
       three_steps();
+      __syncthreads();
       multiply(std::integral_constant<int, 3>{});
       // each group keeps half of the rows, and takes the other's sums of them
       f32x16 kept[I][1];
@@ -388,11 +389,13 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
       if (next < end) {
         go_to(next);
-        load_scales(b_at, buf ^ 1);
+        load_scales(b_at, chunk ^ 1);
         copy(b_at, buf ^ 1);
         copy_vectors(which ^ 1);
       }
       three_steps();
+      store_scales(chunk ^ 1, second ^ 1);
+      __syncthreads();
       multiply(std::integral_constant<int, 3>{});
       write(smem + buf * kStage + wave * 8192, vectors + which * 2 * T, n_at, m_at, wm, acc);
       if (next >= end) break;
@@ -402,6 +405,7 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
         for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
       tile = next;
       buf ^= 1;
+      chunk ^= 1;
       which ^= 1;
       // the LDS just used may be copied over now; the results on their way out are not waited for
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
