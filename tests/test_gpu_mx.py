@@ -311,7 +311,52 @@ def test_product(M, N, blocks, dtype):
     check_product(x, ex, w, ew, dtype, row_scale=randn(3, M), bias=10 * randn(4, N))
 
 
-@pytest.mark.parametrize("M,N,blocks", [(1, 300, 40), (20, 500, 33), (70, 200, 65), (300, 600, 128), (2050, 2100, 36)])
+def large_tiles(M, N, blocks):
+    """Whether a product runs in tiles of 256: they alone have the scales of both operands rearranged in the workspace."""
+    return ops._bytes("fwg_matmul_mx_workspace", M, N, blocks) == (-(-M // 256) + -(-N // 256)) * 256 * -(-blocks // 8) * 8
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,blocks,large", [
+    (4000, 4096, 100, True),   # one tile a block, rows of whole lines, the last stage half full
+    (8200, 8192, 33, True),    # five tiles a block, the last stage one block of eight
+    (3900, 4093, 128, True),   # rows at odd elements
+    (8000, 8100, 40, True),    # four tiles a block, a column of tiles nearly empty
+    (2304, 6000, 61, True),
+    (2700, 3900, 13, False),   # two small tiles a block: two stages, three, four
+    (3000, 3900, 20, False),
+    (2000, 4400, 28, False),
+])
+def test_product_many_tiles(M, N, blocks, large, dtype):
+    assert large_tiles(M, N, blocks) == large
+    x, ex = random_rows(M + 1, M, blocks, 2)
+    w, ew = random_rows(N + 8, N, blocks, 2)
+    got = check_product(x, ex, w, ew, dtype, row_scale=randn(3, M), bias=10 * randn(4, N))
+    again = ops.matmul_mx(x, ex, w, ew, row_scale=randn(3, M), bias=10 * randn(4, N), dtype=dtype)
+    assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("M,N,blocks", [(4000, 4000, 64), (3900, 4090, 100), (3000, 3900, 20)])
+def test_product_many_tiles_of_views(M, N, blocks):
+    """Operands, scales and results in wider arrays, at odd addresses; NaN and zero blocks; one row for all."""
+    x, ex = random_rows(5, M, blocks, 2)
+    w, ew = random_rows(6, N, blocks, 2)
+    x[7], ex[7] = 0, 0
+    x[M - 1, -16:], ex[M - 1, blocks - 1] = 0, 255
+    w[N // 2, :16], ew[N // 2, 0] = 0, 255
+    bias, f = randn(7, N), randn(8, M)
+    for at in (1, 16):
+        for dtype in TYPES:
+            wide = torch.full((M, N + 9), 7.0, dtype=dtype, device="cuda")
+            got = check_product(odd_view(x, at, 48), odd_view(ex, 1, 2), odd_view(w, at, 32), odd_view(ew, 2, 7), dtype, f, bias,
+                                out=wide[:, 3:3 + N])
+            assert bool((wide[:, :3] == 7).all()) and bool((wide[:, 3 + N:] == 7).all())
+            assert int(torch.isnan(got).sum()) == M + N - 1
+    check_product(x[:1].expand(M, -1), ex[:1].expand(M, -1), w, ew, F32)
+
+
+@pytest.mark.parametrize("M,N,blocks", [(1, 300, 40), (20, 500, 33), (70, 200, 65), (300, 600, 128), (2050, 2100, 36),
+                                        (4000, 4000, 70)])
 def test_product_wide_scales(M, N, blocks):
     """Scales 2^30 apart."""
     x, ex = random_rows(1, M, blocks, 30)
@@ -545,6 +590,39 @@ def test_adjust_rows_past_four_gigabytes():
     ops.adjust_logits(z, out=out, **kw)
     ok = (out[590:].double() == want) | ((out[590:].double() - want).abs() <= 2.0 ** -8 * (want.abs() + bar) + bar)
     assert bool(ok.all())
+
+
+# ---- what only large calls reach ----
+
+def test_outputs_past_the_caches():
+    """Outputs of 192 MB and more are stored another way: the same rows as in small calls."""
+    x, res, gain = randn(1, 15000, 8001), randn(2, 15000, 8001), 1 + 0.1 * randn(3, 8001)
+    big = ops.quant_mx(x, values=True)
+    norm = ops.norm_mx(x, gain, residual=res, values=True)
+    for r in (slice(0, 40), slice(7000, 7033), slice(14990, 15000)):
+        for a, b in zip(big, check_rows(x[r])):
+            assert torch.equal(a[r], b)
+        for a, b in zip(norm, check_norm(x[r], gain, res[r], 1e-6)):
+            assert torch.equal(a[r], b)
+
+
+def test_more_rows_than_one_launch_takes():
+    n = (1 << 23) + 5
+    x = randn(1, n, 3)
+    big, norm = ops.quant_mx(x), ops.norm_mx(x)
+    small = n // 4 + 9
+    z, tokens = x[:small], ints(2, -1, 4, small, 2)
+    presence, allowed = rand(3, small), torch.randint(0, 8, (small, 1), device="cuda", dtype=torch.int32)
+    out = ops.adjust_logits(z, tokens, presence=presence, allowed=allowed)
+    for r in (slice(0, 50), slice(n - 40, n), slice((1 << 22) - 10, (1 << 22) + 10)):
+        part = check_rows(x[r])
+        assert torch.equal(big.q[r], part.q) and torch.equal(big.scale[r], part.scale)
+        part = check_norm(x[r], None, None, 1e-6)
+        assert torch.equal(norm.q[r], part.q) and torch.equal(norm.row_scale[r], part.row_scale)
+    for r in (slice(0, 50), slice(small - 40, small), slice((1 << 21) - 10, (1 << 21) + 10)):
+        want, bar = plain_adjust(z[r], tokens=tokens[r], presence=presence[r], allowed=allowed[r])
+        d = out[r].double()
+        assert bool(((d == want) | ((d - want).abs() <= bar)).all())
 
 
 # ---- together, on other streams, in graphs ----
