@@ -10,6 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libfwg.so")
+MARSHAL, MARSHAL_SOURCE = os.path.join(PKG, "_marshal.so"), os.path.join(CSRC, "fwg_marshal.cpp")  # a module of ops.py
 SOURCES = [os.path.join(CSRC, "fwg_host.cpp"), os.path.join(CSRC, "fwg_kernels.hip"),
            os.path.join(CSRC, "fwg_mfma.hip"), os.path.join(CSRC, "fwg_parallel.hip"),
            os.path.join(CSRC, "fwg_parstack.hip"), os.path.join(CSRC, "fwg_parhead.hip"),
@@ -47,14 +48,31 @@ def _run(cmd, verbose):
         raise RuntimeError("hipcc failed: " + " ".join(cmd[-3:]))
 
 
+def build_marshal(verbose: bool = False) -> None:
+    """Compile the module _marshal against this Python's torch (host code only); without torch there is nothing to marshal."""
+    import sysconfig
+    try:
+        import torch
+        from torch.utils.cpp_extension import include_paths, library_paths
+    except ImportError:
+        return
+    tmp = MARSHAL + ".tmp"
+    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + os.path.join(ROOT, "include"),
+          "-I" + sysconfig.get_paths()["include"]] + ["-isystem" + p for p in include_paths()] +
+         ["-o", tmp, MARSHAL_SOURCE] + ["-L" + p for p in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+    os.replace(tmp, MARSHAL)
+
+
 def build(verbose: bool = False) -> str:
     """Compile every source to an object (in parallel: each is one translation unit with its own
-    device code), then link libfwg.so."""
+    device code), then link libfwg.so; beside them the module _marshal."""
     os.makedirs(OBJDIR, exist_ok=True)
     objs = [os.path.join(OBJDIR, os.path.basename(src) + ".o") for src in SOURCES]
-    jobs = max(1, min(len(SOURCES), int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
+    jobs = max(1, min(len(SOURCES) + 1, int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
     with ThreadPoolExecutor(jobs) as ex:
-        for f in [ex.submit(_run, [HIPCC] + FLAGS + ["-c", "-o", o, src], verbose) for src, o in zip(SOURCES, objs)]:
+        for f in [ex.submit(_run, [HIPCC] + FLAGS + ["-c", "-o", o, src], verbose) for src, o in zip(SOURCES, objs)] + \
+                [ex.submit(build_marshal, verbose)]:
             f.result()
     tmp = LIB + ".tmp"
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs, verbose)
@@ -66,7 +84,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(s) > t for s in SOURCES + HEADERS)
+    return any(os.path.getmtime(s) > t for s in SOURCES + HEADERS + [MARSHAL_SOURCE])
 
 
 if __name__ == "__main__":

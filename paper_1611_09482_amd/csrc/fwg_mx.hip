@@ -10,7 +10,7 @@
 //
 // Bound by memory: 32,000 x 4,096 float32 to rows and values 142 us (6.0 TB/s; 147 with the outputs through the caches); 16,381
 // x 4,096 bf16 with residual, new residual, rows and values 105 us (5.5 TB/s; 110 through the caches).  64 x 4,096: the
-// kernels 3 and 5 us, the calls 7.2 and 9.0.
+// kernels 3 and 5 us, the calls 4.3 and 4.6.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

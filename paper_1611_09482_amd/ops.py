@@ -1,8 +1,9 @@
 """The token operators of libfwg.so (include/fwg.h) on torch tensors: embedding lookup and its gradient, rows in 8 or 4
 bits with or without RMS norm and their products, logits as requests want them, log probabilities and their gradient.
 
-Argument marshalling only, as in binding.py: every call checks its tensors, enqueues the library's kernels on the
-current stream of the current device and returns without waiting.  Matrices may have any number of leading
+Argument marshalling only, as in binding.py (for plain arguments of the 4-bit calls and adjust_logits in C++:
+csrc/fwg_marshal.cpp): every call checks its tensors, enqueues the library's kernels on the current stream of the
+current device and returns without waiting.  Matrices may have any number of leading
 dimensions as long as their rows lie evenly apart (views of consecutive rows, every n-th row, expanded rows as
 inputs); elements of a row are consecutive.  Nothing is copied to make an argument fit: what does not fit is
 refused (TypeError, ValueError; sizes that the library refuses raise FwgError).  `out` takes the results' tensors
@@ -20,14 +21,24 @@ import torch
 
 from .binding import FWG_BF16, FWG_EINVAL, FWG_EUNSUPPORTED, FWG_F32, FwgError, _check, load_library
 
+try:
+    from . import _marshal  # the checks of plain arguments in C++, where the host's time counts (csrc/fwg_marshal.cpp)
+except ImportError:
+    _marshal = None
+
 _TYPES = {torch.float32: FWG_F32, torch.bfloat16: FWG_BF16}
 _lib = None
+_plain = None  # _marshal once it knows the library's entries
 
 
 def _library():
-    global _lib
+    global _lib, _plain
     if _lib is None:
         _lib = load_library()
+        if _marshal is not None:
+            _marshal.bind(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
+                "fwg_quant_mx", "fwg_norm_mx", "fwg_matmul_mx_workspace", "fwg_matmul_mx", "fwg_adjust_logits")))
+            _plain = _marshal
     return _lib
 
 
@@ -321,12 +332,20 @@ def quant_mx(x, values: bool = False, out=None) -> MxRows:
     For weights [outputs][inner] these are matmul_mx's w and w_scale.  out: an MxRows or the three tensors (None: no
     values).  No part of autograd: rounding to 4 bits has no gradient."""
     dev = _device()
+    if out is None:
+        _matrix("x", x, dev)
+        qshape, eshape = _mx_shapes(x.shape)
+        out = MxRows(torch.empty(qshape, dtype=torch.uint8, device=x.device),
+                     torch.empty(eshape, dtype=torch.uint8, device=x.device),
+                     torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
+    if _plain is not None:
+        rc = _plain.quant_mx(dev, _stream(dev), x, *out)
+        if rc is not None:
+            if rc:
+                _check(rc)
+            return out if isinstance(out, MxRows) else MxRows(*out)
     kind, rows, width, stride = _matrix("x", x, dev)
     qshape, eshape = _mx_shapes(x.shape)
-    if out is None:
-        out = MxRows(torch.empty(qshape, dtype=torch.uint8, device=x.device),
-                      torch.empty(eshape, dtype=torch.uint8, device=x.device),
-                      torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
     q, scale, vals = out
     qp, qstride = _like("out.q", q, torch.uint8, qshape, dev, True)
     ep, estride = _like("out.scale", scale, torch.uint8, eshape, dev, True)
@@ -343,16 +362,24 @@ def norm_mx(x, gain=None, residual=None, eps: float = 1e-6, values: bool = False
     residual only) and, where values is true, `values` (the norm in bfloat16).  out: a NormMx or the five tensors (None: not
     wanted); out's `summed` may be x or residual itself.  No part of autograd: rounding to 4 bits has no gradient."""
     dev = _device()
+    if out is None:
+        _matrix("x", x, dev)
+        qshape, eshape = _mx_shapes(x.shape)
+        out = NormMx(torch.empty(qshape, dtype=torch.uint8, device=x.device),
+                     torch.empty(eshape, dtype=torch.uint8, device=x.device),
+                     torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device),
+                     None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device),
+                     torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if values else None)
+    if _plain is not None:
+        rc = _plain.norm_mx(dev, _stream(dev), x, gain, residual, eps, *out)
+        if rc is not None:
+            if rc:
+                _check(rc)
+            return out if isinstance(out, NormMx) else NormMx(*out)
     kind, rows, width, stride = _matrix("x", x, dev)
     shape, dtype = x.shape, x.dtype
-    rp, rstride = (None, 0) if residual is None else _like("residual", residual, dtype, shape, dev)
     qshape, eshape = _mx_shapes(shape)
-    if out is None:
-        out = NormMx(torch.empty(qshape, dtype=torch.uint8, device=x.device),
-                      torch.empty(eshape, dtype=torch.uint8, device=x.device),
-                      torch.empty(shape[:-1], dtype=torch.float32, device=x.device),
-                      None if residual is None else torch.empty(shape, dtype=dtype, device=x.device),
-                      torch.empty(shape, dtype=torch.bfloat16, device=x.device) if values else None)
+    rp, rstride = (None, 0) if residual is None else _like("residual", residual, dtype, shape, dev)
     q, scale, row_scale, summed, vals = out
     qp, qstride = _like("out.q", q, torch.uint8, qshape, dev, True)
     ep, estride = _like("out.scale", scale, torch.uint8, eshape, dev, True)
@@ -370,6 +397,18 @@ def matmul_mx(x, x_scale, w, w_scale, row_scale=None, bias=None, dtype=torch.bfl
     x: uint8 [..., 16 blocks] with x_scale uint8 [..., blocks]; w: uint8 [outputs][16 blocks] with w_scale uint8
     [outputs][blocks]; row_scale: float32 [...]; bias: float32 [outputs].  out: [..., outputs] of dtype (float32 or bfloat16)."""
     dev = _device()
+    if out is None:
+        _typed("x", x, torch.uint8, dev)
+        _typed("w", w, torch.uint8, dev)
+        _rows("x", x)
+        _flat("w", w)
+        out = torch.empty(x.shape[:-1] + (w.shape[0],), dtype=dtype, device=x.device)
+    if _plain is not None:
+        rc = _plain.matmul_mx(dev, _stream(dev), x, x_scale, w, w_scale, row_scale, bias, out)
+        if rc is not None:
+            if rc:
+                _check(rc)
+            return out
     _typed("x", x, torch.uint8, dev)
     _typed("w", w, torch.uint8, dev)
     rows, width, stride = _rows("x", x)
@@ -385,11 +424,8 @@ def matmul_mx(x, x_scale, w, w_scale, row_scale=None, bias=None, dtype=torch.bfl
     lead = x.shape[:-1]
     xe, xestride = _like("x_scale", x_scale, torch.uint8, lead + (blocks,), dev)
     we, westride = _like("w_scale", w_scale, torch.uint8, (outputs, blocks), dev)
-    shape = lead + (outputs,)
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=x.device)
     okind, _, _, ostride = _matrix("out", out, dev, True)
-    _shaped("out", out, shape)
+    _shaped("out", out, lead + (outputs,))
     need = _bytes("fwg_matmul_mx_workspace", rows, outputs, blocks)
     ws = _workspace(need)
     _check(_library().fwg_matmul_mx(okind, rows, outputs, blocks, x.data_ptr(), stride, xe, xestride, w.data_ptr(), wstride,
@@ -433,10 +469,18 @@ def adjust_logits(logits, tokens=None, lengths=None, prompts=None, repetition=No
     (int32 [words] or [..., words], words = ceil(vocab / 32), token v in bit v % 32 of word v // 32) is 0 the logit becomes
     -inf.  -inf stays -inf.  out: of the logits' shape and type; may be the logits themselves.  No part of autograd."""
     dev = _device()
+    if out is None:
+        _matrix("logits", logits, dev)
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if _plain is not None:
+        rc = _plain.adjust_logits(dev, _stream(dev), logits, tokens, lengths, prompts, repetition, presence, frequency, bias,
+                                  allowed, out)
+        if rc is not None:
+            if rc:
+                _check(rc)
+            return out
     kind, rows, vocab, stride = _matrix("logits", logits, dev)
     lead = logits.shape[:-1]
-    if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     op, ostride = _like("out", out, logits.dtype, logits.shape, dev, True)
     if tokens is None:
         if not (lengths is None and prompts is None and repetition is None and presence is None and frequency is None):

@@ -783,3 +783,89 @@ def test_example_continues_recordings():
     assert torch.equal(tokens[:, :40], classes) and tokens.shape == (5, 70)
     assert bool((tokens >= 0).all()) and bool((tokens < example.CLASSES).all())
     assert int((tokens[:, 40:] - tokens[:, 39:-1]).abs().max()) <= 16  # as the grammar says
+
+
+# ---- plain arguments, marshalled in C++, and the others ----
+
+def both_ways(monkeypatch, call):
+    """The call's results by either way of marshalling, as copies."""
+    ops.quant_mx(randn(1, 2, 32))  # the library is loaded
+    assert ops._plain is not None
+    fast = [None if t is None else t.clone() for t in call()]
+    with monkeypatch.context() as m:
+        m.setattr(ops, "_plain", None)
+        slow = [None if t is None else t.clone() for t in call()]
+    return fast, slow
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lead", [(7,), (2, 3), (), (0,), (300,)])
+def test_either_way_of_marshalling(lead, dtype, monkeypatch):
+    n, D, V, H = math.prod(lead), 200, 600, 9
+    x, res, gain = randn(1, *lead, D).to(dtype), randn(2, *lead, D).to(dtype), 1 + 0.1 * randn(3, D)
+    w = ops.quant_mx(randn(4, V, D))
+    bias, f = randn(5, V), randn(6, *lead)
+    new = lambda kind, *shape: torch.zeros(lead + shape, dtype=kind, device="cuda")  # noqa: E731
+    u8 = torch.uint8
+    packed = (new(u8, 112), new(u8, 7))
+    z = randn(7, *lead, V).to(dtype)
+    kw = {k: v.view(lead + v.shape[1:]) if v.shape[:1] == (max(n, 1),) and n else v for k, v in request(8, max(n, 1), V, H).items()}
+    if not n:
+        kw = {k: v[:0] for k, v in kw.items()}
+    some = dict(tokens=kw["tokens"], presence=kw["presence"], allowed=randn(9, 19).view(torch.int32))
+    for call in (
+        lambda: ops.quant_mx(x, out=packed + (new(BF16, D),)),
+        lambda: ops.quant_mx(x, out=packed + (None,)),
+        lambda: ops.norm_mx(x, gain, residual=res, eps=1e-5, out=packed + (new(F32), new(dtype, D), new(BF16, D))),
+        lambda: ops.norm_mx(x, out=packed + (new(F32), None, None)),
+        lambda: [ops.matmul_mx(packed[0], packed[1], w.q, w.scale, row_scale=f, bias=bias, out=new(dtype, V))],
+        lambda: [ops.matmul_mx(packed[0], packed[1], w.q, w.scale, out=new(F32, V))],
+        lambda: [ops.adjust_logits(z, out=new(dtype, V), **kw)],
+        lambda: [ops.adjust_logits(z, out=new(dtype, V), **some)],
+        lambda: [ops.adjust_logits(z, bias=bias, out=new(dtype, V))],
+    ):
+        for a, b in zip(*both_ways(monkeypatch, call)):
+            assert (a is None and b is None) or (a.shape == b.shape and same(a, b))
+
+
+def test_refusals_either_way(monkeypatch):
+    """What one way refuses the other refuses with the same error."""
+    x, f = randn(1, 4, 64), torch.zeros(4, device="cuda")
+    r = ops.quant_mx(x, values=True)
+    n = ops.norm_mx(x)
+    z, tok, o = randn(2, 4, 6), ints(3, 0, 6, 4, 5), torch.zeros((4, 4), device="cuda")
+    calls = [
+        lambda: ops.quant_mx(x, out=(r.q, r.scale)), lambda: ops.quant_mx(x, out=(r.q, r.scale, r.values.float())),
+        lambda: ops.quant_mx(x, out=(r.q[:2], r.scale, None)), lambda: ops.quant_mx(x.cpu(), out=r),
+        lambda: ops.quant_mx(x, out=(r.q.cpu(), r.scale, None)), lambda: ops.quant_mx(3, out=r),
+        lambda: ops.norm_mx(x, eps=-1.0, out=n), lambda: ops.norm_mx(x, eps=math.nan, out=n), lambda: ops.norm_mx(x, f, out=n),
+        lambda: ops.norm_mx(x, residual=x[:1], out=n), lambda: ops.norm_mx(x, out=n._replace(row_scale=f[:3])),
+        lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale[:3], out=o), lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale, out=o[:3]),
+        lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale, bias=f[:2], out=o),
+        lambda: ops.matmul_mx(r.q, r.scale, r.q, r.scale, out=o.half()),
+        lambda: ops.matmul_mx(r.q[:, :24].contiguous(), r.scale, r.q, r.scale, out=o),
+        lambda: ops.adjust_logits(z, presence=f, out=z), lambda: ops.adjust_logits(z, tok[:3], presence=f, out=z),
+        lambda: ops.adjust_logits(z, tok, presence=f[:3], out=z), lambda: ops.adjust_logits(z, tok.long(), presence=f, out=z),
+        lambda: ops.adjust_logits(z, bias=f, out=z), lambda: ops.adjust_logits(z, out=z.to(BF16)),
+        lambda: ops.adjust_logits(z, allowed=tok[:, :2].contiguous(), out=z), lambda: ops.adjust_logits(z, out=z[:3]),
+    ]
+    for i, call in enumerate(calls):
+        seen = []
+        for way in (ops._plain, None):
+            with monkeypatch.context() as m:
+                m.setattr(ops, "_plain", way)
+                try:
+                    call()
+                    seen.append(None)
+                except Exception as e:
+                    seen.append((type(e), str(e)))
+        assert seen[0] is not None and seen[0] == seen[1], (i, seen)
+
+
+def test_views_and_parameters_reach_the_thorough_checks():
+    x = torch.nn.Parameter(randn(1, 6, 96))
+    want = ops.quant_mx(x.detach(), values=True)
+    out = ops.quant_mx(x, out=tuple(t.clone() for t in want))
+    view = ops.quant_mx(odd_view(x.detach()), out=tuple(odd_view(t) for t in want))
+    for a, b, c in zip(want, out, view):
+        assert torch.equal(a, b) and torch.equal(a, c)
