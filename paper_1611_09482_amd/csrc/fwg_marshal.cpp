@@ -155,7 +155,7 @@ PyObject *matmul_mx(PyObject *, PyObject *const *a, Py_ssize_t n) try {
   const at::Tensor *x = plain(a[2], take.device), *w = plain(a[4], take.device), *out = take.rows(a[8], &kind);
   if (!x || !w || !out || x->scalar_type() != at::kByte || w->scalar_type() != at::kByte || x->dim() < 1 || w->dim() != 2) Py_RETURN_NONE;
   const int64_t bytes = x->sizes().back(), outputs = w->size(0), blocks = bytes / 16;
-  if (bytes < 16 || bytes % 16 || w->size(1) != bytes || outputs > kMost || !same_lead(*x, *out, outputs)) Py_RETURN_NONE;
+  if (bytes < 16 || bytes > kMost || bytes % 16 || w->size(1) != bytes || outputs > kMost || !same_lead(*x, *out, outputs)) Py_RETURN_NONE;
   const int64_t rows = x->numel() / bytes;
   auto *xs = (const uint8_t *)take.like(a[3], at::kByte, x, blocks), *ws = (const uint8_t *)take.like(a[5], at::kByte, w, blocks);
   auto *row_scale = (const float *)take.vector(a[6], at::kFloat, rows, true);

@@ -36,6 +36,11 @@ int check_stride(const char *name, int64_t stride, int64_t least) {
   if (stride > ((int64_t)1 << 40)) return fail(FWG_EUNSUPPORTED, "%s is %lld: at most 2^40 is supported", name, (long long)stride);
   return FWG_OK;
 }
+// An output that starts where an input does is the input itself, row for row.
+int check_itself(const char *name, const void *out, int64_t out_stride, const void *in, int64_t in_stride, int64_t rows) {
+  if (out != in || out_stride == in_stride || rows <= 1) return FWG_OK;
+  return fail(FWG_EINVAL, "%s: %lld at the address of an input whose stride is %lld", name, (long long)out_stride, (long long)in_stride);
+}
 int check_workspace(size_t need, const void *ws, size_t bytes) {
   if (need == 0) return FWG_OK;
   if (!ws) return fail(FWG_EINVAL, "workspace is NULL: %zu bytes are needed", need);
@@ -127,6 +132,8 @@ int mx_impl(MxArgs a, int dtype, bool norm, void *hip_stream) {
   CHECK(check_ptr("scale", a.scale, 1));
   if (norm) CHECK(check_ptr("row_scale", a.row_scale, 4));
   if (a.values) CHECK(check_ptr("values", a.values, 2));
+  if (a.summed) CHECK(check_itself("summed_stride", a.summed, a.ld_s, a.x, a.ld_x, a.rows));
+  if (a.summed && a.residual) CHECK(check_itself("summed_stride", a.summed, a.ld_s, a.residual, a.ld_r, a.rows));
   const int64_t rows = a.rows, per = rows_per_launch(a.channels);
   for (int64_t r = 0; r < rows; r += per) {
     MxArgs b = a;
@@ -331,6 +338,7 @@ int fwg_adjust_logits(int32_t dtype, int64_t rows, int32_t vocab, const void *lo
   if (rows == 0) return FWG_OK;
   CHECK(check_ptr("logits", logits, size_of(dtype)));
   CHECK(check_ptr("out", out, size_of(dtype)));
+  CHECK(check_itself("out_stride", out, out_stride, logits, logits_stride, rows));
   if (past) CHECK(check_ptr("tokens", tokens, 4));
   if (lengths) CHECK(check_ptr("lengths", lengths, 4));
   if (prompts) CHECK(check_ptr("prompts", prompts, 4));

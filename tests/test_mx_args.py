@@ -72,6 +72,10 @@ CASES = [
     ("fwg_adjust_logits", dict(bias=FAKE + 1), EINVAL), ("fwg_adjust_logits", dict(bias_stride=-1), EINVAL),
     ("fwg_adjust_logits", dict(allowed=FAKE + 1), EINVAL), ("fwg_adjust_logits", dict(allowed_stride=-1), EINVAL),
     ("fwg_adjust_logits", dict(out=None), EINVAL), ("fwg_adjust_logits", dict(out_stride=69), EINVAL),
+    # written where an input of another stride is read: the input's later rows would be the output's
+    ("fwg_adjust_logits", dict(logits_stride=0), EINVAL), ("fwg_adjust_logits", dict(out_stride=71), EINVAL),
+    ("fwg_norm_mx", dict(x_stride=0), EINVAL), ("fwg_norm_mx", dict(x_stride=71, residual=2 * FAKE), EINVAL),
+    ("fwg_norm_mx", dict(residual_stride=0, x=2 * FAKE), EINVAL),
 ]
 
 
