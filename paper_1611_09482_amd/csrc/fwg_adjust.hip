@@ -33,11 +33,15 @@ __device__ __forceinline__ float quotient(float z, float r, float inv) {
   return size < 1e37f && size > 1e-30f ? q : z / r;
 }
 
-// THREADS threads per block, P pieces of eight logits per thread: the pieces of one k lie together.
-template <typename T, int THREADS, int P> __global__ void __launch_bounds__(THREADS) adjust_kernel(AdjustArgs a, int parts, int part) {
+// THREADS threads per block, P pieces of eight logits per thread: the pieces of one k lie together.  TOGETHER: the parts of a row
+// go to one XCD (blocks go to the eight in turn).
+template <typename T, int THREADS, int P, bool TOGETHER>
+__global__ void __launch_bounds__(THREADS) adjust_kernel(AdjustArgs a, int parts, int part) {
   __shared__ __align__(16) uint32_t count[THREADS * kE * P];
-  const int64_t r = blockIdx.x / parts;
-  const int v0 = (int)(blockIdx.x - r * parts) * part, n = min(part, a.vocab - v0);
+  const uint32_t one = TOGETHER ? blockIdx.x >> 3 : blockIdx.x, at = one / (uint32_t)parts;
+  const int64_t r = TOGETHER ? at * 8 + (blockIdx.x & 7) : at;
+  if (TOGETHER && r >= a.rows) return;
+  const int v0 = (int)(one - at * parts) * part, n = min(part, a.vocab - v0);
   const T *z = (const T *)a.logits + r * a.ld + v0;
   T *out = (T *)a.out + r * a.ld_o + v0;
   const float *bias = a.bias ? a.bias + r * a.ld_b + v0 : nullptr;
@@ -141,13 +145,21 @@ template <typename T, int THREADS, int P> hipError_t go(const AdjustArgs &a, hip
   constexpr int kMost = THREADS * kE * P;
   const int parts = (int)(((int64_t)a.vocab + kMost - 1) / kMost);
   const int part = (int)(((int64_t)a.vocab + parts - 1) / parts + 31) / 32 * 32;
-  hipLaunchKernelGGL((adjust_kernel<T, THREADS, P>), dim3((unsigned)(a.rows * parts)), dim3(THREADS), 0, s, a, parts, part);
+  // Together a row's history comes into one L2 alone.  64 rows of 131,072 with 16,381 tokens 17.5 us in turn, 16.9 together, but with
+  // 100 tokens 11.1 and 11.5; 190 rows with 1,000 tokens 29.0 and 27.6, in place 24.1 and 19.5; 2,000 rows of 12,000, two parts
+  // each, 37.1 and 38.1.
+  if (parts >= 4 && (a.rows >= 128 || (a.rows >= 32 && a.tokens && a.history >= 4096))) {
+    const dim3 grid((unsigned)((a.rows + 7) / 8 * 8 * parts));
+    hipLaunchKernelGGL((adjust_kernel<T, THREADS, P, true>), grid, dim3(THREADS), 0, s, a, parts, part);
+  } else {
+    hipLaunchKernelGGL((adjust_kernel<T, THREADS, P, false>), dim3((unsigned)(a.rows * parts)), dim3(THREADS), 0, s, a, parts, part);
+  }
   return hipGetLastError();
 }
 
 // Of 131,072 bf16 logits with histories of up to 1,000 tokens 190 rows took 37.0 us in parts of 8,192 by 1,024 threads, 30.5 by
 // 512, 37.6 by 256, and 35.7 in parts of 2,048 by 256; with 16,381 tokens, which every part reads, 44.7, 40.9, 52.4 and
-// 56.9.  2,048 rows of 256: 9.6 us in parts of 2,048 (the call), 12.2 in parts of 8,192.
+// 56.9 (all in turn).  2,048 rows of 256: 9.6 us in parts of 2,048 (the call), 12.2 in parts of 8,192.
 template <typename T> hipError_t run(const AdjustArgs &a, hipStream_t s) {
   return a.vocab <= 2048 ? go<T, 256, 1>(a, s) : go<T, 512, 2>(a, s);
 }

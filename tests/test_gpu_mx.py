@@ -579,6 +579,21 @@ def test_adjust_many_rows_and_shapes():
     check_adjust(z[:4], tokens=kw["tokens"][:4, :0], presence=kw["presence"][:4])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,V,H", [(128, 25000, 40), (133, 32769, 0), (32, 24577, 4096), (39, 50001, 4100), (31, 25000, 4100)])
+def test_adjust_rows_in_parts(rows, V, H, dtype):
+    """Rows of several parts, as many as the eight XCDs share evenly or not; guarded rows behind the last."""
+    z = (3 * randn(V, rows, V)).to(dtype)
+    kw = request(rows, rows, V, max(H, 1))
+    if H == 0:
+        kw = {k: kw[k] for k in ("bias", "allowed")}
+    want = check_adjust(z, **kw)
+    room = torch.full((rows + 8, V), 7.0, dtype=dtype, device="cuda")
+    room[:rows] = z
+    ops.adjust_logits(room[:rows], out=room[:rows], **kw)
+    assert same(room[:rows], want) and (room[rows:] == 7.0).all()
+
+
 def test_adjust_rows_past_four_gigabytes():
     V = 5000
     far = torch.empty((600, 1 << 22), dtype=BF16, device="cuda")
