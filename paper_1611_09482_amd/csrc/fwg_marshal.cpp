@@ -2,11 +2,12 @@
 //
 // A call of 4-bit rows or adjusted logits for few streams takes the device 3 to 7 us and took the host 7 to 9, of which 4 to 5
 // were the checks of ops.py, tensor by tensor.  Here the same checks read the tensors directly.  Only the plain case is taken:
-// torch.Tensor objects, dense and contiguous, on the current device, of the types and shapes that belong together, no
-// workspace.  Everything else is declined (None), and ops.py goes through its own checks, which take more layouts and say what is
+// torch.Tensor objects, dense and contiguous, on the current device, of the types and shapes that belong together.
+// Everything else is declined (None), and ops.py goes through its own checks, which take more layouts and say what is
 // wrong.  No device work happens here but what the C entries of fwg.h enqueue.
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "fwg.h"
@@ -161,12 +162,15 @@ PyObject *matmul_mx(PyObject *, PyObject *const *a, Py_ssize_t n) try {
   auto *row_scale = (const float *)take.vector(a[6], at::kFloat, rows, true);
   auto *bias = (const float *)take.vector(a[7], at::kFloat, outputs, true);
   size_t need = 0;
-  if (!take.fits || entries.matmul_workspace(rows, (int32_t)outputs, (int32_t)blocks, &need) != FWG_OK || need) Py_RETURN_NONE;
+  if (!take.fits || entries.matmul_workspace(rows, (int32_t)outputs, (int32_t)blocks, &need) != FWG_OK) Py_RETURN_NONE;
+  at::Tensor workspace;  // torch's allocator keeps it for this stream, as ops.py's
+  if (need) workspace = at::empty({(int64_t)need}, x->options());
+  void *const space = need ? workspace.data_ptr() : nullptr;
   auto *xp = (const uint8_t *)x->data_ptr(), *wp = (const uint8_t *)w->data_ptr();
   void *op = out->data_ptr();
   return enqueue([&] {
     return entries.matmul(kind, rows, (int32_t)outputs, (int32_t)blocks, xp, bytes, xs, blocks, wp, bytes, ws, blocks, row_scale,
-                          bias, op, outputs, nullptr, 0, stream);
+                          bias, op, outputs, space, need, stream);
   });
 } catch (...) {
   Py_RETURN_NONE;

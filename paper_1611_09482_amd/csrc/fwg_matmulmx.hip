@@ -65,9 +65,8 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
 }
 
 // Tiles of T outputs x T rows, eight blocks (256 elements, 128 bytes) of k per stage, two stages in LDS: one is filled while
-// the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows: eight waves for T = 256, four for 128.  G = 2: two groups
-// of so many waves take stages in turn, each with two of its own, and add their sums up at the end (333 x 8,000 x 4,096 in
-// 15.7 us, 18.3 with one group; but with two blocks on a compute unit 256 x 32,000 x 4,096 takes 30.7 with one, 36.3 with two).
+// the other is multiplied.  A wave multiplies 64 outputs x T / 2 rows: eight waves for T = 256, four for 128, where two blocks share a
+// compute unit.
 //
 // A step of a stage multiplies 64 elements: which of the stage's blocks they are is free as long as both operands agree, so lanes
 // 0 .. 31 hold block s at step s and lanes 32 .. 63 block 4 + s.  The scales of a lane's four blocks are then four
@@ -75,14 +74,14 @@ __device__ __forceinline__ void copy_16(const uint8_t *g, uint8_t *l) {
 //
 // A stage's scales are 8 bytes of each row, and reading them from the rows brings in whole lines.  Tiles of 256 find them
 // rearranged by stages (pack_kernel, 4 us in 8,192^3: 304 us from the rows, 274 so); those of 128 take 16 bytes for two
-// stages of each group at a time from the rows, through registers, which hold them at any address.
+// stages at a time from the rows, through registers, which hold them at any address.
 constexpr int HK = 128, HB = HK / 16;
-template <int T, int G> struct Tile {
-  static constexpr int kWaves = T / 32, kThreads = 64 * kWaves * G, kWM = T / 2, kJ = kWM / 32;  // kWaves: of a group
+template <int T> struct Tile {
+  static constexpr int kThreads = 2 * T, kWM = T / 2, kJ = kWM / 32;
   static constexpr int kStage = 2 * T * HK;      // bytes of a stage: weights, then rows
   static constexpr int kScales = 2 * T * HB;     // of a stage: weights', then rows'
-  static constexpr int kChunk = T == 256 ? kScales : 2 * G * kScales;  // of the stages whose scales come together
-  static constexpr int kLds = 2 * (G * kStage + kChunk) + 2 * 2 * T * (int)sizeof(float);
+  static constexpr int kChunk = T == 256 ? kScales : 2 * kScales;  // of the stages whose scales come together
+  static constexpr int kLds = 2 * (kStage + kChunk) + 2 * 2 * T * (int)sizeof(float);
 };
 
 // The 16-byte pieces of a stage's row r lie permuted, so that the 32 rows that an instruction reads at one k spread over the banks.
@@ -108,26 +107,20 @@ struct Cut {
   int tiles_m, tiles_n, splits, per;  // k is cut into `splits` parts of `per` blocks (a multiple of HB)
 };
 
-// ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without passing through registers.  SUMS: of a part of k,
-// to the workspace.  STREAM: results go past the caches, which then keep the operands: 4,093 x 32,000 x 4,096 278 us, 315 through
+// ALIGNED: rows start at multiples of 16 bytes and are copied to LDS without passing through registers.  STREAM: results go past the caches, which then keep the operands: 4,093 x 32,000 x 4,096 278 us, 315 through
 // them; with the log probabilities of the results behind it 340 and 350, of 1,024 rows 96.4 and 97.5.  Only where rows are whole
 // lines of 128 bytes: 2,176 x 10,920 x 4,096 takes 69.7 us so, 62.2 through the caches.
-template <typename TO, bool ALIGNED, bool SUMS, bool STREAM, int T, int G>
-__global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulMxArgs a, Cut cut) {
-  constexpr int I = 2, J = Tile<T, G>::kJ, kStage = Tile<T, G>::kStage, kScales = Tile<T, G>::kScales, kChunk = Tile<T, G>::kChunk;
-  extern __shared__ __align__(1024) uint8_t all_smem[];
-  const int lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = all_wave / Tile<T, G>::kWaves, wave = all_wave % Tile<T, G>::kWaves;
-  uint8_t *const smem = all_smem + group * 2 * kStage;  // the group's
-  uint8_t *const scales = all_smem + G * 2 * kStage;    // two chunks
+template <typename TO, bool ALIGNED, bool STREAM, int T> __global__ void __launch_bounds__(Tile<T>::kThreads, 2) tile_kernel(MatmulMxArgs a, Cut cut) {
+  constexpr int I = 2, J = Tile<T>::kJ, kStage = Tile<T>::kStage, kScales = Tile<T>::kScales, kChunk = Tile<T>::kChunk;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t *const scales = smem + 2 * kStage;              // two chunks
   float *const vectors = (float *)(scales + 2 * kChunk);  // [2]: bias, row_scale of the tile
-  const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T, G>::kWM, row = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = (wave >> 1) * 64, wm = (wave & 1) * Tile<T>::kWM, row = lane & 31, half = lane >> 5;
   const int tiles_m = cut.tiles_m, tiles_n = cut.tiles_n;
-  const int b_at = (int)blockIdx.y * cut.per, b_end = min(a.blocks, b_at + cut.per);  // blocks of k
-  TO *const result = (TO *)a.out + (SUMS ? (int64_t)blockIdx.y * a.M * a.ld_o : 0);
   // Each XCD (blocks go to the eight in turn) takes a contiguous share of the tiles, eight rows of tiles at a time;
   // its blocks go through the share together.
-  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = G == 1 ? gridDim.x >> 3 : share;
+  const int tiles = tiles_m * tiles_n, share = (tiles + 7) / 8, stride = gridDim.x >> 3;
   int tile = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
   const int end = min(tiles, (int)(blockIdx.x & 7) * share + share);
   if (tile >= end) return;
@@ -176,10 +169,9 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       }
     }
   };
-  // T = 256: the scales of a stage from block b0 on, of 32 rows of each operand per wave, to chunk `to`.  T = 128: of two stages of
-  // each group, 16 bytes per thread; the first stage's go to LDS with the stage at hand, the second's with the one behind it.
+  // T = 256: the scales of a stage from block b0 on, of 32 rows of each operand per wave, to chunk `to`.  T = 128: of two stages,
+  // 16 bytes per thread; the first stage's go to LDS with the stage at hand, the second's with the one behind it.
   constexpr bool kPacked = T == 256;
-  const int scale_row = threadIdx.x / G, scale_part = threadIdx.x % G;
   i32x4 held;
   auto load_scales = [&](int b0, int to) {
     if constexpr (kPacked) {
@@ -188,24 +180,21 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       copy_4(a.ws + (int64_t)(n0 / T) * stages * (256 * HB) + at, e);
       copy_4(a.ws + (tiles_n + m0 / T) * stages * (256 * HB) + at, e + T * HB);
     } else {
-      const int r = scale_row;
+      const int r = threadIdx.x;
       held = load16(r < T ? a.w_scale + (int64_t)(n0 + min(r, rows_w - 1)) * a.ld_ew
-                          : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex,
-                    b0 + scale_part * 2 * HB, b_end);
+                          : a.x_scale + (m0 + min(r - T, rows_x - 1)) * a.ld_ex, b0, a.blocks);
     }
   };
   auto store_scales = [&](int to, int second) {
     if constexpr (!kPacked)
-      *(u32x2 *)(scales + to * kChunk + (2 * scale_part + second) * kScales + scale_row * HB) =
+      *(u32x2 *)(scales + to * kChunk + second * kScales + threadIdx.x * HB) =
           second ? u32x2{(unsigned)held[2], (unsigned)held[3]} : u32x2{(unsigned)held[0], (unsigned)held[1]};
   };
   auto copy_vectors = [&](int which) {
-    if constexpr (!SUMS) {
-      const int t = threadIdx.x;
-      if (t < T) {
-        vectors[which * 2 * T + t] = a.bias ? a.bias[n0 + min(t, rows_w - 1)] : 0.f;
-        vectors[which * 2 * T + T + t] = a.row_scale ? a.row_scale[m0 + min(t, rows_x - 1)] : 1.f;
-      }
+    const int t = threadIdx.x;
+    if (t < T) {
+      vectors[which * 2 * T + t] = a.bias ? a.bias[n0 + min(t, rows_w - 1)] : 0.f;
+      vectors[which * 2 * T + T + t] = a.row_scale ? a.row_scale[m0 + min(t, rows_x - 1)] : 1.f;
     }
   };
 
@@ -222,7 +211,7 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
     for (int j = 0; j < J; ++j) fx[slot][j] = *(const i32x4 *)(x + j * 32 * HK + p);
   };
   auto read_scales = [&](int chunk, int second) {
-    const uint8_t *w = scales + chunk * kChunk + (second * G + group) * kScales + (wn + row) * HB + half * 4;
+    const uint8_t *w = scales + chunk * kChunk + second * kScales + (wn + row) * HB + half * 4;
     const uint8_t *x = w + (T + wm - wn) * HB;
 #pragma unroll
     for (int i = 0; i < I; ++i) sw_next[i] = *(const int *)(w + i * 32 * HB);
@@ -254,9 +243,8 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
 
   // Results: a wave's 64 outputs x T / 2 rows pass through 8 KB of LDS (of the stage that was multiplied last), 32 or 64
   // rows at a time, so that they go out in whole lines of 128 (bf16) or 256 bytes; pieces of 16 bytes are permuted by the row.
-  auto write = [&](uint8_t *mine, const float *vec, int n_at, int64_t m_at, int wm, const auto &acc) {
-    constexpr int kLine = 64 * (int)sizeof(TO), kPieces = kLine / 16;
-    constexpr int J = sizeof(acc[0]) / sizeof(f32x16), JP = sizeof(TO) == 2 && J > 1 ? 2 : 1, E = 16 / (int)sizeof(TO);
+  auto write = [&](uint8_t *mine, const float *vec, int n_at, int64_t m_at) {
+    constexpr int kLine = 64 * (int)sizeof(TO), kPieces = kLine / 16, JP = sizeof(TO) == 2 ? 2 : 1, E = 16 / (int)sizeof(TO);
     // places in LDS are worked out here: outside the loop over tiles they would hold 40 registers, more than there are left
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
@@ -269,19 +257,15 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int n = i * 32 + g * 8 + half * 4, at = n * (int)sizeof(TO);
-          f32x4 b;
-          if constexpr (!SUMS) b = *(const f32x4 *)(vec + wn + n);
+          const f32x4 b = *(const f32x4 *)(vec + wn + n);
 #pragma unroll
           for (int jj = 0; jj < JP; ++jj) {
             const int r = jj * 32 + row;
             uint8_t *to = mine + r * kLine + (((at >> 4) ^ (r & (kPieces - 1))) << 4) + (at & 15);
-            float v[4], f = 1.f;
-            if constexpr (!SUMS) f = vec[T + wm + (j0 + jj) * 32 + row];
+            const float f = vec[T + wm + (j0 + jj) * 32 + row];
+            float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[e] = acc[i][j0 + jj][4 * g + e];
-              if constexpr (!SUMS) v[e] = v[e] * f + b[e];
-            }
+            for (int e = 0; e < 4; ++e) v[e] = acc[i][j0 + jj][4 * g + e] * f + b[e];
             store_aligned((TO *)to, v);
           }
         }
@@ -294,7 +278,7 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
         const int64_t m = m_at + wm + j0 * 32 + r;
         const uint8_t *line = mine + r * kLine + ((p ^ (r & (kPieces - 1))) << 4);
         if (m >= a.M) continue;
-        TO *out = result + m * a.ld_o + n;
+        TO *out = (TO *)a.out + m * a.ld_o + n;
         if (n + E <= a.N) {
           if constexpr (STREAM) __builtin_nontemporal_store(*(const u32x4 *)line, (u32x4_el *)out);
           else *(u32x4_el *)out = *(const u32x4 *)line;
@@ -306,10 +290,9 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
     }
   };
 
-  const int b_first = b_at + group * HB;
   go_to(tile);
-  load_scales(b_at, 0);
-  copy(b_first, 0);
+  load_scales(0, 0);
+  copy(0, 0);
   store_scales(0, 0);
   store_scales(0, 1);
   copy_vectors(0);
@@ -334,11 +317,10 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       interleave();
       store_scales(chunk ^ 1, second);  // also where no stage follows: a branch here would keep the reads above from their places
     };
-    // stages that are past the end for a group have no scales: their products vanish
-    for (int b = b_at; b + G * HB < b_end; b += G * HB) {
+    for (int b = 0; b + HB < a.blocks; b += HB) {
       if constexpr (kPacked) load_scales(b + HB, chunk ^ 1);
-      else if (!second) load_scales(b + 2 * G * HB, 0);
-      copy(b + (G + group) * HB, buf ^ 1);
+      else if (!second) load_scales(b + 2 * HB, 0);
+      copy(b + HB, buf ^ 1);
       three_steps();
       __syncthreads();  // the next stage has arrived, and this one has been read
       buf ^= 1;
@@ -354,98 +336,313 @@ __global__ void __launch_bounds__((Tile<T, G>::kThreads), 2) tile_kernel(MatmulM
       interleave();
       take_scales();
     }
-    if constexpr (G == 2) {
-      three_steps();
-      __syncthreads();
-      multiply(std::integral_constant<int, 3>{});
-      // each group keeps half of the rows, and takes the other's sums of them
-      f32x16 kept[I][1];
-      auto give = [&](auto other) {
-        uint8_t *const to = all_smem + all_wave * 8192 + lane * 16;
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x16 &c = acc[i][decltype(other)::value];
-            *(f32x4 *)(to + (i * 4 + q) * 1024) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-          }
-#pragma unroll
-        for (int i = 0; i < I; ++i) kept[i][0] = acc[i][1 - decltype(other)::value];
-      };
-      if (group == 0) give(std::integral_constant<int, 1>{});
-      else give(std::integral_constant<int, 0>{});
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 v = *(const f32x4 *)(all_smem + (all_wave ^ 4) * 8192 + lane * 16 + (i * 4 + q) * 1024);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) kept[i][0][4 * q + e] += v[e];
-        }
-      write(all_smem + 65536 + all_wave * 8192, vectors, n_at, m_at, wm + group * 32, kept);
-      break;
-    } else {
-      // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
-      if (next < end) {
-        go_to(next);
-        load_scales(b_at, chunk ^ 1);
-        copy(b_at, buf ^ 1);
-        copy_vectors(which ^ 1);
-      }
-      three_steps();
-      store_scales(chunk ^ 1, second ^ 1);
-      __syncthreads();
-      multiply(std::integral_constant<int, 3>{});
-      write(smem + buf * kStage + wave * 8192, vectors + which * 2 * T, n_at, m_at, wm, acc);
-      if (next >= end) break;
-#pragma unroll
-      for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
-      tile = next;
-      buf ^= 1;
-      chunk ^= 1;
-      which ^= 1;
-      // the LDS just used may be copied over now; the results on their way out are not waited for
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    // the stages of all tiles are one stream: while a tile's last one is multiplied, the next tile's first is copied
+    if (next < end) {
+      go_to(next);
+      load_scales(0, chunk ^ 1);
+      copy(0, buf ^ 1);
+      copy_vectors(which ^ 1);
     }
+    three_steps();
+    store_scales(chunk ^ 1, second ^ 1);
+    __syncthreads();
+    multiply(std::integral_constant<int, 3>{});
+    write(smem + buf * kStage + wave * 8192, vectors + which * 2 * T, n_at, m_at);
+    if (next >= end) break;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) acc[i][j] = f32x16{};
+    tile = next;
+    buf ^= 1;
+    chunk ^= 1;
+    which ^= 1;
+    // the LDS just used may be copied over now; the results on their way out are not waited for
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   }
 }
 
-// Adds the parts of k up, in their order.
-template <typename TO> __global__ void __launch_bounds__(256) add_kernel(MatmulMxArgs a, int splits) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, all = a.M * a.N;
-  if (i >= all) return;
-  const float *sums = (const float *)a.ws;
-  if (i + 4 <= all && a.N % 4 == 0) {
-    f32x4 c = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) c += *(const f32x4 *)(sums + s * all + i);
-    const int64_t m = i / a.N;
-    const int n = (int)(i - m * a.N);
-    const float f = a.row_scale ? a.row_scale[m] : 1.f;
-    float v[4];
+// Where there are no more tiles of 128 x 128 than compute units: eight waves of 64 outputs x 32 rows, and a ring of four stages in
+// LDS, of which three are on their way while one is multiplied.  333 x 8,000 x 4,096 takes 13.2 us (two groups of four waves
+// with two stages each 15.9; four waves of 64 x 64 16.0), 128 x 8,192 x 4,096 11.6 (14.5), 16 x 32,000 x 4,096 to float32, which
+// memory bounds, 14.4 (4.9 TB/s).  A stage takes 0.5 us: its copies alone 0.44, its reads from LDS and products alone 0.41.
+// SUMS: of a part of k, to the workspace.
+constexpr int kRing = 4, kRingT = 128, kRingStage = 2 * kRingT * HK, kRingScales = 2 * kRingT * HB;
+constexpr int kRingLds = kRing * (kRingStage + 2 * kRingScales) + 2 * kRingT * (int)sizeof(float);
+
+template <typename TO, bool ALIGNED, bool SUMS>
+__global__ void __launch_bounds__(512, 2) ring_kernel(MatmulMxArgs a, Cut cut) {
+  constexpr int T = kRingT, I = 2;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t *const scales = smem + kRing * kRingStage;                   // two chunks, of four stages each
+  float *const vectors = (float *)(scales + 2 * kRing * kRingScales);  // bias, row_scale of the tile
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wn = (wave & 1) * 64, wm = (wave >> 1) * 32, row = lane & 31, half = lane >> 5;
+  const int b_at = (int)blockIdx.y * cut.per, b_end = min(a.blocks, b_at + cut.per);  // blocks of k
+  const int stages = (b_end - b_at + HB - 1) / HB;
+  const int tiles = cut.tiles_m * cut.tiles_n, share = (tiles + 7) / 8;
+  const int tile = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x >> 3);
+  if (tile >= min(tiles, (int)(blockIdx.x & 7) * share + share)) return;
+  constexpr int kBand = 8;
+  const int band = tile / (kBand * cut.tiles_n), in_band = tile - band * kBand * cut.tiles_n, high = min(kBand, cut.tiles_m - band * kBand);
+  const int n0 = in_band / high * T;
+  const int64_t m0 = (int64_t)(band * kBand + in_band % high) * T;
+  const uint8_t *const bw = a.w + n0 * a.ld_w, *const bx = a.x + m0 * a.ld_x;
+  const int rows_w = min(T, a.N - n0), rows_x = (int)min((int64_t)T, a.M - m0);
+
+  // A wave brings 16 rows of each operand, in two halves of 8 rows of 8 pieces; rows past the end are the last one, and so are
+  // blocks, as above.
+  const int cr = wave * 16 + (lane >> 3), piece = piece_of(cr, lane & 7) * 16, last = (a.blocks - 1) * 16;
+  i32x4 vw[2], vx[2];  // not ALIGNED: on their way
+  auto copy = [&](int t, int slot, int i) {
+    const int p = min((b_at + t * HB) * 16 + (i ? piece ^ 64 : piece), last), rw = min(cr + i * 8, rows_w - 1), rx = min(cr + i * 8, rows_x - 1);
+    if constexpr (ALIGNED) {
+      uint8_t *w = smem + slot * kRingStage + (wave * 16 + i * 8) * HK;
+      copy_16(bw + ((unsigned)rw * (unsigned)a.ld_w + p), w);  // below 2^31
+      copy_16(bx + ((unsigned)rx * (unsigned)a.ld_x + p), w + T * HK);
+    } else {
+      vw[i] = *(const i32x4_b *)(bw + rw * a.ld_w + p);
+      vx[i] = *(const i32x4_b *)(bx + rx * a.ld_x + p);
+    }
+  };
+  auto put_down = [&](int slot) {
+    if constexpr (!ALIGNED) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c[e] * f + (a.bias ? a.bias[n + e] : 0.f);
-    store((TO *)a.out + m * a.ld_o + n, v);
-    return;
+      for (int i = 0; i < 2; ++i) {
+        uint8_t *w = smem + slot * kRingStage + (wave * 16 + i * 8) * HK + lane * 16;
+        *(i32x4 *)w = vw[i];
+        *(i32x4 *)(w + T * HK) = vx[i];
+      }
+    }
+  };
+  // scales of four stages: 32 bytes of a row by two threads
+  const int scale_row = threadIdx.x >> 1, scale_part = threadIdx.x & 1;
+  const uint8_t *const scale_at = scale_row < T ? a.w_scale + (int64_t)(n0 + min(scale_row, rows_w - 1)) * a.ld_ew
+                                                : a.x_scale + (m0 + min(scale_row - T, rows_x - 1)) * a.ld_ex;
+  // 16 bytes that end with the part at the latest, `shift` bits too early; short rows have one chunk only, which load16 brings.
+  const bool wide = b_end >= 16;
+  i32x4 held;
+  int shift = 0;
+  auto load_scales = [&](int t) {
+    const int k = b_at + t * HB + scale_part * 2 * HB, from = min(k, b_end - 16);
+    held = *(const i32x4_b *)(scale_at + from);
+    shift = 8 * min(k - from, 16);
+  };
+  auto store_scales = [&](int chunk) {
+    const unsigned __int128 all = __builtin_bit_cast(unsigned __int128, held);
+    const i32x4 v = __builtin_bit_cast(i32x4, shift < 128 ? all >> shift : (unsigned __int128)0);
+    const u32x2 lo = {(unsigned)v[0], (unsigned)v[1]}, hi = {(unsigned)v[2], (unsigned)v[3]};
+    const auto to = (__attribute__((address_space(3))) uint8_t *)(scales + (chunk * kRing + 2 * scale_part) * kRingScales + scale_row * HB);
+    // the compiler holds its own stores to LDS back until every copy to LDS is there
+    asm volatile("ds_write_b64 %0, %1\n\tds_write_b64 %0, %2 offset:%3" ::"v"(to), "v"(lo), "v"(hi), "n"(kRingScales) : "memory");
+  };
+
+  f32x16 acc[I] = {};
+  i32x4 fw[2][I], fx[2];
+  int sw[I], sx, sw_next[I], sx_next;
+  auto read = [&](int slot, int step, int to) {
+    const uint8_t *w = smem + slot * kRingStage + (wn + row) * HK, *x = smem + slot * kRingStage + T * HK + (wm + row) * HK;
+    const int p = piece_of(row, 4 * half + step) * 16;
+#pragma unroll
+    for (int i = 0; i < I; ++i) fw[to][i] = *(const i32x4 *)(w + i * 32 * HK + p);
+    fx[to] = *(const i32x4 *)(x + p);
+  };
+  auto read_scales = [&](int chunk, int u) {
+    const uint8_t *w = scales + (chunk * kRing + u) * kRingScales + (wn + row) * HB + half * 4;
+#pragma unroll
+    for (int i = 0; i < I; ++i) sw_next[i] = *(const int *)(w + i * 32 * HB);
+    sx_next = *(const int *)(w + (T + wm - wn) * HB);
+  };
+  auto take_scales = [&] {
+#pragma unroll
+    for (int i = 0; i < I; ++i) sw[i] = sw_next[i];
+    sx = sx_next;
+  };
+  auto multiply = [&](auto step) {
+    constexpr int K = decltype(step)::value;
+#pragma unroll
+    for (int i = 0; i < I; ++i) acc[i] = mma<K>(fw[K & 1][i], fx[K & 1], acc[i], sw[i], sx);
+  };
+  // reads between the products
+  auto interleave = [] {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  };
+  // The next stage has arrived for all, and all have read the one at hand.  Of what a wave has asked for, `more` copies of later
+  // stages (four each) may be on their way: a fence would wait for them too.
+  auto arrive = [](auto more) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | decltype(more)::value);  // vmcnt, and lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // the stage in slot u but for its last step, while stage t + 3 is asked for
+  auto turn = [&](int u, bool ask, int t) {
+    const int to = (u + kRing - 1) % kRing;
+    read(u, 1, 1);
+    multiply(std::integral_constant<int, 0>{});
+    interleave();
+    if (ask) copy(t + kRing - 1, to, 0);
+    read(u, 2, 0);
+    multiply(std::integral_constant<int, 1>{});
+    interleave();
+    if (ask) copy(t + kRing - 1, to, 1);
+    read(u, 3, 1);
+    multiply(std::integral_constant<int, 2>{});
+    interleave();
+    if (ask) put_down(to);
+  };
+  // its last step, and what the next stage, number u of its chunk, begins with
+  auto pass = [&](int chunk, int u) {
+    read(u, 0, 0);
+    read_scales(chunk, u);
+    multiply(std::integral_constant<int, 3>{});
+    interleave();
+    take_scales();
+  };
+  const std::integral_constant<int, 8> two{};
+  const std::integral_constant<int, 4> one{};
+  const std::integral_constant<int, 0> none{};
+  auto fill = [&] {
+#pragma unroll
+    for (int t = 0; t < kRing - 1; ++t) {
+      copy(t, t, 0);
+      copy(t, t, 1);
+      put_down(t);
+    }
+  };
+
+  if constexpr (!SUMS) {
+    uint8_t *to = (uint8_t *)(vectors + wave * 64);
+    const int t = (wave & 1) * 64 + lane;
+    if (wave < 2) {
+      if (a.bias) copy_4((const uint8_t *)(a.bias + n0 + min(t, rows_w - 1)), to);
+      else vectors[t] = 0.f;
+    } else if (wave < 4) {
+      if (a.row_scale) copy_4((const uint8_t *)(a.row_scale + m0 + min(t, rows_x - 1)), to);
+      else vectors[T + t] = 1.f;
+    }
   }
-  for (int64_t e = i; e < i + 4 && e < all; ++e) {
-    float c = 0.f;
-    for (int s = 0; s < splits; ++s) c += sums[s * all + e];
-    const int64_t m = e / a.N;
-    const int n = (int)(e - m * a.N);
-    put((TO *)a.out + m * a.ld_o + n, c * (a.row_scale ? a.row_scale[m] : 1.f) + (a.bias ? a.bias[n] : 0.f));
+  if (wide) load_scales(0);
+  else held = load16(scale_at, scale_part * 2 * HB, b_end);
+  fill();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f7c);  // vmcnt(12): the scales
+  asm volatile("" ::: "memory");
+  asm volatile("" : "+v"(held));
+  store_scales(0);
+  arrive(two);
+  read(0, 0, 0);
+  read_scales(0, 0);
+  take_scales();
+  int t = 0, chunk = 0, slot = 0;
+  for (; t + kRing < stages; t += kRing, chunk ^= 1) {
+    load_scales(t + kRing);
+#pragma unroll
+    for (int u = 0; u < kRing; ++u) {
+      turn(u, true, t + u);
+      if (u == kRing - 1) store_scales(chunk ^ 1);
+      arrive(two);
+      pass(u == kRing - 1 ? chunk ^ 1 : chunk, (u + 1) % kRing);
+    }
   }
+  // the last chunk: the fourth stage's copies may be of a stage past the end
+  turn(0, true, t);
+  arrive(two);
+  if (t + 1 < stages) {
+    pass(chunk, 1);
+    turn(1, false, 0);
+    arrive(one);
+    slot = 1;
+    if (t + 2 < stages) {
+      pass(chunk, 2);
+      turn(2, false, 0);
+      arrive(none);
+      slot = 2;
+      if (t + 3 < stages) {
+        pass(chunk, 3);
+        turn(3, false, 0);
+        arrive(none);
+        slot = 3;
+      }
+    }
+  }
+  multiply(std::integral_constant<int, 3>{});
+
+  // Results go out in whole lines of 128 bytes: 64 (bf16) or 32 outputs x 32 rows at a time pass through 4 KB of LDS, of the
+  // stage that was multiplied last: the others may still be copied to.
+  constexpr int E = 16 / (int)sizeof(TO), kPasses = (int)sizeof(TO) / 2;
+  TO *const result = (TO *)a.out + (SUMS ? (int64_t)blockIdx.y * a.M * a.ld_o : 0);
+  uint8_t *const mine = smem + slot * kRingStage + wave * 4096;
+  float f = 1.f;
+  if constexpr (!SUMS) f = vectors[T + wm + row];
+#pragma unroll
+  for (int pass = 0; pass < kPasses; ++pass) {
+    in_order();
+#pragma unroll
+    for (int i = pass; i < (kPasses == 1 ? I : pass + 1); ++i) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int n = g * 8 + half * 4, at = ((i - pass) * 32 + n) * (int)sizeof(TO);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][4 * g + e];
+        if constexpr (!SUMS) {
+          const f32x4 b = *(const f32x4 *)(vectors + wn + i * 32 + n);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = v[e] * f + b[e];
+        }
+        store_aligned((TO *)(mine + row * 128 + (((at >> 4) ^ (row & 7)) << 4) + (at & 15)), v);
+      }
+    }
+    in_order();
+    const int p = lane % 8, n = n0 + wn + pass * 32 + p * E;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = q * 8 + lane / 8;
+      const int64_t m = m0 + wm + r;
+      const uint8_t *line = mine + r * 128 + ((p ^ (r & 7)) << 4);
+      if (m >= a.M) continue;
+      TO *out = result + m * a.ld_o + n;
+      if (n + E <= a.N) {
+        *(u32x4_el *)out = *(const u32x4 *)line;
+      } else {
+        for (int k = 0; k < E; ++k)
+          if (n + k < a.N) out[k] = ((const TO *)line)[k];
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // copies past the end have arrived before the LDS is another block's
+}
+
+// A row of sums in the workspace: whole lines.
+__host__ __device__ __forceinline__ int sums_row(int N) { return (N + 31) / 32 * 32; }
+
+// Adds the parts of k up, in their order.  All sums of a part are fewer than 2^22 (256 tiles).
+template <typename TO> __global__ void __launch_bounds__(256) add_kernel(MatmulMxArgs a, int splits) {
+  const uint32_t ld = sums_row(a.N), all = (uint32_t)a.M * ld, i = (blockIdx.x * 256 + threadIdx.x) * 4, m = i / ld, n = i - m * ld;
+  if (i >= all || n >= (uint32_t)a.N) return;
+  const float *sums = (const float *)a.ws + i;
+  const int have = a.N - (int)n;
+  f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) c += *(const f32x4 *)(sums + (size_t)s * all);
+  const float f = a.row_scale ? a.row_scale[m] : 1.f;
+  float b[4] = {}, v[4];
+  if (a.bias) load_part(a.bias + n, have, 0.f, b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = c[e] * f + b[e];
+  store_part((TO *)a.out + m * a.ld_o + n, have, v);
 }
 
 // Few rows (M <= 16 MT): the weights are read once, straight into registers, by one block per 16 NT outputs; the rows
 // come from the caches.  The W waves of a block take 16 blocks of k (256 bytes of a row) in turn, and their sums meet in LDS,
 // where they are added in the waves' order.  Four lanes hold four neighbouring blocks of a row at each of a turn's four steps.
-// Bound by memory: 16 x 32,000 x 4,096 to float32 in 16.4 us (4.4 TB/s), one row in 14.9 (4.7).
+// Bound by latency: one row x 12,000 x 4,096 in 8.2 us, 16 rows in 9.7 (2.7 TB/s).
 template <typename TO, int MT, int NT> __global__ void __launch_bounds__(512) rows_kernel(MatmulMxArgs a) {
   constexpr int W = 8;
   __shared__ float sums[W][MT * 16][NT * 16];
@@ -523,10 +720,14 @@ template <typename TO, int MT, int NT> __global__ void __launch_bounds__(512) ro
   }
 }
 
-// rows_kernel or tiles (us): 32 rows x 8,192 outputs x 4,096 9.8 or 12.9, x 8,192 16.8 or 14.9; 32 x 32,000 x 1,024 12.7 or
-// 9.3; 64 x 4,096 x 8,192 15.0 or 15.4, 64 x 8,192 x 4,096 16.6 or 14.7.
+// rows_kernel or tiles (us): 16 rows x 12,000 outputs x 4,096 9.8 or 10.6, x 20,000 13.5 or 11.5, x 10,000 x 8,192 17.0 or 14.6; one
+// row x 12,000 x 4,096 8.3 or 10.5, x 28,000 14.5 or 12.6; 32 x 8,192 x 4,096 9.6 or 10.8, x 8,192 16.6 or 12.9, 32 x 16,000 x
+// 2,048 10.1 or 7.8; 64 x 4,096 x 4,096 8.8 or 10.5, x 8,192 14.7 or 13.6, 64 x 1,000 x 8,000 13.6 or 9.5.
 bool rows_form(int64_t M, int N, int blocks) {
-  return M <= 16 || (M <= 64 && (int64_t)N * blocks <= 1 << 20 && (M <= 32 || N <= 4096));
+  const int64_t size = (int64_t)N * blocks;
+  if (M <= 16) return N <= 16384 && size <= 1 << 21;
+  if (M <= 32) return N <= 8192 && size <= 1 << 20;
+  return M <= 64 && blocks <= 128 && size <= 1 << 19;
 }
 // How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.  A round of
 // tiles of 256, one on each compute unit, takes about 5 us and 1.5 a stage, behind 9 for the launches and the scales; of 128, two
@@ -540,13 +741,13 @@ int cut_of(int64_t M, int N, int blocks, Cut *c) {
   c->tiles_m = (int)((M + side - 1) / side);
   c->tiles_n = (N + side - 1) / side;
   const int64_t tiles = (int64_t)c->tiles_m * c->tiles_n;
-  // Two stages take 1.3 us; adding parts up 4, and 1 more for each half million sums (written and read again).  In tenths:
-  // 1,000 x 2,000 x 2,016 takes 10.6 us whole and 21.2 in two parts, 300 x 515 x 4,096 16.4 and 13.5 in four.  Parts of less
-  // than four stages measured no better.
-  int64_t splits = 1, least = (stages + 1) / 2 * 13;
+  // A stage takes 0.47 us; adding parts up 4.4, and 1 more for each 600,000 sums (written and read again).  In hundredths: 1,000 x
+  // 1,000 x 8,192 takes 19.7 us whole and 17.1 in three parts, 98 x 4,750 x 7,200 21.1 and 15.4 in four, 128 x 4,096 x 4,096 10.9
+  // and 12.9.  Parts of less than four stages measured no better.
+  int64_t splits = 1, least = stages * 47;
   if (side == 128)
     for (int64_t n = 2; n <= 256 / tiles && n <= stages / 4; ++n) {
-      const int64_t cost = ((stages + n - 1) / n + 1) / 2 * 13 + 40 + n * M * N / 50000;
+      const int64_t cost = (stages + n - 1) / n * 47 + 440 + n * M * N / 6000;
       if (cost < least) {
         splits = n;
         least = cost;
@@ -569,23 +770,39 @@ hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done)
   return e;
 }
 
-template <typename TO, bool ALIGNED, bool SUMS, bool STREAM, int T, int G>
+template <typename TO, bool ALIGNED, bool STREAM, int T>
 hipError_t run_tiles(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, SUMS, STREAM, T, G>, Tile<T, G>::kLds, done);
+  const hipError_t e = allow_lds((const void *)tile_kernel<TO, ALIGNED, STREAM, T>, Tile<T>::kLds, done);
   if (e != hipSuccess) return e;
   // a block goes through several tiles where there are more than the device holds (one of 256, or two of 128 per
   // compute unit)
-  const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = G == 2 ? blocks : T == 256 ? 256 : 512;
-  const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)c.splits), block((Tile<T, G>::kThreads));
-  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, SUMS, STREAM, T, G>), grid, block, (Tile<T, G>::kLds), s, a, c);
+  const int64_t blocks = ((int64_t)c.tiles_m * c.tiles_n + 7) / 8 * 8, most = T == 256 ? 256 : 512;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(Tile<T>::kThreads);
+  hipLaunchKernelGGL((tile_kernel<TO, ALIGNED, STREAM, T>), grid, block, Tile<T>::kLds, s, a, c);
   return hipGetLastError();
 }
 
-template <typename TO, bool SUMS, bool STREAM, int T, int G> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+// Whether rows can be copied to LDS without passing through registers.
+bool copies(const MatmulMxArgs &a) {
   const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.ld_x | (uintptr_t)a.ld_w) & 15) == 0;
-  const bool near = a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
-  return aligned && near ? run_tiles<TO, true, SUMS, STREAM, T, G>(a, c, s) : run_tiles<TO, false, SUMS, STREAM, T, G>(a, c, s);
+  return aligned && a.ld_x < (1 << 22) && a.ld_w < (1 << 22);  // a tile's rows lie within 2^30 bytes
+}
+
+template <typename TO, bool STREAM, int T> hipError_t run_cut(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+  return copies(a) ? run_tiles<TO, true, STREAM, T>(a, c, s) : run_tiles<TO, false, STREAM, T>(a, c, s);
+}
+
+template <typename TO, bool ALIGNED, bool SUMS> hipError_t run_ring_as(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_lds((const void *)ring_kernel<TO, ALIGNED, SUMS>, kRingLds, done);
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)((c.tiles_m * c.tiles_n + 7) / 8 * 8), (unsigned)c.splits);
+  hipLaunchKernelGGL((ring_kernel<TO, ALIGNED, SUMS>), grid, dim3(512), kRingLds, s, a, c);
+  return hipGetLastError();
+}
+template <typename TO, bool SUMS> hipError_t run_ring(const MatmulMxArgs &a, const Cut &c, hipStream_t s) {
+  return copies(a) ? run_ring_as<TO, true, SUMS>(a, c, s) : run_ring_as<TO, false, SUMS>(a, c, s);
 }
 
 template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulMxArgs &a, hipStream_t s) {
@@ -617,16 +834,16 @@ template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const bool lines = (((uintptr_t)a.out | (uintptr_t)(a.ld_o * (int64_t)sizeof(TO))) & 127) == 0;
-    return lines ? run_cut<TO, false, true, 256, 1>(a, c, s) : run_cut<TO, false, false, 256, 1>(a, c, s);
+    return lines ? run_cut<TO, true, 256>(a, c, s) : run_cut<TO, false, 256>(a, c, s);
   }
-  if ((int64_t)c.tiles_m * c.tiles_n > 256) return run_cut<TO, false, false, 128, 1>(a, c, s);
-  if (c.splits == 1) return run_cut<TO, false, false, 128, 2>(a, c, s);
+  if ((int64_t)c.tiles_m * c.tiles_n > 256) return run_cut<TO, false, 128>(a, c, s);
+  if (c.splits == 1) return run_ring<TO, false>(a, c, s);
   MatmulMxArgs b = a;
   b.out = a.ws;
-  b.ld_o = a.N;
-  const hipError_t e = run_cut<float, true, false, 128, 2>(b, c, s);
+  b.ld_o = sums_row(a.N);
+  const hipError_t e = run_ring<float, true>(b, c, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((add_kernel<TO>), dim3((unsigned)((a.M * a.N + 1023) / 1024)), dim3(256), 0, s, a, c.splits);
+  hipLaunchKernelGGL((add_kernel<TO>), dim3((unsigned)((a.M * sums_row(a.N) + 1023) / 1024)), dim3(256), 0, s, a, c.splits);
   return hipGetLastError();
 }
 
@@ -637,7 +854,7 @@ size_t matmul_mx_bytes(int64_t rows, int outputs, int blocks) {
   mmx::Cut c;
   if (mmx::cut_of(rows, outputs, blocks, &c) == 256)  // both operands' scales by stages
     return (size_t)(c.tiles_n + c.tiles_m) * 256 * ((blocks + mmx::HB - 1) / mmx::HB * mmx::HB);
-  return c.splits > 1 ? (size_t)c.splits * rows * outputs * sizeof(float) : 0;
+  return c.splits > 1 ? (size_t)c.splits * rows * mmx::sums_row(outputs) * sizeof(float) : 0;
 }
 
 hipError_t launch_matmul_mx(const MatmulMxArgs &a, int out_dtype, hipStream_t s) {

@@ -311,6 +311,39 @@ def test_product(M, N, blocks, dtype):
     check_product(x, ex, w, ew, dtype, row_scale=randn(3, M), bias=10 * randn(4, N))
 
 
+@pytest.mark.parametrize("blocks", [1, 8, 9, 15, 16, 17, 24, 31, 32, 33, 40, 49, 57, 64, 65, 96, 127])
+def test_product_every_count_of_stages(blocks):
+    """One stage of eight blocks to several rounds of four, the last one full or not; wide outputs of one row, tiles that are not full."""
+    for M, N, dtype in ((1, 17000, F32), (16, 17003, BF16), (130, 387, F32), (97, 1290, BF16)):
+        x, ex = random_rows(M, M, blocks, 2)
+        w, ew = random_rows(N + 7, N, blocks, 2)
+        f, bias = randn(3, M), 10 * randn(4, N)
+        got = check_product(x, ex, w, ew, dtype, row_scale=f, bias=bias)
+        check_product(x, ex, w, ew, dtype, bias=bias)
+        check_product(x, ex, w, ew, dtype, row_scale=f)
+        wide = torch.full((M, N + 9), 7.0, dtype=dtype, device="cuda")
+        again = check_product(odd_view(x, 1, 48), odd_view(ex, 1, 2), odd_view(w, 3, 32), odd_view(ew, 2, 7), dtype, f, bias,
+                              out=wide[:, 3:3 + N])
+        assert torch.equal(got, again) and bool((wide[:, :3] == 7).all()) and bool((wide[:, 3 + N:] == 7).all())
+
+
+@pytest.mark.parametrize("M,N,blocks", [(100, 130, 128), (128, 128, 250), (65, 2307, 193), (98, 4750, 225), (577, 1565, 255),
+                                        (500, 501, 500), (1, 500, 7000), (70, 33, 1030)])
+def test_product_in_parts(M, N, blocks):
+    """Few tiles and long rows: parts of k are added up in a second step, always in the same order."""
+    assert ops._bytes("fwg_matmul_mx_workspace", M, N, blocks) > 0
+    x, ex = random_rows(M, M, blocks, 2)
+    w, ew = random_rows(N + 7, N, blocks, 2)
+    f, bias = randn(3, M), 10 * randn(4, N)
+    for dtype in TYPES:
+        got = check_product(x, ex, w, ew, dtype, row_scale=f, bias=bias, exact=False)
+        check_product(x, ex, w, ew, dtype, exact=False)
+        wide = torch.full((M, N + 9), 7.0, dtype=dtype, device="cuda")
+        again = check_product(odd_view(x, 1, 48), odd_view(ex, 1, 2), odd_view(w, 3, 32), odd_view(ew, 2, 7), dtype, f, bias,
+                              exact=False, out=wide[:, 3:3 + N])
+        assert torch.equal(got, again) and bool((wide[:, :3] == 7).all()) and bool((wide[:, 3 + N:] == 7).all())
+
+
 def large_tiles(M, N, blocks):
     """Whether a product runs in tiles of 256: they alone have the scales of both operands rearranged in the workspace."""
     return ops._bytes("fwg_matmul_mx_workspace", M, N, blocks) == (-(-M // 256) + -(-N // 256)) * 256 * -(-blocks // 8) * 8

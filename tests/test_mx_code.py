@@ -48,3 +48,15 @@ def test_results_past_the_caches_where_rows_are_whole_lines(tmp_path):
     stores = {n: re.findall(r"global_store_dwordx4[^\n]*", b) for n, b in tiles.items()}
     streamed = [n for n, s in stores.items() if any(x.endswith(" nt") for x in s)]
     assert len(streamed) == 4 and all(all(x.endswith(" nt") for x in stores[n]) for n in streamed), stores
+
+
+def test_the_ring_waits_for_what_it_needs_only(tmp_path):
+    """Three stages are on their way to LDS while one is multiplied: a wait for all of them inside the loop would end that."""
+    rings = {n: b for n, (b, _, _) in kernels(device_asm("fwg_matmulmx.hip", str(tmp_path / "m.s"))).items()
+             if re.search("ring_kernelI.Lb1", n)}
+    assert len(rings) == 3
+    for name, body in rings.items():
+        loops = [b for b in re.split(r"\n(?=\.LBB)", body) if "Loop Header" in b and b.count("s_barrier") >= 4]
+        assert len(loops) == 1, name
+        waits = re.findall(r"vmcnt\((\d+)\)", loops[0])
+        assert waits == ["8"] * 4 and loops[0].count("global_load_lds_dwordx4") == 16, (name, waits)
