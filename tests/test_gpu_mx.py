@@ -876,6 +876,27 @@ def test_either_way_of_marshalling(lead, dtype, monkeypatch):
             assert (a is None and b is None) or (a.shape == b.shape and same(a, b))
 
 
+@pytest.mark.parametrize("M,N,blocks", [(100, 130, 256), (4000, 4096, 64)])
+def test_products_with_a_workspace_either_way(M, N, blocks, monkeypatch):
+    """Parts of k added up, and scales rearranged: the module takes the call with a workspace of its own."""
+    assert ops._bytes("fwg_matmul_mx_workspace", M, N, blocks) > 0
+    x, ex = random_rows(21, M, blocks, 2)
+    w, ew = random_rows(22, N, blocks, 2)
+    f, bias = randn(23, M), randn(24, N)
+    (fast,), (slow,) = both_ways(monkeypatch, lambda: [ops.matmul_mx(x, ex, w, ew, row_scale=f, bias=bias)])
+    assert torch.equal(fast, slow)
+    out = torch.empty_like(fast)
+    device = torch.cuda.current_device()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):  # two streams' workspaces are their own
+        other = ops.matmul_mx(x, ex, w, ew, row_scale=f, bias=bias)
+        assert ops._plain.matmul_mx(device, stream.cuda_stream, x, ex, w, ew, f, bias, out) == 0
+    mine = ops.matmul_mx(x, ex, w, ew, row_scale=f, bias=bias)
+    torch.cuda.synchronize()
+    assert torch.equal(out, fast) and torch.equal(other, fast) and torch.equal(mine, fast)
+
+
 def test_refusals_either_way(monkeypatch):
     """What one way refuses the other refuses with the same error."""
     x, f = randn(1, 4, 64), torch.zeros(4, device="cuda")
