@@ -722,12 +722,12 @@ template <typename TO, int MT, int NT> __global__ void __launch_bounds__(512) ro
 
 // rows_kernel or tiles (us): 16 rows x 12,000 outputs x 4,096 9.8 or 10.6, x 20,000 13.5 or 11.5, x 10,000 x 8,192 17.0 or 14.6; one
 // row x 12,000 x 4,096 8.3 or 10.5, x 28,000 14.5 or 12.6; 32 x 8,192 x 4,096 9.6 or 10.8, x 8,192 16.6 or 12.9, 32 x 16,000 x
-// 2,048 10.1 or 7.8; 64 x 4,096 x 4,096 8.8 or 10.5, x 8,192 14.7 or 13.6, 64 x 1,000 x 8,000 13.6 or 9.5.
+// 2,048 10.1 or 7.8; 64 x 4,096 x 4,096 8.8 or 10.5, x 8,192 14.7 or 13.6, 64 x 1,000 x 8,000 13.6 or 9.5, 64 x 8,192 x 1,024 7.0 or 5.5.
 bool rows_form(int64_t M, int N, int blocks) {
   const int64_t size = (int64_t)N * blocks;
   if (M <= 16) return N <= 16384 && size <= 1 << 21;
   if (M <= 32) return N <= 8192 && size <= 1 << 20;
-  return M <= 64 && blocks <= 128 && size <= 1 << 19;
+  return M <= 64 && N <= 4096 && blocks <= 128;
 }
 // How a product of more rows is cut: the tile's side, and parts of k where the tiles alone leave compute units idle.  A round of
 // tiles of 256, one on each compute unit, takes about 5 us and 1.5 a stage, behind 9 for the launches and the scales; of 128, two
@@ -806,19 +806,8 @@ template <typename TO, bool SUMS> hipError_t run_ring(const MatmulMxArgs &a, con
 }
 
 template <typename TO, int MT, int NT> hipError_t run_rows(const MatmulMxArgs &a, hipStream_t s) {
-  constexpr int64_t kSlice = ((int64_t)16 * NT) << 22;  // outputs of a launch: it has at most 2^32 threads
-  for (int64_t n = 0; n < a.N; n += kSlice) {
-    MatmulMxArgs b = a;
-    b.N = (int)(a.N - n < kSlice ? a.N - n : kSlice);
-    b.w = a.w + n * a.ld_w;
-    b.w_scale = a.w_scale + n * a.ld_ew;
-    if (a.bias) b.bias = a.bias + n;
-    b.out = (TO *)a.out + n;
-    hipLaunchKernelGGL((rows_kernel<TO, MT, NT>), dim3((unsigned)((b.N + 16 * NT - 1) / (16 * NT))), dim3(512), 0, s, b);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  hipLaunchKernelGGL((rows_kernel<TO, MT, NT>), dim3((unsigned)((a.N + 16 * NT - 1) / (16 * NT))), dim3(512), 0, s, a);
+  return hipGetLastError();
 }
 
 template <typename TO> hipError_t run(const MatmulMxArgs &a, hipStream_t s) {
