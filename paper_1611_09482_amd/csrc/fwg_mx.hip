@@ -26,6 +26,11 @@ using namespace opd;
 constexpr int kE = 8;                        // elements of a thread's piece; four threads make a block of 32
 constexpr uint32_t kTinyBits = 27u << 23;    // 2^-100: blocks that lie below are zero
 constexpr uint32_t kInfBits = 0x7f800000u;
+// Squares of small elements lie below float32's normal numbers (2^-126), where they have fewer bits or none.  A sum from kSmall
+// on misses less than 32,768 * 2^-150 of them, 2^-35 of itself, and so does one to whose mean such an eps is added.  Below,
+// every element is smaller than 2^-50, and times kUp even the smallest, 2^-149, has a normal square: the scaling is exact, and
+// 32,768 squares stay below 2^115.
+constexpr float kSmall = 0x1p-100f, kUp = 0x1p100f;
 
 typedef unsigned int u32_b __attribute__((aligned(1)));
 
@@ -90,17 +95,19 @@ template <typename T, bool STREAM> __global__ void __launch_bounds__(256) quant_
   }
 }
 
-// TPR threads per row (64: a wave per row), NP pieces per thread.
-template <typename T, int TPR, int NP, bool STREAM>
+// TPR threads per row (64: a wave per row), NP pieces per thread.  BARE: eps below kSmall does not hide what the sum of squares
+// misses; the second sum costs 64 x 4,096 0.15 us of 4.9, so other calls go without it.
+template <typename T, int TPR, int NP, bool STREAM, bool BARE>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(MxArgs a) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kW = TPR / 64;
-  __shared__ float red[2 * kW];
+  constexpr int kSums = BARE ? 3 : 2;
+  __shared__ float red[kSums * kW];
   const int t = threadIdx.x % TPR;
   const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (r >= a.rows) return;  // whole waves, and whole blocks where a block is one row
   const int padded = (a.channels + 31) / 32 * 32;
   uint32_t q[NP], top[NP];
-  float ss = 0.f, some = 0.f;
+  float ss = 0.f, ss_up = 0.f, some = 0.f;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int c = (p * TPR + t) * kE, have = a.channels - c;
@@ -115,6 +122,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(MxArgs a) {
     if (a.summed) store_part<STREAM>((T *)a.summed + r * a.ld_s + c, have, h);
 #pragma unroll
     for (int i = 0; i < kE; ++i) ss += h[i] * h[i];
+    if constexpr (BARE) {
+#pragma unroll
+      for (int i = 0; i < kE; ++i) ss_up += (h[i] * kUp) * (h[i] * kUp);
+    }
     if (a.gain) {
       float g[kE];
       load_part(a.gain + c, have, 0.f, g);
@@ -130,22 +141,26 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(MxArgs a) {
   }
   ss = wave_sum(ss);
   some = wave_max(some);
+  if constexpr (BARE) ss_up = wave_sum(ss_up);
   if (kW > 1) {
     const int w = t >> 6;
     if ((t & 63) == 0) {
-      red[2 * w] = ss;
-      red[2 * w + 1] = some;
+      red[kSums * w] = ss;
+      red[kSums * w + 1] = some;
+      if constexpr (BARE) red[kSums * w + 2] = ss_up;
     }
     __syncthreads();
-    ss = some = 0.f;
+    ss = ss_up = some = 0.f;
 #pragma unroll
     for (int i = 0; i < kW; ++i) {
-      ss += red[2 * i];
-      some = fmaxf(some, red[2 * i + 1]);
+      ss += red[kSums * i];
+      some = fmaxf(some, red[kSums * i + 1]);
+      if constexpr (BARE) ss_up += red[kSums * i + 2];
     }
   }
-  const float rs = rsqrtf(ss / (float)a.channels + a.eps);
-  // a row of nothing is zero whatever its factor; a sum of squares that passes float32's numbers gives none
+  float rs = rsqrtf(ss / (float)a.channels + a.eps);
+  if (BARE && ss < kSmall) rs = rsqrtf(ss_up / (float)a.channels + a.eps * kUp * kUp) * kUp;
+  // a row of nothing is zero whatever its factor; a sum of squares or a factor that passes float32's numbers gives none
   const float factor = !(ss < kInf) ? __builtin_nanf("") : some == 0.f ? 0.f : rs < kInf ? rs : __builtin_nanf("");
   if (t == 0) a.row_scale[r] = factor;
   if (!a.values) return;
@@ -163,12 +178,15 @@ template <typename T> int64_t written(const MxArgs &a) {
   return a.rows * a.channels * ((a.summed ? (int64_t)sizeof(T) : 0) + (a.values ? 2 : 0)) + a.rows * (a.channels / 2);
 }
 
-template <typename T, int TPR, int NP> hipError_t go(const MxArgs &a, hipStream_t s) {
+template <typename T, int TPR, int NP, bool STREAM> hipError_t go_as(const MxArgs &a, hipStream_t s) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
   const dim3 grid((unsigned)((a.rows + kRows - 1) / kRows)), block(TPR < 256 ? 256 : TPR);
-  if (written<T>(a) < kStreamBytes) hipLaunchKernelGGL((norm_kernel<T, TPR, NP, false>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((norm_kernel<T, TPR, NP, true>), grid, block, 0, s, a);
+  if (a.eps < kSmall) hipLaunchKernelGGL((norm_kernel<T, TPR, NP, STREAM, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_kernel<T, TPR, NP, STREAM, false>), grid, block, 0, s, a);
   return hipGetLastError();
+}
+template <typename T, int TPR, int NP> hipError_t go(const MxArgs &a, hipStream_t s) {
+  return written<T>(a) < kStreamBytes ? go_as<T, TPR, NP, false>(a, s) : go_as<T, TPR, NP, true>(a, s);
 }
 
 template <typename T> hipError_t run_norm(const MxArgs &a, hipStream_t s) {
