@@ -353,7 +353,7 @@ int fwg_quant_mx(int32_t dtype, int64_t rows, int32_t channels, const void *x, i
 
 /* Residual addition, RMS norm and rows in 4 bits: h = x + residual, row_scale = 1 / sqrt(mean(h^2) + eps), q and scale of
  * h * gain as in fwg_quant_mx: the norm's rows are row_scale[r] times what the 4 bits stand for.  row_scale is 0 for a row
- * whose blocks are all zero, and NaN where the sum of squares or row_scale itself is no number or passes float32's largest
+ * whose blocks are all zero, else NaN where the sum of squares or row_scale itself is no number or passes float32's largest
  * value; eps may be 0, and squares below float32's numbers count.  residual NULL: none; gain
  * (float32 [channels]) NULL: ones.  Optional outputs: summed, h rounded to dtype (may be x or residual itself: the same
  * address and stride), and values, row_scale times what the 4 bits stand for, in bf16.  The

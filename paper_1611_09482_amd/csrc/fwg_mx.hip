@@ -160,8 +160,8 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(MxArgs a) {
   }
   float rs = rsqrtf(ss / (float)a.channels + a.eps);
   if (BARE && ss < kSmall) rs = rsqrtf(ss_up / (float)a.channels + a.eps * kUp * kUp) * kUp;
-  // a row of nothing is zero whatever its factor; a sum of squares or a factor that passes float32's numbers gives none
-  const float factor = !(ss < kInf) ? __builtin_nanf("") : some == 0.f ? 0.f : rs < kInf ? rs : __builtin_nanf("");
+  // a row of nothing is zero whatever its size (a gain of zero); a NaN or an infinity makes its block something
+  const float factor = some == 0.f ? 0.f : ss < kInf && rs < kInf ? rs : __builtin_nanf("");
   if (t == 0) a.row_scale[r] = factor;
   if (!a.values) return;
 #pragma unroll

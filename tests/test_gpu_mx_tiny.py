@@ -96,6 +96,22 @@ def test_rows_out_of_the_ordinary_without_eps():
     assert bool(torch.isnan(r.row_scale).all()) and bool(torch.isnan(r.values[:, :32]).all())
 
 
+@pytest.mark.parametrize("channels", CHANNELS)
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_rows_without_a_block_are_zero_whatever_their_size(channels, eps):
+    """A gain of zero leaves nothing, also of a row whose sum of squares passes float32; NaN and infinity stay something."""
+    x = randn(channels, 6, channels)
+    x[1] = 0.0
+    x[2] = torch.finfo(F32).max
+    x[3] = x[3].sign() * 2.0 ** 100
+    x[4, 0] = math.nan
+    x[5, channels - 1] = math.inf
+    r = ops.norm_mx(x, torch.zeros(channels, device="cuda"), eps=eps, values=True)
+    assert torch.isnan(r.row_scale).tolist() == [False] * 4 + [True] * 2
+    assert not r.row_scale[:4].any() and not r.scale[:4].any() and not r.values[:4].any()
+    assert bool((r.scale[4:] == 255).any(1).all())
+
+
 def test_the_same_bits_in_place_and_again():
     x = (randn(1, 9, 3000) * 2.0 ** -70).to(BF16)
     want = ops.norm_mx(x, residual=x, eps=0.0, values=True)
