@@ -45,23 +45,31 @@ def _run(cmd, verbose):
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("hipcc failed: " + " ".join(cmd[-3:]))
+        raise RuntimeError(f"{cmd[0]} failed: " + " ".join(cmd[-3:]))
 
 
 def build_marshal(verbose: bool = False) -> None:
-    """Compile the module _marshal against this Python's torch (host code only); without torch there is nothing to marshal."""
+    """Compile the module _marshal against this Python's torch (host code only); without torch there is nothing to marshal.
+    ops.py works without the module: where it cannot be compiled (no host compiler, no headers) a warning says so, and a module
+    of other sources does not stay."""
     import sysconfig
+    import warnings
     try:
         import torch
         from torch.utils.cpp_extension import include_paths, library_paths
     except ImportError:
         return
     tmp = MARSHAL + ".tmp"
-    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
-          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + os.path.join(ROOT, "include"),
-          "-I" + sysconfig.get_paths()["include"]] + ["-isystem" + p for p in include_paths()] +
-         ["-o", tmp, MARSHAL_SOURCE] + ["-L" + p for p in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
-    os.replace(tmp, MARSHAL)
+    try:
+        _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + os.path.join(ROOT, "include"),
+              "-I" + sysconfig.get_paths()["include"]] + ["-isystem" + p for p in include_paths()] +
+             ["-o", tmp, MARSHAL_SOURCE] + ["-L" + p for p in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+        os.replace(tmp, MARSHAL)
+    except (OSError, RuntimeError) as e:
+        if os.path.exists(MARSHAL):
+            os.remove(MARSHAL)
+        warnings.warn(f"the module _marshal was not built: calls of few rows take the host longer ({e})")
 
 
 def build(verbose: bool = False) -> str:
