@@ -1,16 +1,19 @@
 """Compile libfwg.so for gfx950 with hipcc (in-tree, next to this file)."""
 from __future__ import annotations
 
+import glob
 import os
 import subprocess
 import sys
+import sysconfig
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libfwg.so")
-MARSHAL, MARSHAL_SOURCE = os.path.join(PKG, "_marshal.so"), os.path.join(CSRC, "fwg_marshal.cpp")  # a module of ops.py
+MARSHAL, MARSHAL_SOURCE = os.path.join(PKG, "_marshal"), os.path.join(CSRC, "fwg_marshal.cpp")  # a module of ops.py
 SOURCES = [os.path.join(CSRC, "fwg_host.cpp"), os.path.join(CSRC, "fwg_kernels.hip"),
            os.path.join(CSRC, "fwg_mfma.hip"), os.path.join(CSRC, "fwg_parallel.hip"),
            os.path.join(CSRC, "fwg_parstack.hip"), os.path.join(CSRC, "fwg_parhead.hip"),
@@ -48,28 +51,38 @@ def _run(cmd, verbose):
         raise RuntimeError(f"{cmd[0]} failed: " + " ".join(cmd[-3:]))
 
 
-def build_marshal(verbose: bool = False) -> None:
-    """Compile the module _marshal against this Python's torch (host code only); without torch there is nothing to marshal.
-    ops.py works without the module: where it cannot be compiled (no host compiler, no headers) a warning says so, and a module
-    of other sources does not stay."""
-    import sysconfig
-    import warnings
+def marshal_path():
+    """Where the module _marshal for this Python and this torch lies (None without torch).  It reads tensors by torch's own
+    layouts, so the file's name has both versions and another's module is not found."""
     try:
         import torch
-        from torch.utils.cpp_extension import include_paths, library_paths
     except ImportError:
-        return
-    tmp = MARSHAL + ".tmp"
+        return None
+    return f"{MARSHAL}-torch{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}"
+
+
+def build_marshal(verbose: bool = False) -> None:
+    """Compile the module _marshal (host code only); without torch there is nothing to marshal.  ops.py works without the
+    module: where it cannot be compiled (no host compiler, no headers) a warning says so.  Modules of other sources or
+    versions do not stay."""
+    path = marshal_path()
+    built = False
     try:
-        _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
-              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + os.path.join(ROOT, "include"),
-              "-I" + sysconfig.get_paths()["include"]] + ["-isystem" + p for p in include_paths()] +
-             ["-o", tmp, MARSHAL_SOURCE] + ["-L" + p for p in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
-        os.replace(tmp, MARSHAL)
-    except (OSError, RuntimeError) as e:
-        if os.path.exists(MARSHAL):
-            os.remove(MARSHAL)
+        if path is not None:
+            import torch
+            from torch.utils.cpp_extension import include_paths, library_paths
+            _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                  f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I" + os.path.join(ROOT, "include"),
+                  "-I" + sysconfig.get_paths()["include"]] + ["-isystem" + p for p in include_paths()] +
+                 ["-o", path + ".tmp", MARSHAL_SOURCE] + ["-L" + p for p in library_paths()] +
+                 ["-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+            os.replace(path + ".tmp", path)
+            built = True
+    except (ImportError, OSError, RuntimeError) as e:
         warnings.warn(f"the module _marshal was not built: calls of few rows take the host longer ({e})")
+    for other in glob.glob(glob.escape(MARSHAL) + "*.so"):
+        if not built or other != path:
+            os.remove(other)
 
 
 def build(verbose: bool = False) -> str:
@@ -89,7 +102,8 @@ def build(verbose: bool = False) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    marshal = marshal_path()
+    if not os.path.exists(LIB) or (marshal is not None and not os.path.exists(marshal)):
         return True
     t = os.path.getmtime(LIB)
     return any(os.path.getmtime(s) > t for s in SOURCES + HEADERS + [MARSHAL_SOURCE])

@@ -15,26 +15,40 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib.util
+import os
 from typing import NamedTuple, Optional
 
 import torch
 
 from .binding import FWG_BF16, FWG_EINVAL, FWG_EUNSUPPORTED, FWG_F32, FwgError, _check, load_library
-
-try:
-    from . import _marshal  # the checks of plain arguments in C++, where the host's time counts (csrc/fwg_marshal.cpp)
-except ImportError:
-    _marshal = None
+from .build import marshal_path
 
 _TYPES = {torch.float32: FWG_F32, torch.bfloat16: FWG_BF16}
 _lib = None
-_plain = None  # _marshal once it knows the library's entries
+_marshal = None  # the checks of plain arguments in C++, where the host's time counts (csrc/fwg_marshal.cpp)
+_plain = None    # _marshal once it knows the library's entries
+
+
+def _load_marshal():
+    """The module _marshal, or None where it was not built for this Python and this torch."""
+    path = marshal_path()
+    if not os.path.exists(path):
+        return None
+    spec = importlib.util.spec_from_file_location(__package__ + "._marshal", path)
+    try:
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:
+        return None
+    return module
 
 
 def _library():
-    global _lib, _plain
+    global _lib, _marshal, _plain
     if _lib is None:
         _lib = load_library()
+        _marshal = _load_marshal()
         if _marshal is not None:
             _marshal.bind(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
                 "fwg_quant_mx", "fwg_norm_mx", "fwg_matmul_mx_workspace", "fwg_matmul_mx", "fwg_adjust_logits")))
