@@ -140,7 +140,8 @@ __global__ void __launch_bounds__(THREADS) adjust_kernel(AdjustArgs a, int parts
   }
 }
 
-template <typename T, int THREADS, int P> hipError_t go(const AdjustArgs &a, hipStream_t s) {
+// PARTS: rows may have several parts.
+template <typename T, int THREADS, int P, bool PARTS> hipError_t go(const AdjustArgs &a, hipStream_t s) {
   // parts of one size, of whole words of `allowed`
   constexpr int kMost = THREADS * kE * P;
   const int parts = (int)(((int64_t)a.vocab + kMost - 1) / kMost);
@@ -148,12 +149,14 @@ template <typename T, int THREADS, int P> hipError_t go(const AdjustArgs &a, hip
   // Together a row's history comes into one L2 alone.  64 rows of 131,072 with 16,381 tokens 17.5 us in turn, 16.9 together, but with
   // 100 tokens 11.1 and 11.5; 190 rows with 1,000 tokens 29.0 and 27.6, in place 24.1 and 19.5; 2,000 rows of 12,000, two parts
   // each, 37.1 and 38.1.
-  if (parts >= 4 && (a.rows >= 128 || (a.rows >= 32 && a.tokens && a.history >= 4096))) {
-    const dim3 grid((unsigned)((a.rows + 7) / 8 * 8 * parts));
-    hipLaunchKernelGGL((adjust_kernel<T, THREADS, P, true>), grid, dim3(THREADS), 0, s, a, parts, part);
-  } else {
-    hipLaunchKernelGGL((adjust_kernel<T, THREADS, P, false>), dim3((unsigned)(a.rows * parts)), dim3(THREADS), 0, s, a, parts, part);
+  if constexpr (PARTS) {
+    if (parts >= 4 && (a.rows >= 128 || (a.rows >= 32 && a.tokens && a.history >= 4096))) {
+      const dim3 grid((unsigned)((a.rows + 7) / 8 * 8 * parts));
+      hipLaunchKernelGGL((adjust_kernel<T, THREADS, P, true>), grid, dim3(THREADS), 0, s, a, parts, part);
+      return hipGetLastError();
+    }
   }
+  hipLaunchKernelGGL((adjust_kernel<T, THREADS, P, false>), dim3((unsigned)(a.rows * parts)), dim3(THREADS), 0, s, a, parts, part);
   return hipGetLastError();
 }
 
@@ -161,7 +164,7 @@ template <typename T, int THREADS, int P> hipError_t go(const AdjustArgs &a, hip
 // 512, 37.6 by 256, and 35.7 in parts of 2,048 by 256; with 16,381 tokens, which every part reads, 44.7, 40.9, 52.4 and
 // 56.9 (all in turn).  2,048 rows of 256: 9.6 us in parts of 2,048 (the call), 12.2 in parts of 8,192.
 template <typename T> hipError_t run(const AdjustArgs &a, hipStream_t s) {
-  return a.vocab <= 2048 ? go<T, 256, 1>(a, s) : go<T, 512, 2>(a, s);
+  return a.vocab <= 2048 ? go<T, 256, 1, false>(a, s) : go<T, 512, 2, true>(a, s);
 }
 
 }  // namespace adj
