@@ -347,7 +347,7 @@ int fwg_adjust_logits(int32_t dtype, int64_t rows, int32_t vocab, const void *lo
   if (frequency) CHECK(check_ptr("frequency", frequency, 4));
   if (bias) CHECK(check_ptr("bias", bias, 4));
   if (allowed) CHECK(check_ptr("allowed", allowed, 4));
-  const int64_t quarter = rows_per_launch(vocab) / 4, per = quarter < 1 ? 1 : quarter;  // up to 1,024 threads a row
+  const int64_t per = rows_per_launch(vocab);  // 256 threads for up to 2,048 logits, else 512 for up to 8,192
   for (int64_t r = 0; r < rows; r += per) {
     AdjustArgs a{};
     a.logits = at(logits, r * logits_stride, dtype);
