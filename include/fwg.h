@@ -365,8 +365,9 @@ int fwg_norm_mx(int32_t dtype, int64_t rows, int32_t channels, const void *x, in
 
 /* out[m][n] = row_scale[m] * (sum over k of x[m][k] w[n][k]) + bias[n], x and w in microscaled 4 bits as fwg_quant_mx and
  * fwg_norm_mx leave them: x [rows] and w [outputs] (PyTorch's layout) rows of `blocks` blocks each, at any address.  row_scale (float32 [rows])
- * NULL: ones; bias (float32 [outputs]) NULL: none.  Products and sums are float32.  A block with scale 255 makes its
- * row's (or output's) results NaN.  1 <= blocks <= 32768, rows <= 2^30. */
+ * NULL: ones; bias (float32 [outputs]) NULL: none.  Products and sums are float32: where a sum passes its largest value on the
+ * way the result is infinite or NaN, and parts of a sum below its smallest number, 2^-149, may be lost.  A block with scale
+ * 255 makes its row's (or output's) results NaN.  1 <= blocks <= 32768, rows <= 2^30. */
 int fwg_matmul_mx_workspace(int64_t rows, int32_t outputs, int32_t blocks, size_t *bytes);
 int fwg_matmul_mx(int32_t out_dtype, int64_t rows, int32_t outputs, int32_t blocks, const uint8_t *x, int64_t x_stride,
                    const uint8_t *x_scale, int64_t x_scale_stride, const uint8_t *w, int64_t w_stride,

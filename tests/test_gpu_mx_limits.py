@@ -2,8 +2,6 @@
 
 Bars: as derived in test_gpu_mx.py.
 """
-import math
-
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -13,7 +11,8 @@ if not torch.cuda.is_available():  # pragma: no cover
     pytest.skip("needs a GPU", allow_module_level=True)
 
 from paper_1611_09482_amd import ops  # noqa: E402
-from test_gpu_mx import BF16, F32, INF, TYPES, U, ints, plain_adjust, rand, randn  # noqa: E402
+from test_gpu_mx import (BF16, F32, TYPES, check_product, ints, large_tiles, odd_view, plain_adjust, rand, randn,  # noqa: E402
+                         random_rows, unpacked)
 
 
 # ---- more rows than a launch takes ----
@@ -33,3 +32,73 @@ def test_adjust_more_rows_than_one_launch_takes(V, n):
         assert bool(((d == want) | ((d - want).abs() <= bar)).all())
     mine = z.clone()
     assert torch.equal(ops.adjust_logits(mine, tokens, lengths, presence=presence, allowed=allowed, out=mine), out)
+
+
+def test_product_of_more_tiles_than_the_scales_launch_has_blocks():
+    """65,536 tiles of 256 and more: the launch that rearranges the scales goes through them in rounds."""
+    M, N = (1 << 24) + 300, 200
+    assert large_tiles(M, N, 1) and -(-M // 256) + -(-N // 256) > 1 << 16
+    x, ex = random_rows(1, M, 1, 2)
+    w, ew = random_rows(2, N, 1, 2)
+    got = ops.matmul_mx(x, ex, w, ew)
+    b = unpacked(w, ew).t().contiguous()
+    for at in range(0, M, 1 << 20):
+        r = slice(at, min(M, at + (1 << 20)))
+        assert torch.equal(got[r], (unpacked(x[r], ex[r]) @ b).float().to(BF16)), at
+
+
+# ---- scales at both ends of their type ----
+
+# a kernel each: few rows; the ring, whole and in parts of k; small tiles; large ones
+KERNELS = [(1, 77, 5), (16, 300, 40), (60, 4000, 33), (16, 20000, 24), (300, 600, 33), (100, 130, 220), (3000, 3900, 20), (4000, 4096, 100)]
+
+
+@pytest.mark.parametrize("M,N,blocks", KERNELS)
+def test_product_of_the_largest_and_smallest_scales(M, N, blocks):
+    """Scale bytes from 0 to 254 that belong together: every product is as in test_gpu_mx.py, so the sums are exact."""
+    x, ex = random_rows(M, M, blocks, 2)
+    w, ew = random_rows(N + 7, N, blocks, 2)
+    apart = ints(5, -126, 127, blocks)
+    apart[0], apart[-1] = -126, 126
+    ex, ew = (ex.int() + apart).to(torch.uint8), (ew.int() - apart).to(torch.uint8)
+    assert int(ex.min()) <= 2 and int(ex.max()) >= 252 and int(torch.cat([ex.view(-1), ew.view(-1)]).max()) <= 254
+    f, bias = randn(3, M), 10 * randn(4, N)
+    for dtype in TYPES:
+        check_product(x, ex, w, ew, dtype)
+        check_product(odd_view(x, 1, 48), odd_view(ex, 1, 2), odd_view(w, 3, 32), odd_view(ew, 2, 7), dtype, f, bias)
+
+
+def ones(rows, blocks, byte, code=2):
+    """Rows of one element, 1 by default, with one scale."""
+    return (torch.full((rows, 16 * blocks), 17 * code, dtype=torch.uint8, device="cuda"),
+            torch.full((rows, blocks), byte, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("M,N,blocks", KERNELS)
+def test_product_past_the_ends_of_float32(M, N, blocks):
+    """Sums past float32's largest value are infinite, and what lies far below its smallest is zero."""
+    for bx, bw in [(254, 254), (254, 200), (254, 130), (190, 190), (186, 186), (127, 127), (254, 0), (0, 254), (60, 60), (0, 120),
+                   (1, 70), (0, 70), (40, 40), (1, 1), (0, 0)]:
+        want = torch.tensor(32.0 * blocks * 2.0 ** (bx + bw - 254), dtype=torch.float64).float()
+        for sign in (1, -1):
+            x, ex = ones(M, blocks, bx, 2 if sign > 0 else 10)
+            w, ew = ones(N, blocks, bw)
+            got = ops.matmul_mx(x, ex, w, ew, dtype=F32)
+            assert bool((got == sign * want).all()), (bx, bw, sign, got.unique(), want)
+
+
+@pytest.mark.parametrize("M,N,blocks", KERNELS)
+def test_product_of_denormal_size(M, N, blocks):
+    """One element of a row each: 0.25 times 2^s is a multiple of 2^-149, float32's smallest number, from s = -147 on, and
+    below half of it nothing is left."""
+    x, ex = ones(M, blocks, 0, 0)
+    w, ew = ones(N, blocks, 0, 0)
+    x[:, 16 * (blocks // 2)] = 1
+    w[:, 16 * (blocks // 2)] = 1
+    for s in range(-154, -120):
+        ex[:] = (s + 254) // 2
+        ew[:] = s + 254 - (s + 254) // 2
+        got = ops.matmul_mx(x, ex, w, ew, dtype=F32).double()
+        want = 2.0 ** (s - 2) if s >= -147 else 0.0
+        if s != -148:  # half of the smallest number may go either way
+            assert bool((got == want).all()), (s, got.unique(), want)
