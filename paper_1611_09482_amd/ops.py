@@ -450,20 +450,6 @@ def matmul_mx(x, x_scale, w, w_scale, row_scale=None, bias=None, dtype=torch.bfl
     return out
 
 
-def _per_row(rows: int, dev: int, *given):
-    """Addresses of `rows` consecutive elements, or None, for each (name, tensor or None, type)."""
-    at = []
-    for name, t, dtype in given:
-        if t is None:
-            at.append(None)
-        elif (isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype == dtype and t.numel() == rows
-              and t.is_contiguous()):
-            at.append(t.data_ptr())
-        else:
-            at.append(_vector(name, t, rows, dtype, dev))  # says what is wrong
-    return at
-
-
 def _one_or_each(name: str, t, dtype, lead, width: int, dev: int):
     """(address, stride) of one row for all (stride 0) or a row for each."""
     if t is None:
@@ -509,9 +495,9 @@ def adjust_logits(logits, tokens=None, lengths=None, prompts=None, repetition=No
             _int32("the history's length", history)
     bp, bstride = _one_or_each("bias", bias, torch.float32, lead, vocab, dev)
     ap, astride = _one_or_each("allowed", allowed, torch.int32, lead, (vocab + 31) // 32, dev)
-    int32, f32 = torch.int32, torch.float32
-    vectors = _per_row(rows, dev, ("lengths", lengths, int32), ("prompts", prompts, int32), ("repetition", repetition, f32),
-                       ("presence", presence, f32), ("frequency", frequency, f32))
+    vectors = [None if t is None else _vector(name, t, rows, dtype, dev) for name, t, dtype in (
+        ("lengths", lengths, torch.int32), ("prompts", prompts, torch.int32), ("repetition", repetition, torch.float32),
+        ("presence", presence, torch.float32), ("frequency", frequency, torch.float32))]
     _check(_library().fwg_adjust_logits(kind, rows, vocab, logits.data_ptr(), stride, history, tp, tstride, *vectors, bp, bstride,
                                         ap, astride, op, ostride, _stream(dev)))
     return out
