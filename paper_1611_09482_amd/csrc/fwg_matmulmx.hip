@@ -365,9 +365,9 @@ template <typename TO, bool ALIGNED, bool STREAM, int T> __global__ void __launc
 }
 
 // Where there are no more tiles of 128 x 128 than compute units: eight waves of 64 outputs x 32 rows, and a ring of four stages in
-// LDS, of which three are on their way while one is multiplied.  333 x 8,000 x 4,096 takes 13.2 us (two groups of four waves
-// with two stages each 15.9; four waves of 64 x 64 16.0), 128 x 8,192 x 4,096 11.6 (14.5), 16 x 32,000 x 4,096 to float32, which
-// memory bounds, 14.4 (4.9 TB/s).  A stage takes 0.5 us: its copies alone 0.44, its reads from LDS and products alone 0.41.
+// LDS, of which three are on their way while one is multiplied.  Elements and scales at random, calls back to back: 333 x 8,000 x
+// 4,096 takes 13.3 us (two groups of four waves with two stages each 15.9; four waves of 64 x 64 16.0), 128 x 8,192 x 4,096 11.5
+// (14.5), 16 x 32,000 x 4,096 to float32, which memory bounds, 15.0 (4.8 TB/s).  A stage takes 0.5 us: its copies alone 0.44, its reads from LDS and products alone 0.41.
 // SUMS: of a part of k, to the workspace.
 constexpr int kRing = 4, kRingT = 128, kRingStage = 2 * kRingT * HK, kRingScales = 2 * kRingT * HB;
 constexpr int kRingLds = kRing * (kRingStage + 2 * kRingScales) + 2 * kRingT * (int)sizeof(float);

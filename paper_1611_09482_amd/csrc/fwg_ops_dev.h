@@ -1,5 +1,5 @@
-// Device helpers of the token operators (fwg_embed.hip, fwg_normq.hip, fwg_matmulq.hip,
-// fwg_logprob.hip): vectors of float32 or bf16 elements at any element address, reductions over a
+// Device helpers of the token operators (fwg_embed.hip, fwg_normq.hip, fwg_matmulq.hip, fwg_mx.hip,
+// fwg_matmulmx.hip, fwg_adjust.hip, fwg_logprob.hip): vectors of float32 or bf16 elements at any element address, reductions over a
 // wavefront.  Not part of the public ABI.
 #pragma once
 
